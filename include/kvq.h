@@ -273,6 +273,62 @@ int kvq_token_features(const void* logits, int logits_are_fp32, int n, int vocab
 int kvq_attend_last(kvq_ctx* ctx, int layer, const void* Q, void* O, int n_queries, void* stream);
 
 /*
+ * Speculative decoding: attention for a TREE of drafted tokens over the cache (Eq. 5 at every node), before any of
+ * them is stored.  Sequence b holds len tokens of `layer` (0 is fine) and n_nodes <= KVQ_MAX_TREE_NODES drafted
+ * nodes; parents (dev int32 [batch][n_nodes]) gives every node's parent, an earlier node, or -1 for a child of the
+ * last cached token.  Any other value (and a descent from one) marks a node that is not in use: its rows of O are
+ * zero and nobody sees it, so sequences may draft trees of different sizes.  The depth of a node is 0 for children
+ * of the last cached token and one more than its parent's below; its position is len + depth.
+ *   Q, O   dev fp16 [batch][n_nodes][q_heads][64]
+ *   K, V   dev fp16 [batch][n_nodes][kv_heads][64], the nodes' own rows
+ *   bits_opt dev uint8 [batch][n_nodes], values in {2,4,8,16}, or NULL.  The rows take part in the attention as they
+ *          would be stored at that bit-width (Eq. 24, then code * scale + zero-point, rounded once to fp16), so that a
+ *          chain of nodes gives what appending them and kvq_attend_last give; NULL: as fp16 rows.  Any other value
+ *          counts as 16 and sets KVQ_FLAG_BAD_BITS.
+ *   window, sinks  window == 0: a node sees every cached token, its ancestors and itself.  window > 0: of those, the
+ *          ones whose position is less than `window` before its own, and the tokens at positions < sinks.
+ * The cache is not changed: append the accepted rows afterwards (kvq_append_ragged).  n_nodes == 0 is a no-op.  One
+ * launch.  Q, K, V, O 16-byte aligned; O may not overlap the inputs.  Caches with one scale group per row only
+ * (kvq_create, kvq_create_arena and their workspace forms); KVQ_ERR_ARG for the other layouts.
+ */
+#define KVQ_MAX_TREE_NODES 64
+int kvq_attend_tree(kvq_ctx* ctx, int layer, const void* Q, const void* K, const void* V, const uint8_t* bits_opt,
+                    const int32_t* parents, int n_nodes, void* O, int window, int sinks, void* stream);
+
+/*
+ * kvq_decode_attn for a sliding-window layer: the query of every sequence's last cached token sees the last `window`
+ * cached tokens (its own included) and the first `sinks` ones, O = Softmax(q K^T / 8) V over those.  Q, O: dev fp16
+ * [batch][q_heads][64], 16-byte aligned.  window >= 1, sinks >= 0 (both may exceed the length).  A sequence of a
+ * ragged layer that holds nothing gets a zero row; KVQ_ERR_EMPTY if none holds a token.  Reads the packed rows inside
+ * the window and the sinks only.  One launch.  Caches with one scale group per row only (KVQ_ERR_ARG otherwise).
+ */
+int kvq_decode_attn_window(kvq_ctx* ctx, int layer, const void* Q, void* O, int window, int sinks, void* stream);
+
+/*
+ * Verification of a tree of drafted tokens against the target's probabilities (speculative sampling), from given
+ * random numbers.  No handle is needed; the buffers belong to the current device.
+ *   target    dev fp32 [batch][n_nodes + 1][vocab]: the target's next-token probabilities after the last cached token
+ *             (row 0) and after node i (row i + 1); finite, not negative
+ *   draft_opt dev fp32, same shape: the distributions the children of row 0 / of node i were drawn from, each child on
+ *             its own; or NULL: the drafted tokens are fixed guesses
+ *   tokens, parents  dev int32 [batch][n_nodes]; parents as in kvq_attend_tree.  A token outside [0, vocab) is turned down
+ *   u_accept  dev fp32 [batch][n_nodes], u_next dev fp32 [batch]: uniform numbers in [0, 1)
+ * From the root, the children of the node reached so far are tested in index order.  Child i with token x is accepted
+ * when u_accept[i] * Z * q(x) < r(x), where r = max(p - c q, 0); before a rejection c = 0 and Z = 1, a rejection sets
+ * c += Z and then Z = sum_v r(v).  (With fixed guesses q(x) = 1, r = p without the tokens turned down, and a rejection
+ * takes r(x) off Z.)  If no child is accepted the next token is the first v whose running sum of r exceeds u_next times
+ * the sum of r (r = p where that sum is zero; -1 if p has no mass either).  So the tokens follow the target's
+ * distribution, whatever the draft's.  Sums are fp64.
+ *   n_accepted dev int32 [batch]; path dev int32 [batch][n_nodes]: the accepted nodes from the root down, then -1;
+ *   next_token dev int32 [batch]
+ * 0 <= n_nodes <= KVQ_MAX_TREE_NODES (0: only the next token is drawn; tokens, parents, u_accept and path may be NULL).
+ * batch == 0 is a no-op.  One launch.
+ */
+int kvq_verify_tree(const float* target, const float* draft_opt, const int32_t* tokens, const int32_t* parents, int batch,
+                    int n_nodes, int vocab, const float* u_accept, const float* u_next, int32_t* n_accepted,
+                    int32_t* path, int32_t* next_token, void* stream);
+
+/*
  * kvq_decode_attn without any buffer that had to be allocated for it.  (No counterpart in
  * the paper: this is a packaging variant of the call above, same arithmetic, same result.)
  *

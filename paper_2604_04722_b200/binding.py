@@ -26,6 +26,7 @@ KVQ_ERR_NOMEM = -7
 KVQ_ERR_TOO_LARGE = -8
 KVQ_STATIC_MAX_PARTIALS = 8192
 KVQ_EXPORT_ROW_BYTES = 128
+KVQ_MAX_TREE_NODES = 64
 
 _vp, _i, _u64p = C.c_void_p, C.c_int, C.POINTER(C.c_uint64)
 
@@ -50,6 +51,9 @@ SIGNATURES = {
     "kvq_decode_attn_var": (_i, [_vp, _i, _vp, _vp, _vp, _vp]),
     "kvq_token_features": (_i, [_vp, _i, _i, _i, _vp, _vp, C.c_uint64, C.c_uint32, _vp, _vp, _vp]),
     "kvq_attend_last": (_i, [_vp, _i, _vp, _vp, _i, _vp]),
+    "kvq_attend_tree": (_i, [_vp, _i, _vp, _vp, _vp, _vp, _vp, _i, _vp, _i, _i, _vp]),
+    "kvq_decode_attn_window": (_i, [_vp, _i, _vp, _vp, _i, _i, _vp]),
+    "kvq_verify_tree": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
     "kvq_decode_attn_static": (_i, [_vp, _i, _vp, _vp, _vp]),
     "kvq_decode_step": (_i, [_vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "kvq_decode_step_host": (_i, [_vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
@@ -241,6 +245,27 @@ def kvq_token_features(logits, logits_are_fp32: bool, n: int, vocab: int, token_
 
 def kvq_attend_last(ctx: int, layer: int, Q, O, n_queries: int, stream=None) -> None:
     check(lib().kvq_attend_last(ctx, layer, _ptr(Q), _ptr(O), n_queries, _stream(stream)), "kvq_attend_last")
+
+
+def kvq_attend_tree(ctx: int, layer: int, Q, K, V, bits, parents, n_nodes: int, O, window: int = 0, sinks: int = 0,
+                    stream=None) -> None:
+    """Attention for a tree of drafted tokens over the cache, none of them stored yet."""
+    check(lib().kvq_attend_tree(ctx, layer, _ptr(Q), _ptr(K), _ptr(V), _ptr(bits), _ptr(parents), n_nodes, _ptr(O),
+                                window, sinks, _stream(stream)), "kvq_attend_tree")
+
+
+def kvq_decode_attn_window(ctx: int, layer: int, Q, O, window: int, sinks: int = 0, stream=None) -> None:
+    """kvq_decode_attn over the last ``window`` cached tokens and the first ``sinks`` ones."""
+    check(lib().kvq_decode_attn_window(ctx, layer, _ptr(Q), _ptr(O), window, sinks, _stream(stream)),
+          "kvq_decode_attn_window")
+
+
+def kvq_verify_tree(target, draft, tokens, parents, batch: int, n_nodes: int, vocab: int, u_accept, u_next, n_accepted,
+                    path, next_token, stream=None) -> None:
+    """Which drafted tokens the target accepts, and the token after them, from given random numbers."""
+    check(lib().kvq_verify_tree(_ptr(target), _ptr(draft), _ptr(tokens), _ptr(parents), batch, n_nodes, vocab,
+                                _ptr(u_accept), _ptr(u_next), _ptr(n_accepted), _ptr(path), _ptr(next_token),
+                                _stream(stream)), "kvq_verify_tree")
 
 
 def kvq_decode_attn_static(ctx: int, layer: int, Q, O, stream=None) -> None:

@@ -8,10 +8,10 @@ import sys
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libkvq.so")
-SOURCES = [os.path.join(CSRC, "kvq.cu")]
+SOURCES = [os.path.join(CSRC, "kvq.cu"), os.path.join(CSRC, "kvq_rows.cu")]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "-shared", "-Xcompiler", "-fPIC", "-Xptxas", "-v",
+    "-Xcompiler", "-fPIC", "-Xptxas", "-v",
 ]
 
 
@@ -37,12 +37,26 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB
     nvcc = os.environ.get("NVCC", "nvcc")
     tmp = LIB + ".tmp.%d" % os.getpid()
-    cmd = [nvcc, *NVCC_FLAGS, "-o", tmp, *SOURCES]
-    proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    if verbose or proc.returncode != 0:
-        sys.stderr.write(proc.stdout)
-    if proc.returncode != 0:
-        raise RuntimeError("nvcc failed (%d): %s" % (proc.returncode, " ".join(cmd)))
+    objects = ["%s.%d.o" % (tmp, i) for i in range(len(SOURCES))]
+    try:
+        # the sources are compiled side by side, then linked
+        jobs = [([nvcc, *NVCC_FLAGS, "-c", "-o", obj, src], subprocess.Popen(
+            [nvcc, *NVCC_FLAGS, "-c", "-o", obj, src], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True))
+            for src, obj in zip(SOURCES, objects)]
+        done = [(cmd, proc.communicate()[0], proc.returncode) for cmd, proc in jobs]
+        if all(rc == 0 for _, _, rc in done):
+            cmd = [nvcc, *NVCC_FLAGS, "-shared", "-o", tmp, *objects]
+            link = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+            done.append((cmd, link.stdout, link.returncode))
+        for cmd, text, rc in done:
+            if verbose or rc != 0:
+                sys.stderr.write(text)
+            if rc != 0:
+                raise RuntimeError("nvcc failed (%d): %s" % (rc, " ".join(cmd)))
+    finally:
+        for obj in objects:
+            if os.path.exists(obj):
+                os.remove(obj)
     os.replace(tmp, LIB)
     return LIB
 

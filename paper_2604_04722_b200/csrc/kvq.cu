@@ -19,6 +19,7 @@
 #include "k_decode.cuh"
 #include "k_export.cuh"
 #include "k_features.cuh"
+#include "kvq_rows.h"
 
 #ifndef KVQ_NVTX
 #define KVQ_NVTX 1                       // NVTX ranges around the entry points that launch the hot kernels
@@ -66,6 +67,9 @@ struct kvq_ctx {
     float* part_s2 = nullptr;            //                [units][partial slots] sum of squared weights (kvq_decode_attn_var)
     float* unit_var = nullptr;           //                [units] variance of a unit's attention weights
     uint32_t* vis = nullptr;             // kvq_attend_last: visible pool fills [batch][query rows of a launch][4]
+    float* rows_o = nullptr;             // many-row attention scratch [records][kRowsMaxRows][64]
+    float2* rows_ml = nullptr;           //                            [records][kRowsMaxRows]
+    uint32_t* rows_cnt = nullptr;        //                            [records] arrival counters, zero between launches
     int splits_override = 0;
     int chunk_override = 0;              // kvq_set_append_chunk: 0 = automatic, else tokens per thread of a prefill chunk
     uint32_t* flags = nullptr;
@@ -200,6 +204,9 @@ void free_all(kvq_ctx* c) {
     cudaFree(c->part_ml);
     cudaFree(c->part_cnt);
     cudaFree(c->vis);
+    cudaFree(c->rows_o);
+    cudaFree(c->rows_ml);
+    cudaFree(c->rows_cnt);
     cudaFree(c->part_s2);
     cudaFree(c->unit_var);
     cudaFree(c->d_lens);
@@ -720,6 +727,10 @@ int create_impl(kvq_ctx** out, int layers, int q_heads, int kv_heads, int head_d
     ok = ok && dev_alloc(c, &c->part_s2, sizeof(float) * max_partial_records(c)) == cudaSuccess;
     ok = ok && dev_alloc(c, &c->unit_var, sizeof(float) * units) == cudaSuccess;
     ok = ok && dev_alloc(c, &c->vis, sizeof(uint32_t) * 4 * (size_t)batch * kMaxQueryRows) == cudaSuccess;
+    const size_t rows_records = rows_max_records(c->sm_count);
+    ok = ok && dev_alloc(c, &c->rows_o, sizeof(float) * rows_records * kRowsMaxRows * kHeadDim) == cudaSuccess;
+    ok = ok && dev_alloc(c, &c->rows_ml, sizeof(float2) * rows_records * kRowsMaxRows) == cudaSuccess;
+    ok = ok && dev_alloc(c, &c->rows_cnt, sizeof(uint32_t) * rows_records) == cudaSuccess;
     ok = ok && dev_alloc(c, &c->d_lens, sizeof(int) * 3 * (size_t)batch * kvq_ctx::kLenSlots) == cudaSuccess;
     ok = ok && dev_alloc(c, &c->flags, sizeof(uint32_t)) == cudaSuccess;
     ok = ok && dev_alloc(c, &c->st_feats, sizeof(float) * 4 * batch) == cudaSuccess;
@@ -756,6 +767,8 @@ int create_impl(kvq_ctx** out, int layers, int q_heads, int kv_heads, int head_d
         ok = ok && cudaMemset(c->chunk_arrivals, 0, sizeof(uint32_t) * batch) == cudaSuccess;
         ok = ok && cudaMemset(c->step_cls, 0, sizeof(uint32_t) * batch) == cudaSuccess;
         ok = ok && cudaMemset(c->part_cnt, 0, sizeof(uint32_t) * units * kMaxQueryRows) == cudaSuccess;
+        ok = ok && cudaMemset(c->rows_cnt, 0, sizeof(uint32_t) * rows_records) == cudaSuccess;
+        ok = ok && rows_setup() == cudaSuccess;
         // the controller block may exceed the default 48 KB of dynamic shared memory
         const int smem_max = (int)controller_smem(kMaxHidden);
         ok = ok && cudaFuncSetAttribute(k_select_bits, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_max) == cudaSuccess;
@@ -1066,6 +1079,85 @@ int kvq_attend_last(kvq_ctx* c, int layer, const void* Q, void* O, int n_queries
     }
     KVQ_CUDA(c, cudaGetLastError());
     return KVQ_OK;
+}
+
+// Shared by kvq_attend_tree and kvq_decode_attn_window: plan, parameters, launch.
+static int rows_impl(kvq_ctx* c, int layer, const void* Q, void* O, const void* K, const void* V, const uint8_t* bits,
+                     const int32_t* parents, int nodes, int window, int sinks, cudaStream_t st) {
+    DeviceGuard guard(c->device);
+    RowsParams p{};
+    p.store = c->store;
+    p.counts = counts_of(c, c->cur[layer], layer);
+    p.Q = static_cast<const __half*>(Q);
+    p.O = static_cast<__half*>(O);
+    p.K = static_cast<const __half*>(K);
+    p.V = static_cast<const __half*>(V);
+    p.bits = bits;
+    p.parents = parents;
+    p.part_o = c->rows_o;
+    p.part_ml = c->rows_ml;
+    p.part_cnt = c->rows_cnt;
+    p.layer = layer;
+    p.group = c->q_heads / c->kv_heads;
+    p.nodes = nodes;
+    p.rows = nodes * p.group;
+    p.window = window;
+    p.sinks = sinks;
+    const int64_t seen = window > 0 ? std::min<int64_t>(c->len[layer], (int64_t)window + sinks) : c->len[layer];
+    const uint64_t pairs = (uint64_t)c->batch * c->kv_heads;
+    const RowsPlan plan = rows_plan(c->sm_count, pairs, p.rows, (int)seen);
+    if (pairs * plan.row_blocks * plan.parts > 0x7fffffffull) return KVQ_ERR_ARG;
+    p.row_blocks = plan.row_blocks;
+    p.parts = plan.parts;
+    rows_launch(p, plan, parents != nullptr, pairs, st);
+    c->launches += 1;
+    KVQ_CUDA(c, cudaGetLastError());
+    return KVQ_OK;
+}
+
+int kvq_attend_tree(kvq_ctx* c, int layer, const void* Q, const void* K, const void* V, const uint8_t* bits_opt,
+                    const int32_t* parents, int n_nodes, void* O, int window, int sinks, void* stream) {
+    TraceRange trace("kvq_attend_tree");
+    if (check_layer(c, layer) != KVQ_OK || n_nodes < 0 || n_nodes > KVQ_MAX_TREE_NODES || window < 0 || sinks < 0) return KVQ_ERR_ARG;
+    if (c->groups != 1) return KVQ_ERR_ARG;            // the kernel reads the fragment layout of one scale group per row
+    if (n_nodes == 0) return KVQ_OK;
+    if (!Q || !K || !V || !parents || !O || !aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O)) return KVQ_ERR_ARG;
+    return rows_impl(c, layer, Q, O, K, V, bits_opt, parents, n_nodes, window, sinks, static_cast<cudaStream_t>(stream));
+}
+
+int kvq_decode_attn_window(kvq_ctx* c, int layer, const void* Q, void* O, int window, int sinks, void* stream) {
+    TraceRange trace("kvq_decode_attn_window");
+    if (check_layer(c, layer) != KVQ_OK || !Q || !O || !aligned16(Q) || !aligned16(O) || window < 1 || sinks < 0) return KVQ_ERR_ARG;
+    if (c->groups != 1) return KVQ_ERR_ARG;
+    if (c->len[layer] == 0) return KVQ_ERR_EMPTY;
+    return rows_impl(c, layer, Q, O, nullptr, nullptr, nullptr, nullptr, 1, window, sinks, static_cast<cudaStream_t>(stream));
+}
+
+int kvq_verify_tree(const float* target, const float* draft_opt, const int32_t* tokens, const int32_t* parents, int batch,
+                    int n_nodes, int vocab, const float* u_accept, const float* u_next, int32_t* n_accepted, int32_t* path,
+                    int32_t* next_token, void* stream) {
+    if (batch < 0 || n_nodes < 0 || n_nodes > KVQ_MAX_TREE_NODES || vocab < 1) return KVQ_ERR_ARG;
+    if (batch == 0) return KVQ_OK;
+    if (!target || !u_next || !n_accepted || !next_token || batch > (1 << 24)) return KVQ_ERR_ARG;
+    if (n_nodes > 0 && (!tokens || !parents || !u_accept || !path)) return KVQ_ERR_ARG;
+    int device = 0, sm_count = 0;
+    if (cudaGetDevice(&device) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, device) != cudaSuccess)
+        return KVQ_ERR_CUDA;
+    VerifyParams p{};
+    p.target = target;
+    p.draft = draft_opt;
+    p.tokens = tokens;
+    p.parents = parents;
+    p.u_accept = u_accept;
+    p.u_next = u_next;
+    p.n_accepted = n_accepted;
+    p.path = path;
+    p.next_token = next_token;
+    p.nodes = n_nodes;
+    p.vocab = vocab;
+    const cudaError_t e = verify_launch(p, batch, sm_count, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? KVQ_OK : KVQ_ERR_CUDA;
 }
 
 // ---- decode attention with its partials in the library image (no allocation at all)
@@ -1510,6 +1602,7 @@ int kvq_recover(kvq_ctx* c) {
     DeviceGuard guard(c->device);
     KVQ_CUDA(c, cudaDeviceSynchronize());
     KVQ_CUDA(c, cudaMemset(c->part_cnt, 0, sizeof(uint32_t) * (size_t)c->batch * c->q_heads * kMaxQueryRows));
+    KVQ_CUDA(c, cudaMemset(c->rows_cnt, 0, sizeof(uint32_t) * rows_max_records(c->sm_count)));
     KVQ_CUDA(c, cudaMemset(c->flags, 0, sizeof(uint32_t)));
     float* base = nullptr;
     if (c->device >= 0 && c->device < KVQ_STATIC_MAX_DEVICES) {
