@@ -412,6 +412,9 @@ int kvq_seq_len(kvq_ctx* ctx, int layer, int* host_len_out);
  * How kvq_decode_attn cuts the work: 0 = automatic (default): one launch of as many warps as
  * stay resident on the device, each taking an equal share of all (sequence, query head)
  * units; 1..64 = every unit is cut into exactly that many equal parts, one warp each.
+ * kvq_attend_tree and kvq_decode_attn_window follow it too (a unit there is a block of rows of a
+ * (sequence, KV head) pair; the number is rounded up to whole CTAs of four warps, and down to
+ * what the handle's partial records hold).
  */
 int kvq_set_splits(kvq_ctx* ctx, int splits);
 

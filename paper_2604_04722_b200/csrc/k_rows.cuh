@@ -6,27 +6,35 @@
 //
 // The decode kernel (k_decode.cuh) gives every (sequence, query head) its own walk over the cache, which is right for
 // one row.  Here the rows of a tree and the heads of a group share a walk: a unit is (sequence, KV head, block of up
-// to 16 or 32 rows), row = node * group + head, and both products run on the fp16 matrix instructions with the rows as
-// the 16-row operand (mma.sync m16n8k16, fp32 accumulation):
-//   S[row][slot] = sum_i q_i c_i        columns = slots of a 16-slot tile (two column groups of 8)
-//   O[row][channel] += sum_slot w c     columns = channels
-// with the packed codes as the column operand of both.  The fragment layout of the store (kvq_common.cuh) has, in
-// lane (g, q), the codes of slots g and g + 8, and for V of slots 4q .. 4q + 3: a column operand needs exactly those
-// bytes, two 16-bit lanes per register.
+// to 8 or 16 rows), row = node * group + head, and both products run on the fp16 matrix instructions with the rows as
+// the 8 columns (mma.sync m16n8k16, fp32 accumulation):
+//   S[slot][row] = sum_i c_i q_i            16 rows = the slots of a tile
+//   O[channel][row] += sum_slot c w         16 rows = channels, four products for the 64 of a head
+// with the packed codes as the 16-row operand of both.  The fragment layout of the store (kvq_common.cuh) has, in lane
+// (g, q), the codes of slots g and g + 8, and for V of slots 4q .. 4q + 3: the operand needs exactly those bytes, two
+// 16-bit lanes per register.  The weights of a tile leave the softmax with slots as rows and enter the second product
+// with slots as columns: one 8x8 transposition (movmatrix) per eight slots.  Eight columns instead of sixteen rows
+// keep a decode step of three grouped heads at half the matrix instructions, and the scales belong to slots g and
+// g + 8 of a lane alone.
 //
-// Unpacking costs one AND per two codes: a field cut out in place at bit k <= 8 of a 16-bit lane IS the fp16 number
+// Unpacking K costs one AND per two codes: a field cut out in place at bit k <= 8 of a 16-bit lane IS the fp16 number
 // code * 2^(k-24) (a subnormal: that encoding is linear), and the matrix instruction takes subnormals exactly.  The
-// power 2^-k is undone on the other operand (K: the query of the channel is scaled by 2^-k when the row operand is
-// built) or on the accumulators (V: they move to the class's units when a pool is entered).  Both factors of the K
-// product are exact (the query is only scaled by powers of two), so a logit
+// power 2^-k is undone on the query's side.  Both factors are exact (the query is only scaled by powers of two), so a
+// logit
 //   y = log2(e)/8 * (s_k * sum_i q_i c_i + z_k * sum_i q_i)
-// carries fp32 accumulation error only.  On the V side the weight w = p * s_v * G is rounded once to fp16 (half a
-// step, 2^-11 relative at most: the rounding that the fp16 matrix operand forces; it is smaller than the final
-// rounding of the output), G a power of two that the warp picks so that the largest weight sits at 2^13: a weight
-// loses bits only when it is 2^27 times smaller than that.  The sums of p and of p * z_v stay in fp32.
+// carries fp32 accumulation error only.  V codes are cut out the same
+// way, but as prefixes of their byte (c0, c0 + 4 c1, ...: the last needs no AND at all), which the accumulators undo
+// when the pool is left.  The weight w = p * s_v is rounded once to fp16 (by at most 2^-11 of its value: the rounding
+// that the fp16 operand forces).  What that does is made to act on centred codes:
+//   sum p (s c + z) = sum w (c - mid) + sum p (z + mid s),   mid = 2^(bits-1),
+// with the same rounded w in both terms of (c - mid).  With channels far larger than the others in a row (keys and
+// values have such) c is near the middle of its range for all the ordinary channels, and the rounding of w would
+// otherwise act on the middle instead of on the value.  The sums of p, of p (z + mid s) and of mid w stay in fp32.
 //
-// The softmax statistics are kept per row and warp with a lazy maximum: a logit may exceed it by 2^8 before the
-// accumulators are rescaled, which one vote per tile decides.
+// Softmax reference.  p = 2^(y - m), m kept per row and warp.  m is no running maximum: it is moved only when some w
+// overflows fp16 (one vote per tile decides), and then to where the row's largest w of the tile is 2^4.  So logits may
+// grow by 2^11 or so before anything is rescaled -- with sixteen rows, a reference that followed every new maximum was
+// moved on a fifth of all tiles -- and w keeps all its bits down to 2^-18 of the row's largest.
 //
 // Work split: the tiles of a unit (of its four pools laid end to end, a tile weighted by its cost) are cut into
 // parts * 4 equal shares, one per warp.  A warp streams its share through its own ring of bulk copies, as in the decode
@@ -50,30 +58,53 @@ namespace kvq {
 
 constexpr int kRowsWarps = 4, kRowsThreads = kRowsWarps * 32;
 constexpr int kRowsStages = 2;
-constexpr int kRowsStageBytes = 4352;                  // 6 / 3 / 2 / 1 tiles of the four classes
+constexpr int kRowsStageBytes = 4608;
 constexpr int kRowsOutStride = kHeadDim + 4;           // floats per row of the merge buffer
 constexpr int kRowsQStride = kHeadDim + 8;             // halves per row of the query block
-__host__ __device__ constexpr int kRowsTps(int c) { return kRowsStageBytes / pool_rec_bytes(c); }
+// Tiles of class c that a chunk holds at most.
+__host__ __device__ constexpr int kRowsTps(int c) { return c == 0 ? 6 : c == 1 ? 4 : c == 2 ? 2 : 1; }
+static_assert(6 * pool_rec_bytes(0) <= kRowsStageBytes && 4 * pool_rec_bytes(1) <= kRowsStageBytes &&
+              2 * pool_rec_bytes(2) <= kRowsStageBytes && pool_rec_bytes(3) <= kRowsStageBytes, "a chunk fits a stage");
 constexpr int kDraftTileBytes = 4096;                  // one fp16 tile: K units, then V units
 // What a tile of each class costs a warp, for cutting a unit into equal shares.
 __device__ constexpr uint32_t kRowsTileCost[kNumPools] = {6u, 7u, 9u, 12u};
-constexpr float kWeightTop = 8192.0f;                  // the largest weight of a warp's grid choice, 2^13
-constexpr float kGridStart = 1.0995116277760000e12f;   // 2^40: any weight overflows it, so the first tile picks a grid
+constexpr int kWeightTop = 4;                          // log2 of a row's largest weight when its reference is set
 
-template <int MT>
+// Resident CTAs per SM that the kernel is compiled for (registers): 8 rows per unit, 16 rows per unit.
+#ifndef KVQ_ROWS_CTAS1
+#define KVQ_ROWS_CTAS1 4
+#endif
+#ifndef KVQ_ROWS_CTAS2
+#define KVQ_ROWS_CTAS2 4
+#endif
+__host__ __device__ constexpr int rows_ctas_per_sm(int nt) { return nt == 1 ? KVQ_ROWS_CTAS1 : KVQ_ROWS_CTAS2; }
+// NT: blocks of 8 rows per unit.
+template <int NT>
 __host__ __device__ constexpr size_t rows_smem_bytes(int draft_tiles) {
-    return (size_t)kRowsWarps * kRowsStages * kRowsStageBytes + (size_t)kNumPools * MT * 4 * 32 * 16 +
+    return (size_t)kRowsWarps * kRowsStages * kRowsStageBytes + (size_t)kNumPools * NT * 2 * 32 * 16 +
            (size_t)draft_tiles * kDraftTileBytes;
 }
-static_assert((size_t)kRowsWarps * 2 * 16 * kRowsOutStride * 4 <= (size_t)kRowsWarps * kRowsStages * kRowsStageBytes,
+static_assert(kRowsWarps * kRowsMaxRows * kRowsOutStride * 4 <= kRowsWarps * kRowsStages * kRowsStageBytes,
               "the merge buffer lives in the rings");
 
 // ---------------------------------------------------------------- small pieces
 
-__device__ __forceinline__ void mma_f16(float (&d)[4], const uint4& a, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// d = a b
+__device__ __forceinline__ void mma_f16_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+// 8x8 matrix of 16-bit elements, lane (g, q) holding row g, columns 2q and 2q + 1: its transpose.
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+    return d;
 }
 __device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel) {
     uint32_t d;
@@ -114,6 +145,10 @@ __device__ __forceinline__ uint32_t pack_half2(float2 v) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 __device__ __forceinline__ float2 unpack_half2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
+__device__ __forceinline__ uint32_t max_half2(uint32_t a, uint32_t b) {
+    const __half2 m = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&m);
+}
 __device__ __forceinline__ float two_to(int e) { return __int_as_float((127 + e) << 23); }
 
 // The slot of the first token of class c at a position >= p of a sequence of len tokens (n_c if there is none), for the
@@ -136,148 +171,149 @@ __device__ __forceinline__ uint32_t first_slot_from(const uint32_t* idx, int p, 
     return n_c;
 }
 
-template <int MT>
+// Chunks of a warp's share are planned 32 at most at a time, a lane each.
+struct RowsChunks {
+    uint4 chunk[32];               // x, y: source address; z: first tile, class in the top bits; w: bytes | tiles << 16 | mask of edge tiles << 20
+    int seg, tile;                 // range of the share and tile that the next plan starts with
+};
+
+template <int NT>
 struct RowsScratch {
+    static constexpr int ROWS = 8 * NT;
     uint64_t bars[kRowsWarps][kRowsStages];
     unsigned long long anc[kMaxTreeNodes];             // a node and its ancestors
     unsigned long long vis[kMaxTreeNodes];             // those of them that it sees (0: the node is not used)
     unsigned long long step_bits[kNumPools];           // class c among the 64 positions after the first window start
     unsigned long long used;                           // nodes that are used
+    alignas(16) RowsChunks plan[kRowsWarps];
+    uint2 chunk[kRowsWarps][kRowsStages];              // what a stage holds: z, and w >> 16, of its chunk
+    int in_sinks[kNumPools], from[kNumPools], full[kNumPools];     // tiles that every row sees whole: [0, in_sinks), [from, full)
     int seg_lo[kRowsWarps][2 * kNumPools], seg_hi[kRowsWarps][2 * kNumPools];   // tile ranges of a warp's share
     uint32_t cnt[kNumPools], sink[kNumPools], start[kNumPools];   // pool fills; slots before the sinks' end; first window slot
-    uint32_t lo_row[kNumPools][16 * MT];               // first window slot of every row
-    float2 ml[kRowsWarps][16 * MT];
-    float sumq[16 * MT];                               // log2(e)/8 * sum_i q_i
+    uint32_t lo_row[kNumPools][ROWS];               // first window slot of every row
+    float2 ml[kRowsWarps][ROWS];
+    float sumq[ROWS];                               // log2(e)/8 * sum_i q_i
     float wmax[kRowsWarps];
-    int16_t node[16 * MT];                             // node of a row, -1 behind the last
+    int16_t node[ROWS];                             // node of a row, -1 behind the last
     int8_t link[kMaxTreeNodes], bad[kMaxTreeNodes];
     uint32_t last;
-    alignas(16) __half q[16 * MT][kRowsQStride];
+    alignas(16) __half q[ROWS][kRowsQStride];
 };
 
-// Softmax state of a warp: per lane rows g (r = 0) and g + 8 (r = 1) of every 16-row block.
-template <int MT>
+// Softmax state of a warp: per lane rows 2q and 2q + 1 (the two halves of a pair) of every block of eight.
+template <int NT>
 struct RowsState {
-    float m[MT][2];                // running maximum, log2 units
-    float2 l2[MT][2], b2[MT][2];   // sum of p, sum of p * zero-point, over the lane's columns (two chains)
-    float acc[MT][8][4];           // output accumulators: column group (i, j) = i * 4 + j, channel 4 (column + 8 i) + j
-    float grid;                    // G
+    float2 negm[NT];               // minus the reference m of the row, log2 units
+    float2 sumq[NT];               // log2(e)/8 * sum_i q_i
+    float2 l[NT], b[NT];           // sum of p, sum of p * (centred zero-point), over the lane's slots
+    float acc[NT][4][4];           // output: [j][0, 1] channel 4 g + j, [j][2, 3] channel 32 + 4 g + j, of the two rows
 };
 
-// What the columns of a tile carry, this lane's: column group i, slots 8 i + 2 q and + 1.
-struct TileCols {
-    float2 sk[2], zk[2];           // scale (times the common factor of the K product) and zero-point of K
-    float2 sv[2], zv[2];
+// What the K side of a tile leaves for the softmax: products of slots g (s = 0) and g + 8 (s = 1) with rows 2q and 2q + 1 in
+// D[nt][2 s], [2 s + 1], and what the two slots carry.
+template <int NT>
+struct TileLogits {
+    float D[NT][4];
+    float sk[2], zk[2];            // scale (times the common factor of the K product) and zero-point of K
+    float sv[2], zv[2];            // scale and centred zero-point of V
+    float mid;                     // the code that V is centred on
 };
 
-// From the products D to the fp16 row operand of the V product.  EDGE: `seen` bit (2 i + x) of [mt][r] says whether that
-// row sees that slot.
-template <int MT, bool PLAIN>
-__device__ __forceinline__ void weigh(RowsState<MT>& st, const float (&D)[MT][2][4], const TileCols& tc, const float (&sumq)[MT][2],
-                                      bool edge, const uint32_t (&seen)[MT][2], uint4 (&w)[MT]) {
-    auto logits = [&](float2 (&y)[MT][2][2], bool relative) {
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// Logits of a tile, relative to the references or as they are.
+template <int NT>
+__device__ __forceinline__ void logits_of(const RowsState<NT>& st, const TileLogits<NT>& t, bool relative, float2 (&y)[NT][2]) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int r = 0; r < 2; ++r)
+        for (int s = 0; s < 2; ++s)
+            y[n][s] = fma2v(make_float2(t.D[n][2 * s], t.D[n][2 * s + 1]), both(t.sk[s]),
+                            fma2v(both(t.zk[s]), st.sumq[n], relative ? st.negm[n] : both(0.f)));
+}
+// From relative logits y to p = 2^y and the fp16 weights; false if a weight overflows.  (Every scale is at least 2^-24, see
+// k_side, so that p itself stays far from the end of fp32.)
+template <int NT>
+__device__ __forceinline__ bool weigh(const TileLogits<NT>& t, float2 (&y)[NT][2], uint32_t (&w)[NT][2]) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const float base = relative ? -st.m[mt][r] : 0.f, s = sumq[mt][r];
-                    const float2 t = PLAIN ? make_float2(base, base) : fma2v(tc.zk[i], make_float2(s, s), make_float2(base, base));
-                    y[mt][r][i] = fma2v(make_float2(D[mt][i][2 * r], D[mt][i][2 * r + 1]), tc.sk[i], t);
-                    if (edge) {
-                        if (!((seen[mt][r] >> (2 * i)) & 1u)) y[mt][r][i].x = -INFINITY;
-                        if (!((seen[mt][r] >> (2 * i)) & 2u)) y[mt][r][i].y = -INFINITY;
-                    }
-                }
-    };
-    auto top_of = [&](const float2 (&y)[2]) { return fmaxf(fmaxf(y[0].x, y[0].y), fmaxf(y[1].x, y[1].y)); };
-    auto weights = [&](const float2 (&p)[MT][2][2]) {
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            uint32_t h[2][2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float2 sg = PLAIN ? make_float2(st.grid, st.grid) : mul2v(tc.sv[i], make_float2(st.grid, st.grid));
-#pragma unroll
-                for (int r = 0; r < 2; ++r) h[r][i] = pack_half2(mul2v(p[mt][r][i], sg));
-            }
-            w[mt] = make_uint4(h[0][0], h[1][0], h[0][1], h[1][1]);
+        for (int s = 0; s < 2; ++s) {
+            y[n][s] = make_float2(fast_exp2(y[n][s].x), fast_exp2(y[n][s].y));
+            w[n][s] = pack_half2(mul2v(y[n][s], both(t.sv[s])));
         }
-    };
-    float2 p[MT][2][2];
-    logits(p, true);
-    float top = top_of(p[0][0]);
-    uint32_t big = 0;
+    uint32_t big = max_half2(w[0][0], w[0][1]);
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int n = 1; n < NT; ++n) big = max_half2(big, max_half2(w[n][0], w[n][1]));
+    // weights are not negative; a bit pattern of 0x7c00 or above is an overflow
+    return !__any_sync(0xffffffffu, (big + 0x04000400u) & 0x80008000u);
+}
+// The tile's part of the sums of p and p (z + mid s) - w mid; w becomes the column operand of the V product.
+template <int NT>
+__device__ __forceinline__ void add_tile(RowsState<NT>& st, const TileLogits<NT>& t, const float2 (&p)[NT][2], uint32_t (&w)[NT][2]) {
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            top = fmaxf(top, top_of(p[mt][r]));
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) p[mt][r][i] = make_float2(fast_exp2(p[mt][r][i].x), fast_exp2(p[mt][r][i].y));
+        for (int s = 0; s < 2; ++s) {
+            st.l[n] = add2v(st.l[n], p[n][s]);
+            st.b[n] = fma2v(unpack_half2(w[n][s]), both(-t.mid), fma2v(p[n][s], both(t.zv[s]), st.b[n]));
+            w[n][s] = transpose8(w[n][s]);             // (slot g: rows 2q, 2q + 1) -> (row g: slots 2q, 2q + 1)
         }
-    weights(p);
-    // weights are not negative, so their bit patterns are ordered; 0x7c00 and above is an overflow
+}
+// Where `edge` holds, bit (2 s + x) of seen[nt] says whether row 2q + x sees slot g + 8 s.
+template <int NT>
+__device__ __forceinline__ void hide(bool edge, const uint32_t (&seen)[NT], float2 (&y)[NT][2]) {
+    if (!edge) return;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) big = __vmaxu2(__vmaxu2(big, __vmaxu2(w[mt].x, w[mt].y)), __vmaxu2(w[mt].z, w[mt].w));
-    if (__builtin_expect(__any_sync(0xffffffffu, top > kRescaleSlack || ((big + 0x04000400u) & 0x80008000u)), 0)) {
-        // rare: raise the maxima of all rows, choose the grid anew, do the tile again
-        logits(p, false);
-        float most = 0.f;
-        float f[MT][2];
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int s = 0; s < 2; ++s) {
+            if (!((seen[n] >> (2 * s)) & 1u)) y[n][s].x = -INFINITY;
+            if (!((seen[n] >> (2 * s)) & 2u)) y[n][s].y = -INFINITY;
+        }
+}
+// Moves the references of the rows that this tile makes overflow (or nearly: those whose largest weight is above 2^kWeightTop).
+template <int NT>
+__device__ __forceinline__ void move_references(RowsState<NT>& st, const TileLogits<NT>& t, bool edge, const uint32_t (&seen)[NT]) {
+    float2 y[NT][2];
+    logits_of(st, t, false, y);
+    hide(edge, seen, y);
+    const float lg[2] = {__log2f(t.sv[0]), __log2f(t.sv[1])};
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                float t = top_of(p[mt][r]);
-                t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
-                t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
-                const float m = fmaxf(st.m[mt][r], t);
-                f[mt][r] = fast_exp2(st.m[mt][r] - m);
-                st.m[mt][r] = m;
-                st.l2[mt][r] = mul2v(st.l2[mt][r], make_float2(f[mt][r], f[mt][r]));
-                st.b2[mt][r] = mul2v(st.b2[mt][r], make_float2(f[mt][r], f[mt][r]));
+    for (int n = 0; n < NT; ++n) {
+        float2 m = make_float2(fmaxf(y[n][0].x + lg[0], y[n][1].x + lg[1]), fmaxf(y[n][0].y + lg[0], y[n][1].y + lg[1]));
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    p[mt][r][i] = make_float2(fast_exp2(p[mt][r][i].x - m), fast_exp2(p[mt][r][i].y - m));
-                    const float2 v = PLAIN ? p[mt][r][i] : mul2v(p[mt][r][i], tc.sv[i]);
-                    most = fmaxf(most, fmaxf(v.x, v.y));
-                }
-            }
-        most = warp_max(most);
-        // G = 2^13 / (the power of two at or below the largest weight); weights of nothing but zeros keep the grid
-        float grid = st.grid;
-        if (most > 0.f) grid = fminf(kWeightTop / __uint_as_float(__float_as_uint(fmaxf(most, 1e-30f)) & 0x7f800000u), kGridStart);
-        const float g = grid / st.grid;                // a power of two
-        st.grid = grid;
+        for (int d = 4; d < 32; d <<= 1) {
+            m.x = fmaxf(m.x, __shfl_xor_sync(0xffffffffu, m.x, d));
+            m.y = fmaxf(m.y, __shfl_xor_sync(0xffffffffu, m.y, d));
+        }
+        // (a row that sees nothing here has m = -inf and keeps its reference)
+        m = make_float2(fmaxf(-st.negm[n].x, m.x - kWeightTop), fmaxf(-st.negm[n].y, m.y - kWeightTop));
+        const float2 f = make_float2(fast_exp2(-st.negm[n].x - m.x), fast_exp2(-st.negm[n].y - m.y));
+        st.negm[n] = make_float2(-m.x, -m.y);
+        st.l[n] = mul2v(st.l[n], f);
+        st.b[n] = mul2v(st.b[n], f);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int n = 0; n < 8; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) st.acc[mt][n][e] *= f[mt][e >> 1] * g;
-        weights(p);
+            for (int e = 0; e < 4; ++e) st.acc[n][j][e] *= (e & 1) ? f.y : f.x;
     }
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int r = 0; r < 2; ++r)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                st.l2[mt][r] = add2v(st.l2[mt][r], p[mt][r][i]);
-                if (!PLAIN) st.b2[mt][r] = fma2v(p[mt][r][i], tc.zv[i], st.b2[mt][r]);
-            }
 }
 
 // ---------------------------------------------------------------- tile consumers (lane = 4 g + q)
 
-// A quantized class.  kw / vw: words of the fragment layout (see kvq_common.cuh).
+// The query as the column operand of step s: qf[nt][s >> 1], words 2 (s & 1) and + 1.
+template <int NT>
+using RowsQuery = uint4[NT][2];
+__device__ __forceinline__ uint32_t query_word(const uint4& v, int k) { return k == 0 ? v.x : k == 1 ? v.y : k == 2 ? v.z : v.w; }
+
+// A quantized class.  kw, va, vb: words of the fragment layout (see kvq_common.cuh).
 template <int CLS>
 struct RowsQuant {
-    static constexpr int BITS = pool_bits(CLS), REC = pool_rec_bytes(CLS);
+    static constexpr int BITS = pool_bits(CLS);
     static constexpr int NW = 2 << CLS;                // words per lane of one tensor: 2, 4, 8
     static constexpr uint32_t MASK = CLS == 0 ? 0x00030003u : CLS == 1 ? 0x000f000fu : 0x00ff00ffu;
+    static constexpr float MID = (float)(1 << (BITS - 1));
 
     // Register r of step s of the K product: channel of 16-bit lane x, and the bit its field is cut out at.
     __device__ static constexpr int k_channel(int s, int r, int q, int x) {
@@ -288,7 +324,7 @@ struct RowsQuant {
     __device__ static constexpr int k_bit(int s, int r) {
         return CLS == 0 ? 2 * ((2 * s + r) & 3) : CLS == 1 ? 4 * r : 0;
     }
-    // The column operand of slot g + 8 i for step s, register r.
+    // The codes of slot g + 8 i for step s, register r.
     __device__ static __forceinline__ uint32_t k_operand(const uint32_t (&kw)[NW], int i, int s, int r) {
         if (CLS == 0) {
             const int e = 2 * s + r;
@@ -298,12 +334,8 @@ struct RowsQuant {
             const uint32_t w = kw[(s >> 1) * 2 + i];
             return ((s & 1) ? w >> 8 : w) & (MASK << (4 * r));
         }
-        const uint32_t w = kw[s * 2 + i];
-        return r ? (w >> 8) & MASK : w & MASK;
+        return prmt(kw[s * 2 + i], 0u, r ? 0x4341u : 0x4240u);
     }
-    // Bit of the V field of column group (i, j).
-    __device__ static constexpr int v_bit(int j) { return CLS == 0 ? 2 * j : CLS == 1 ? 4 * (j & 1) : 0; }
-
     __device__ static __forceinline__ void load_words(const uint8_t* codes, int lane, uint32_t (&w)[NW]) {
         if (CLS == 0) {
             const uint2 v = *reinterpret_cast<const uint2*>(codes + lane * 8);
@@ -317,111 +349,160 @@ struct RowsQuant {
         }
     }
 
-    template <int MT>
-    __device__ static __forceinline__ void tile(const uint8_t* rec, int lane, const uint4 (&qf)[MT][4], float kfactor,
-                                                const float (&sumq)[MT][2], RowsState<MT>& st, bool edge,
-                                                const uint32_t (&seen)[MT][2], uint32_t) {
-        const int g = lane >> 2, q = lane & 3;
+    template <int NT>
+    __device__ static __forceinline__ void k_side(const uint8_t* rec, int lane, const RowsQuery<NT>& qf, float kfactor, TileLogits<NT>& t) {
+        const int g = lane >> 2;
         uint32_t kw[NW];
         load_words(rec, lane, kw);
-        TileCols tc;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint2 km = *reinterpret_cast<const uint2*>(rec + meta_offset(CLS, 0, 8 * i + 2 * q));
-            const uint2 vm = *reinterpret_cast<const uint2*>(rec + meta_offset(CLS, 1, 8 * i + 2 * q));
-            const float2 k0 = unpack_half2(km.x), k1 = unpack_half2(km.y), v0 = unpack_half2(vm.x), v1 = unpack_half2(vm.y);
-            tc.sk[i] = mul2v(make_float2(k0.x, k1.x), make_float2(kfactor, kfactor));
-            tc.zk[i] = make_float2(k0.y, k1.y);
-            tc.sv[i] = make_float2(v0.x, v1.x);
-            tc.zv[i] = make_float2(v0.y, v1.y);
+        for (int s = 0; s < 2; ++s) {
+            const float2 km = unpack_half2(*reinterpret_cast<const uint32_t*>(rec + meta_offset(CLS, 0, g + 8 * s)));
+            const float2 vm = unpack_half2(*reinterpret_cast<const uint32_t*>(rec + meta_offset(CLS, 1, g + 8 * s)));
+            t.sk[s] = km.x * (kfactor * 16777216.0f);
+            t.zk[s] = km.y;
+            // A constant row has scale zero and codes zero.  It is read with a scale of 2^-24, the smallest there is, which
+            // its codes multiply by zero all the same: s (c - mid) + (z + mid s) = z.
+            t.sv[s] = fmaxf(vm.x, 5.9604645e-8f);
+            t.zv[s] = fmaf(t.sv[s], MID, vm.y);
         }
-        float D[MT][2][4];
+        t.mid = MID;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int s = 0; s < 4; ++s) {
+            const uint32_t a[4] = {k_operand(kw, 0, s, 0), k_operand(kw, 1, s, 0), k_operand(kw, 0, s, 1), k_operand(kw, 1, s, 1)};
 #pragma unroll
-            for (int i = 0; i < 2; ++i) D[mt][i][0] = D[mt][i][1] = D[mt][i][2] = D[mt][i][3] = 0.f;
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint32_t b0 = k_operand(kw, i, s, 0), b1 = k_operand(kw, i, s, 1);
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) mma_f16(D[mt][i], qf[mt][s], b0, b1);
+            for (int n = 0; n < NT; ++n) {
+                const uint32_t b0 = query_word(qf[n][s >> 1], 2 * (s & 1)), b1 = query_word(qf[n][s >> 1], 2 * (s & 1) + 1);
+                if (s == 0) mma_f16_first(t.D[n], a, b0, b1);
+                else mma_f16(t.D[n], a, b0, b1);
             }
+        }
+    }
+    template <int NT>
+    __device__ static __forceinline__ void v_side(const uint8_t* rec, int lane, RowsState<NT>& st, const uint32_t (&w)[NT][2], uint32_t) {
+        const int g = lane >> 2, q = lane & 3;
         // V words of slots 2q, 2q + 1 (a) and 8 + 2q, 9 + 2q (b): halves of the words of slot quads q >> 1 and 2 + (q >> 1)
         uint32_t va[NW], vb[NW];
         load_words(rec + pool_codes_bytes(CLS), 4 * g + (q >> 1), va);
         load_words(rec + pool_codes_bytes(CLS), 4 * g + 2 + (q >> 1), vb);
-        uint4 w[MT];
-        weigh<MT, false>(st, D, tc, sumq, edge, seen, w);
         const uint32_t sel = (q & 1) ? 0x4342u : 0x4140u;
+        constexpr int PER = 8 / BITS;                              // channels per byte
 #pragma unroll
-        for (int k = 0; k < NW; ++k) {                 // word k: CLS 0: i = k; CLS 1, 2: (byte of the group) * 2 + i
-            const uint32_t xa = prmt(va[k], 0u, sel), xb = prmt(vb[k], 0u, sel);
-            const int i = CLS == 0 ? k : k & 1, byte = CLS == 0 ? 0 : k >> 1;
-            constexpr int PER = 8 / BITS;              // channels per byte
+        for (int byte = 0; byte < 4 / PER; ++byte) {               // word of channel group i: CLS 0: i, CLS 1, 2: 2 byte + i
+            uint32_t x[4];                             // x0: channel group 0, slots 2q ..; x1: group 1; x2, x3: slots 8 + 2q ..
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] = prmt((k >> 1) ? vb[2 * byte + (k & 1)] : va[2 * byte + (k & 1)], 0u, sel);
 #pragma unroll
             for (int f = 0; f < PER; ++f) {
-                const int n = i * 4 + byte * PER + f;
-                const uint32_t b0 = PER == 1 ? xa : xa & (MASK << (BITS * f)), b1 = PER == 1 ? xb : xb & (MASK << (BITS * f));
+                const uint32_t prefix = ((1u << (BITS * (f + 1))) - 1u) * 0x00010001u;
+                uint32_t a[4];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) mma_f16(st.acc[mt][n], w[mt], b0, b1);
+                for (int k = 0; k < 4; ++k) a[k] = f + 1 == PER ? x[k] : x[k] & prefix;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) mma_f16(st.acc[n][byte * PER + f], a, w[n][0], w[n][1]);
             }
         }
     }
 };
 
-// fp16 rows: the fp16 pool, and the drafted tokens.  valid: bit (2 i + x) says that the lane's slot holds a row (the
-// bytes of other slots may be anything, an Inf or NaN pattern included).
+// fp16 rows: the fp16 pool, and the drafted tokens.
 struct RowsFp16 {
-    static constexpr int REC = pool_rec_bytes(3);
     __device__ static constexpr int k_channel(int s, int r, int q, int x) { return 8 * (2 * s + r) + 2 * q + x; }
 
-    template <int MT>
-    __device__ static __forceinline__ void tile(const uint8_t* rec, int lane, const uint4 (&qf)[MT][4], float kfactor,
-                                                const float (&sumq)[MT][2], RowsState<MT>& st, bool edge,
-                                                const uint32_t (&seen)[MT][2], uint32_t valid) {
-        const int g = lane >> 2, q = lane & 3;
-        float D[MT][2][4];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) D[mt][i][0] = D[mt][i][1] = D[mt][i][2] = D[mt][i][3] = 0.f;
+    template <int NT>
+    __device__ static __forceinline__ void k_side(const uint8_t* rec, int lane, const RowsQuery<NT>& qf, float kfactor, TileLogits<NT>& t) {
         const int row = lane & 7, mat = lane >> 3;
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {                  // four 8x8 matrices: (unit 2s, 2s + 1) x (slots 0..7, 8..15)
-            uint32_t b[4];
-            ldsm_x4(b, rec + ((2 * s + (mat & 1)) * kTileTokens + 8 * (mat >> 1) + row) * 16);
+        for (int s = 0; s < 4; ++s) {                  // four 8x8 matrices: (slots 0..7, 8..15) x (unit 2s, 2s + 1)
+            uint32_t a[4];
+            ldsm_x4(a, rec + ((2 * s + (mat >> 1)) * kTileTokens + 8 * (mat & 1) + row) * 16);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) mma_f16(D[mt][i], qf[mt][s], b[2 * i], b[2 * i + 1]);
+            for (int n = 0; n < NT; ++n) {
+                const uint32_t b0 = query_word(qf[n][s >> 1], 2 * (s & 1)), b1 = query_word(qf[n][s >> 1], 2 * (s & 1) + 1);
+                if (s == 0) mma_f16_first(t.D[n], a, b0, b1);
+                else mma_f16(t.D[n], a, b0, b1);
+            }
         }
-        TileCols tc;
-        tc.sk[0] = tc.sk[1] = make_float2(kfactor, kfactor);
-        uint4 w[MT];
-        weigh<MT, true>(st, D, tc, sumq, edge, seen, w);
+        t.sk[0] = t.sk[1] = kfactor;
+        t.sv[0] = t.sv[1] = 1.f;
+        t.zk[0] = t.zk[1] = t.zv[0] = t.zv[1] = t.mid = 0.f;
+    }
+    // valid: bit k says that slot 2 q + (k & 1) + 8 (k >> 1) holds a row (the bytes of other slots may be anything, an Inf
+    // or NaN pattern included, which a weight of zero would not silence).
+    template <int NT>
+    __device__ static __forceinline__ void v_side(const uint8_t* rec, int lane, RowsState<NT>& st, const uint32_t (&w)[NT][2], uint32_t valid) {
+        const int g = lane >> 2, q = lane & 3;
         const uint8_t* v = rec + pool_codes_bytes(3) + (g >> 1) * kTileTokens * 16 + (g & 1) * 8;
+        uint2 x[2][4];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {                  // channels 32 i + 4 g .. + 3 of the lane's four slots
-            uint2 x[4];
+        for (int i = 0; i < 2; ++i)                    // channels 32 i + 4 g .. + 3 of the lane's four slots
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int slot = 2 * q + (k & 1) + 8 * (k >> 1);
-                x[k] = *reinterpret_cast<const uint2*>(v + (i * 4 * kTileTokens + slot) * 16);
-                if (edge && !((valid >> k) & 1u)) x[k] = make_uint2(0u, 0u);
+                x[i][k] = (valid >> k) & 1u ? *reinterpret_cast<const uint2*>(v + (i * 4 * kTileTokens + slot) * 16) : make_uint2(0u, 0u);
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t sel = (j & 1) ? 0x7632u : 0x5410u;
-                const uint32_t b0 = j < 2 ? prmt(x[0].x, x[1].x, sel) : prmt(x[0].y, x[1].y, sel);
-                const uint32_t b1 = j < 2 ? prmt(x[2].x, x[3].x, sel) : prmt(x[2].y, x[3].y, sel);
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t sel = (j & 1) ? 0x7632u : 0x5410u;
+            uint32_t a[4];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) mma_f16(st.acc[mt][i * 4 + j], w[mt], b0, b1);
+            for (int k = 0; k < 4; ++k) {              // a0, a1: slots 2q, 2q + 1 of channel groups 0, 1; a2, a3: slots 8 + 2q ..
+                const uint2 lo = x[k & 1][2 * (k >> 1)], hi = x[k & 1][2 * (k >> 1) + 1];
+                a[k] = j < 2 ? prmt(lo.x, hi.x, sel) : prmt(lo.y, hi.y, sel);
             }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma_f16(st.acc[n][j], a, w[n][0], w[n][1]);
         }
     }
 };
+
+// n tiles in a row that every row sees whole; stops in front of a tile with a weight that overflows.  Returns the tiles done.
+template <int NT, class C>
+__device__ __forceinline__ uint32_t whole_tiles(const uint8_t* rec, uint32_t n, uint32_t step, int lane, const RowsQuery<NT>& qf,
+                                                float kfactor, RowsState<NT>& st) {
+    uint32_t i = 0;
+#pragma unroll 1
+    for (; i < n; ++i, rec += step) {
+        TileLogits<NT> t;
+        C::template k_side<NT>(rec, lane, qf, kfactor, t);
+        float2 p[NT][2];
+        uint32_t w[NT][2];
+        logits_of(st, t, true, p);
+        if (__builtin_expect(!weigh(t, p, w), 0)) break;
+        add_tile(st, t, p, w);
+        C::template v_side<NT>(rec, lane, st, w, 15u);
+    }
+    return i;
+}
+
+// Accumulators and the units of a class.  V operand j of a byte holds the fields up to that of channels 4 g + j and
+// 32 + 4 g + j, as multiples of 2^-24: with b_j the bit of the field inside its byte, the accumulator of operand j is
+//   F_j = 2^(b_j - 24) o_j + (b_j > 0 ? F_(j-1) : 0).
+// fp16 rows: F_j = o_j.
+__device__ __forceinline__ int v_bit(int c, int j) { return c == 0 ? 2 * j : c == 1 ? 4 * (j & 1) : 0; }
+template <int NT>
+__device__ __forceinline__ void enter_class(RowsState<NT>& st, int c) {
+    if (c == 3) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float f = two_to(v_bit(c, j) - 24), carry = v_bit(c, j) > 0 ? 1.f : 0.f;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) st.acc[n][j][e] = fmaf(st.acc[n][j > 0 ? j - 1 : 0][e], carry, st.acc[n][j][e] * f);
+    }
+}
+template <int NT>
+__device__ __forceinline__ void leave_class(RowsState<NT>& st, int c) {
+    if (c == 3) return;
+#pragma unroll
+    for (int j = 3; j >= 0; --j) {
+        const float f = two_to(24 - v_bit(c, j)), carry = v_bit(c, j) > 0 ? -1.f : 0.f;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) st.acc[n][j][e] = fmaf(st.acc[n][j > 0 ? j - 1 : 0][e], carry, st.acc[n][j][e]) * f;
+    }
+}
 
 // ---------------------------------------------------------------- the kernel
 
@@ -467,17 +548,18 @@ __device__ __forceinline__ uint4 draft_row_as_stored(uint4 raw, int c) {
     return make_uint4(out[0], out[1], out[2], out[3]);
 }
 
-// grid = batch * kv_heads * parts * row_blocks, block = kRowsThreads, dynamic smem = rows_smem_bytes<MT>(draft tiles).
-// MT: 16-row blocks per unit.  TREE: rows belong to drafted nodes (otherwise nodes == 1 and the row is the last
+// grid = batch * kv_heads * parts * row_blocks, block = kRowsThreads, dynamic smem = rows_smem_bytes<NT>(draft tiles).
+// NT: blocks of eight rows per unit.  TREE: rows belong to drafted nodes (otherwise nodes == 1 and the row is the last
 // cached token's).
-template <int MT, bool TREE>
-__global__ void __launch_bounds__(kRowsThreads, MT == 1 ? 4 : 2) k_attend_rows(const RowsParams P) {
-    constexpr int ROWS = 16 * MT;
+template <int NT, bool TREE>
+__global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_rows(const RowsParams P) {
+    constexpr int ROWS = 8 * NT;
     extern __shared__ __align__(128) uint8_t dyn[];
-    __shared__ RowsScratch<MT> sc;
+    __shared__ RowsScratch<NT> sc;
     uint8_t* const rings = dyn;
-    uint4* const qfrag = reinterpret_cast<uint4*>(dyn + (size_t)kRowsWarps * kRowsStages * kRowsStageBytes);   // [class][MT][4][32]
-    uint8_t* const draft = reinterpret_cast<uint8_t*>(qfrag + kNumPools * MT * 4 * 32);
+    uint4* const qfrag = reinterpret_cast<uint4*>(dyn + (size_t)kRowsWarps * kRowsStages * kRowsStageBytes);   // [class][NT][2][32]
+    const uint32_t draft_at = (uint32_t)((size_t)kRowsWarps * kRowsStages * kRowsStageBytes + (size_t)kNumPools * NT * 2 * 32 * 16);
+    uint8_t* const draft = dyn + draft_at;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
     const StoreView& S = P.store;
 
@@ -502,9 +584,8 @@ __global__ void __launch_bounds__(kRowsThreads, MT == 1 ? 4 : 2) k_attend_rows(c
 
     // ---- the query block
     float qmax = 0.f;
-#pragma unroll
-    for (int k = 0; k < MT; ++k) {
-        const int row = 16 * k + (tid >> 3), piece = tid & 7;
+    if (tid < 8 * ROWS) {                              // (whole warps) thread = (row, eight channels)
+        const int row = tid >> 3, piece = tid & 7;
         const int R = (int)rb * ROWS + row;
         const int node = R / P.group;
         uint4 v = make_uint4(0u, 0u, 0u, 0u);
@@ -513,8 +594,8 @@ __global__ void __launch_bounds__(kRowsThreads, MT == 1 ? 4 : 2) k_attend_rows(c
         *reinterpret_cast<uint4*>(&sc.q[row][piece * 8]) = v;
         const float2 f0 = unpack_half2(v.x), f1 = unpack_half2(v.y), f2 = unpack_half2(v.z), f3 = unpack_half2(v.w);
         float sum = ((f0.x + f0.y) + (f1.x + f1.y)) + ((f2.x + f2.y) + (f3.x + f3.y));
-        qmax = fmaxf(qmax, fmaxf(fmaxf(fmaxf(fabsf(f0.x), fabsf(f0.y)), fmaxf(fabsf(f1.x), fabsf(f1.y))),
-                                 fmaxf(fmaxf(fabsf(f2.x), fabsf(f2.y)), fmaxf(fabsf(f3.x), fabsf(f3.y)))));
+        qmax = fmaxf(fmaxf(fmaxf(fabsf(f0.x), fabsf(f0.y)), fmaxf(fabsf(f1.x), fabsf(f1.y))),
+                     fmaxf(fmaxf(fabsf(f2.x), fabsf(f2.y)), fmaxf(fabsf(f3.x), fabsf(f3.y))));
 #pragma unroll
         for (int d = 1; d < 8; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         if (piece == 0) {
@@ -655,12 +736,13 @@ __global__ void __launch_bounds__(kRowsThreads, MT == 1 ? 4 : 2) k_attend_rows(c
             before += k < c ? wk : 0u;
             total += wk;
         }
-        const uint32_t shares = P.parts * kRowsWarps, me = part * kRowsWarps + warp;
-        const long long r0 = (long long)((unsigned long long)total * me / shares) - before;
-        const long long r1 = (long long)((unsigned long long)total * (me + 1) / shares) - before;
+        // floor(total * j / shares) without a 64-bit division (shares <= 256)
+        const uint32_t shares = P.parts * kRowsWarps, me = part * kRowsWarps + warp, whole = total / shares, rest = total - whole * shares;
+        const int r0 = (int)(whole * me + rest * me / shares) - (int)before;
+        const int r1 = (int)(whole * (me + 1) + rest * (me + 1) / shares) - (int)before;
         // the same rounding for a share's end and the next one's start
-        const int lo = (int)min(max(r0, 0ll) / cost, (long long)n);
-        const int hi = me + 1 == shares ? (int)n : (int)min(max(r1, 0ll) / cost, (long long)n);
+        const int lo = min(max(r0, 0) / (int)cost, (int)n);
+        const int hi = me + 1 == shares ? (int)n : min(max(r1, 0) / (int)cost, (int)n);
         sc.seg_lo[warp][2 * c] = lo;
         sc.seg_hi[warp][2 * c] = min(hi, ns);
         sc.seg_lo[warp][2 * c + 1] = max(lo, ns) - ns + ws;
@@ -668,74 +750,95 @@ __global__ void __launch_bounds__(kRowsThreads, MT == 1 ? 4 : 2) k_attend_rows(c
     }
     __syncwarp();
 
-    // ---- producer: the chunks of the share in order; a chunk stays inside one 64 KB block and fits a stage
-    uint8_t* const ring = rings + (size_t)warp * kRowsStages * kRowsStageBytes;
-    int p_seg = -1, p_left = 0, p_tps = 0, p_bt = 0, p_block_left = 0;
-    uint32_t p_rec = 0, p_next = 0;
-    const uint8_t* p_ptr = nullptr;
-    const uint32_t* p_tab = nullptr;                   // entry of the block after the current one
-    auto next_segment = [&]() {
-        while (p_left <= 0 && ++p_seg < 2 * kNumPools) {
-            const int lo = sc.seg_lo[warp][p_seg], c = p_seg >> 1;
-            p_left = sc.seg_hi[warp][p_seg] - lo;
-            if (p_left <= 0) continue;
-            p_rec = (uint32_t)(c == 0 ? pool_rec_bytes(0) : c == 1 ? pool_rec_bytes(1) : c == 2 ? pool_rec_bytes(2) : pool_rec_bytes(3));
-            p_tps = c == 0 ? kRowsTps(0) : c == 1 ? kRowsTps(1) : c == 2 ? kRowsTps(2) : kRowsTps(3);
-            p_bt = (int)block_tiles(c);
-            const int blk = lo / p_bt, ib = lo - blk * p_bt;
-            p_tab = stream_table(S, c, P.layer, b, h) + blk;
-            p_ptr = S.arena + (size_t)p_tab[0] * kBlockBytes + (size_t)ib * p_rec;
-            ++p_tab;
-            p_block_left = p_bt - ib;
-            if (p_left > p_block_left) p_next = p_tab[0];
+    // ---- the copies: chunks of the share in order; a chunk stays inside one 64 KB block and fits a stage
+    const uint32_t ring = (uint32_t)warp * kRowsStages * kRowsStageBytes;          // offset in dyn
+    RowsChunks& plan = sc.plan[warp];
+    int planned = 0, taken = 0;
+    auto plan_more = [&]() {                           // (whole warp) the chunks up to the end of the range or of the block
+        __syncwarp();
+        int seg = plan.seg, tile = plan.tile;
+        planned = taken = 0;
+        while (tile >= sc.seg_hi[warp][seg]) {
+            if (++seg == 2 * kNumPools) return;
+            tile = sc.seg_lo[warp][seg];
         }
+        const int c = seg >> 1, bt = (int)block_tiles(c), blk = tile / bt, ib = tile - blk * bt, tps = kRowsTps(c);
+        const uint32_t rec = (uint32_t)(c == 0 ? pool_rec_bytes(0) : c == 1 ? pool_rec_bytes(1) : c == 2 ? pool_rec_bytes(2) : pool_rec_bytes(3));
+        const uint8_t* src = S.arena + (size_t)stream_table(S, c, P.layer, b, h)[blk] * kBlockBytes + (uint32_t)ib * rec;
+        const int in_sinks = sc.in_sinks[c], from = sc.from[c], full = sc.full[c];
+        const int piece = min(bt - ib, sc.seg_hi[warp][seg] - tile);
+        planned = min((piece + tps - 1) / tps, 32);
+        const int t0 = tile + lane * tps, n = min(tps, tile + piece - t0);
+        uint32_t edge = 0;
+        for (int i = 0; i < n; ++i) edge |= t0 + i < full && (t0 + i >= from || t0 + i < in_sinks) ? 0u : 1u << i;
+        src += (size_t)((uint32_t)(lane * tps) * rec);
+        if (lane < planned)
+            plan.chunk[lane] = make_uint4((uint32_t)(uintptr_t)src, (uint32_t)((uintptr_t)src >> 32), (uint32_t)t0 | ((uint32_t)c << 30),
+                                          (uint32_t)n * rec | ((uint32_t)n << 16) | (edge << 20));
+        __syncwarp();
+        if (lane == 0) {
+            plan.seg = seg;
+            plan.tile = tile + min(piece, planned * tps);
+        }
+        __syncwarp();
     };
-    next_segment();
-    int pslot = 0, cslot = 0, in_flight = 0;
+    auto feed = [&](int slot) -> int {                 // start the next copy; 0 if there is none
+        if (taken == planned) {
+            plan_more();
+            if (planned == 0) return 0;
+        }
+        if (lane == 0) {
+            const uint4 k = plan.chunk[taken];
+            const uint32_t bytes = k.w & 0xffffu;
+            mbar_arrive_expect_tx(&sc.bars[warp][slot], bytes);
+            bulk_load(dyn + ring + (uint32_t)slot * kRowsStageBytes, reinterpret_cast<const uint8_t*>((uintptr_t)k.x | ((uintptr_t)k.y << 32)), bytes,
+                      &sc.bars[warp][slot]);
+            sc.chunk[warp][slot] = make_uint2(k.z, k.w >> 16);
+        }
+        ++taken;
+        return 1;
+    };
+    int in_flight = 0, cslot = 0;
     uint32_t parity = 0;
     bool failed = false;
-    auto issue = [&]() {
-        const int n = min(min(p_tps, p_block_left), p_left);
-        const uint32_t bytes = (uint32_t)n * p_rec;
+    if (lane < kNumPools) {
+        const int c = lane;
+        const uint32_t lo_last = P.window > 0 ? sc.start[c] + (TREE ? (uint32_t)__popcll(sc.step_bits[c]) : 0u) : 0u;
+        if (warp == 0) {
+            sc.in_sinks[c] = (int)(sc.sink[c] / kTileTokens);
+            sc.from[c] = (int)((lo_last + kTileTokens - 1) / kTileTokens);
+            sc.full[c] = (int)(sc.cnt[c] / kTileTokens);
+        }
         if (lane == 0) {
-            mbar_arrive_expect_tx(&sc.bars[warp][pslot], bytes);
-            bulk_load(ring + (size_t)pslot * kRowsStageBytes, p_ptr, bytes, &sc.bars[warp][pslot]);
+            plan.seg = 0;
+            plan.tile = sc.seg_lo[warp][0];
         }
-        pslot = pslot + 1 == kRowsStages ? 0 : pslot + 1;
-        p_ptr += bytes;
-        p_left -= n;
-        p_block_left -= n;
-        if (p_left == 0) {
-            next_segment();
-        } else if (p_block_left == 0) {                // on to the stream's next block
-            p_ptr = S.arena + (size_t)p_next * kBlockBytes;
-            p_block_left = p_bt;
-            ++p_tab;
-            if (p_left > p_bt) p_next = p_tab[0];
-        }
-    };
-    for (; in_flight < kRowsStages && p_left > 0; ++in_flight) issue();
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (; in_flight < kRowsStages; ++in_flight)
+        if (!feed(in_flight)) break;
 
-    // ---- row operands of the K product, one set per class (warp = class): q * F * 2^-k, F a power of two that puts the
+    // ---- column operands of the K product, one set per class (warp = class): q * F * 2^-k, F a power of two that puts the
     // block's largest query value below 2^15
     const float block_max = fmaxf(fmaxf(fmaxf(sc.wmax[0], sc.wmax[1]), fmaxf(sc.wmax[2], sc.wmax[3])), 6.103515625e-05f);
     const int e_max = (int)(__float_as_uint(block_max) >> 23) - 127;           // -14 .. 15
     const float F = two_to(14 - e_max);
     {
-        auto build = [&](auto channel, auto bit) {
+        auto build = [&](auto channel, auto bit) {     // column g of block n: step s, register r = channels of lane q
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    uint32_t a[4];
+                for (int s2 = 0; s2 < 2; ++s2) {
+                    uint32_t w[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {      // a0: row g, r = 0; a1: row g + 8, r = 0; a2, a3: r = 1
-                        const int r = k >> 1;
-                        const __half* row = sc.q[16 * mt + g + 8 * (k & 1)];
+                    for (int k = 0; k < 4; ++k) {
+                        const int s = 2 * s2 + (k >> 1), r = k & 1;
+                        const __half* row = sc.q[8 * n + g];
                         const float f = F * two_to(-bit(s, r));
-                        a[k] = pack_half2(make_float2(__half2float(row[channel(s, r, q, 0)]) * f, __half2float(row[channel(s, r, q, 1)]) * f));
+                        w[k] = pack_half2(make_float2(__half2float(row[channel(s, r, q, 0)]) * f, __half2float(row[channel(s, r, q, 1)]) * f));
                     }
-                    qfrag[((warp * MT + mt) * 4 + s) * 32 + lane] = make_uint4(a[0], a[1], a[2], a[3]);
+                    qfrag[((warp * NT + n) * 2 + s2) * 32 + lane] = make_uint4(w[0], w[1], w[2], w[3]);
                 }
         };
         if (warp == 0) build(RowsQuant<0>::k_channel, RowsQuant<0>::k_bit);
@@ -746,119 +849,123 @@ __global__ void __launch_bounds__(kRowsThreads, MT == 1 ? 4 : 2) k_attend_rows(c
     __syncthreads();
 
     // ---- the walk
-    RowsState<MT> st;
-    float sumq[MT][2];
+    RowsState<NT> st;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
+    for (int n = 0; n < NT; ++n) {
+        st.negm[n] = both(-kNegBig);
+        st.l[n] = st.b[n] = both(0.f);
+        st.sumq[n] = make_float2(sc.sumq[8 * n + 2 * q], sc.sumq[8 * n + 2 * q + 1]);
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            st.m[mt][r] = kNegBig;
-            st.l2[mt][r] = st.b2[mt][r] = make_float2(0.f, 0.f);
-            sumq[mt][r] = sc.sumq[16 * mt + g + 8 * r];
-        }
-#pragma unroll
-        for (int n = 0; n < 8; ++n) st.acc[mt][n][0] = st.acc[mt][n][1] = st.acc[mt][n][2] = st.acc[mt][n][3] = 0.f;
+        for (int j = 0; j < 4; ++j) st.acc[n][j][0] = st.acc[n][j][1] = st.acc[n][j][2] = st.acc[n][j][3] = 0.f;
     }
-    st.grid = kGridStart;
 
-    auto load_queries = [&](int c, uint4 (&qf)[MT][4]) {
+    auto load_queries = [&](int c, RowsQuery<NT>& qf) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int s = 0; s < 4; ++s) qf[mt][s] = qfrag[((c * MT + mt) * 4 + s) * 32 + lane];
+            for (int s2 = 0; s2 < 2; ++s2) qf[n][s2] = qfrag[((c * NT + n) * 2 + s2) * 32 + lane];
     };
-    auto scale_acc = [&](auto factor) {                // per column group j
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int n = 0; n < 8; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) st.acc[mt][n][e] *= factor(n & 3);
-    };
-    auto walk = [&](auto cls_tag, auto consumer) {
-        constexpr int CLS = decltype(cls_tag)::value;
-        using C = decltype(consumer);
-        constexpr int TPS = kRowsTps(CLS), BT = (int)block_tiles(CLS);
-        if (sc.seg_lo[warp][2 * CLS] >= sc.seg_hi[warp][2 * CLS] && sc.seg_lo[warp][2 * CLS + 1] >= sc.seg_hi[warp][2 * CLS + 1]) return;
-        uint4 qf[MT][4];
-        load_queries(CLS, qf);
-        const float kfactor = kLogitScale * (CLS == 3 ? 1.0f : 16777216.0f) / F;
-        if constexpr (CLS < 3) scale_acc([](int j) { return two_to(RowsQuant<CLS == 3 ? 0 : CLS>::v_bit(j) - 24); });
-        const uint32_t cnt = sc.cnt[CLS], sink = sc.sink[CLS];
-        const uint32_t lo_last = P.window > 0 ? sc.start[CLS] + (TREE ? (uint32_t)__popcll(sc.step_bits[CLS]) : 0u) : 0u;
-#pragma unroll 1
-        for (int part_of_pool = 0; part_of_pool < 2; ++part_of_pool) {
-            int tile0 = sc.seg_lo[warp][2 * CLS + part_of_pool];
-            const int hi = sc.seg_hi[warp][2 * CLS + part_of_pool];
-            int block_left = BT - tile0 % BT;
-            while (tile0 < hi && !failed) {
-                failed = !__all_sync(0xffffffffu, mbar_wait(&sc.bars[warp][cslot], (parity >> cslot) & 1u));
-                if (failed) break;
-                const int n = min(min(TPS, block_left), hi - tile0);
-                const uint8_t* buf = ring + (size_t)cslot * kRowsStageBytes;
-#pragma unroll 1
-                for (int i = 0; i < n; ++i) {
-                    const uint32_t s0 = (uint32_t)(tile0 + i) * kTileTokens;
-                    uint32_t seen[MT][2], valid = 0;
-                    // at an edge: the pool's last tile, or one where the window starts or the sinks end
-                    const bool edge = s0 + kTileTokens > cnt || (s0 < lo_last && s0 + kTileTokens > sink);
-                    if (edge) {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const uint32_t slot = s0 + 8 * (k >> 1) + 2 * q + (k & 1);
-                            valid |= slot < cnt ? 1u << k : 0u;
-                        }
-#pragma unroll
-                        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                            for (int r = 0; r < 2; ++r) {
-                                const uint32_t lo = P.window > 0 ? sc.lo_row[CLS][16 * mt + g + 8 * r] : 0u;
-                                seen[mt][r] = 0;
-#pragma unroll
-                                for (int k = 0; k < 4; ++k) {
-                                    const uint32_t slot = s0 + 8 * (k >> 1) + 2 * q + (k & 1);
-                                    seen[mt][r] |= slot >= lo || slot < sink ? 1u << k : 0u;
-                                }
-                                seen[mt][r] &= valid;
-                            }
-                    }
-                    C::template tile<MT>(buf + (size_t)i * C::REC, lane, qf, kfactor, sumq, st, edge, seen, valid);
-                }
-                tile0 += n;
-                block_left -= n;
-                if (block_left == 0) block_left = BT;
-                --in_flight;
-                __syncwarp();                          // every lane is done with the stage before it is refilled
-                if (p_left > 0) {
-                    issue();
-                    ++in_flight;
-                }
-                parity ^= 1u << cslot;
-                cslot = cslot + 1 == kRowsStages ? 0 : cslot + 1;
-            }
+    const float kfactor = kLogitScale / F;
+    RowsQuery<NT> qf;
+    // One tile of class c in general.  There is one copy of this code for all classes, and a short loop per class for the
+    // tiles in the middle (whole_tiles): the loops have to stay inside the instruction caches.
+    auto any_tile = [&](int c, const uint8_t* rec, bool edge, const uint32_t (&seen)[NT], uint32_t valid) {
+        TileLogits<NT> t;
+        if (c == 0) RowsQuant<0>::k_side<NT>(rec, lane, qf, kfactor, t);
+        else if (c == 1) RowsQuant<1>::k_side<NT>(rec, lane, qf, kfactor, t);
+        else if (c == 2) RowsQuant<2>::k_side<NT>(rec, lane, qf, kfactor, t);
+        else RowsFp16::k_side<NT>(rec, lane, qf, kfactor, t);
+        float2 p[NT][2];
+        uint32_t w[NT][2];
+        for (int moved = 0; moved < 2; ++moved) {
+            logits_of(st, t, true, p);
+            hide(edge, seen, p);
+            if (weigh(t, p, w) || moved) break;
+            move_references(st, t, edge, seen);
         }
-        if constexpr (CLS < 3) scale_acc([](int j) { return two_to(24 - RowsQuant<CLS == 3 ? 0 : CLS>::v_bit(j)); });
+        add_tile(st, t, p, w);
+        if (c == 0) RowsQuant<0>::v_side<NT>(rec, lane, st, w, valid);
+        else if (c == 1) RowsQuant<1>::v_side<NT>(rec, lane, st, w, valid);
+        else if (c == 2) RowsQuant<2>::v_side<NT>(rec, lane, st, w, valid);
+        else RowsFp16::v_side<NT>(rec, lane, st, w, valid);
     };
-    walk(std::integral_constant<int, 0>{}, RowsQuant<0>{});
-    walk(std::integral_constant<int, 1>{}, RowsQuant<1>{});
-    walk(std::integral_constant<int, 2>{}, RowsQuant<2>{});
-    walk(std::integral_constant<int, 3>{}, RowsFp16{});
-    if (has_draft && warp < draft_tiles) {             // a tile of drafted tokens per warp, under the mask of ancestors
-        uint4 qf[MT][4];
-        load_queries(3, qf);
-        const uint32_t use = (uint32_t)(sc.used >> (16 * warp));
-        const uint32_t valid = ((use >> (2 * q)) & 3u) | (((use >> (8 + 2 * q)) & 3u) << 2);
-        uint32_t seen[MT][2];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const int node = sc.node[16 * mt + g + 8 * r];
-                const uint32_t v = node >= 0 ? (uint32_t)(sc.vis[node] >> (16 * warp)) : 0u;
-                seen[mt][r] = ((v >> (2 * q)) & 3u) | (((v >> (8 + 2 * q)) & 3u) << 2);
+    int cls = 3;
+    bool draft_left = has_draft && warp < draft_tiles; // a tile of drafted tokens per warp, at the end
+    load_queries(3, qf);
+    while ((in_flight > 0 || draft_left) && !failed) {
+        const bool drafted = in_flight == 0;
+        const uint2 ck = drafted ? make_uint2(3u << 30, 1u | 16u) : sc.chunk[warp][cslot];
+        const int c = (int)(ck.x >> 30);
+        if (c != cls) {
+            leave_class<NT>(st, cls);
+            enter_class<NT>(st, c);
+            load_queries(c, qf);
+            cls = c;
+        }
+        if (!drafted) {
+            failed = !__all_sync(0xffffffffu, mbar_wait(&sc.bars[warp][cslot], (parity >> cslot) & 1u));
+            if (failed) break;
+        }
+        const uint8_t* rec = dyn + (drafted ? draft_at + (uint32_t)warp * kDraftTileBytes : ring + (uint32_t)cslot * kRowsStageBytes);
+        const uint32_t step = (uint32_t)(c == 0 ? pool_rec_bytes(0) : c == 1 ? pool_rec_bytes(1) : c == 2 ? pool_rec_bytes(2) : pool_rec_bytes(3));
+        uint32_t left = ck.y & 15u, edges = ck.y >> 4, s0 = (ck.x & 0x3fffffffu) * kTileTokens;
+#pragma unroll 1
+        while (true) {
+            const uint32_t run = edges ? (uint32_t)__ffs(edges) - 1u : left;
+            if (run > 0) {
+                uint32_t done;
+                if (c == 0) done = whole_tiles<NT, RowsQuant<0>>(rec, run, pool_rec_bytes(0), lane, qf, kfactor, st);
+                else if (c == 1) done = whole_tiles<NT, RowsQuant<1>>(rec, run, pool_rec_bytes(1), lane, qf, kfactor, st);
+                else if (c == 2) done = whole_tiles<NT, RowsQuant<2>>(rec, run, pool_rec_bytes(2), lane, qf, kfactor, st);
+                else done = whole_tiles<NT, RowsFp16>(rec, run, pool_rec_bytes(3), lane, qf, kfactor, st);
+                left -= done;
+                if (left == 0) break;
+                rec += done * step;
+                s0 += done * kTileTokens;
+                edges >>= done;
             }
-        RowsFp16::tile<MT>(draft + (size_t)warp * kDraftTileBytes, lane, qf, kLogitScale / F, sumq, st, true, seen, valid);
+            uint32_t seen[NT] = {}, valid = 15u;
+            const bool edge = edges & 1u;
+            if (edge) {                                // the pool's last tile, one where a window starts or the sinks end, a drafted one
+                const uint32_t use = drafted ? (uint32_t)(sc.used >> (16 * warp)) : 0u, cnt = sc.cnt[c], sink = sc.sink[c];
+                valid = 0;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t at = 2 * q + (k & 1) + 8 * (k >> 1);
+                    valid |= (drafted ? (use >> at) & 1u : s0 + at < cnt) ? 1u << k : 0u;
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {      // row 2q + x
+                        const int row = 8 * n + 2 * q + x, node = sc.node[row];
+                        const uint32_t lo = P.window > 0 ? sc.lo_row[c][row] : 0u;
+                        const uint32_t vis = drafted && node >= 0 ? (uint32_t)(sc.vis[node] >> (16 * warp)) : 0u;
+#pragma unroll
+                        for (int s = 0; s < 2; ++s) {
+                            const uint32_t at = g + 8 * s, slot = s0 + at;
+                            const bool see = drafted ? (vis >> at) & 1u : slot < cnt && (slot >= lo || slot < sink);
+                            seen[n] |= see ? 1u << (2 * s + x) : 0u;
+                        }
+                    }
+            }
+            any_tile(c, rec, edge, seen, valid);
+            if (--left == 0) break;
+            rec += step;
+            s0 += kTileTokens;
+            edges >>= 1;
+        }
+        if (drafted) {
+            draft_left = false;
+        } else {
+            __syncwarp();                              // every lane is done with the stage before it is refilled
+            in_flight += feed(cslot) - 1;
+            parity ^= 1u << cslot;
+            cslot = cslot + 1 == kRowsStages ? 0 : cslot + 1;
+            __syncwarp();                              // (sc.chunk of the refilled stage)
+        }
     }
+    leave_class<NT>(st, cls);
     if (failed) {                                      // give up: no further copy; those in flight are let land first
         if (lane == 0) atomicOr(S.flags, kFlagWaitTimeout);
         while (in_flight > 0) {
@@ -870,41 +977,37 @@ __global__ void __launch_bounds__(kRowsThreads, MT == 1 ? 4 : 2) k_attend_rows(c
     }
 
     // ---- merge the four warps: M = max m_w, l = sum l_w 2^(m_w - M), O = sum o_w 2^(m_w - M)
-    float bsum[MT][2];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            float l = st.l2[mt][r].x + st.l2[mt][r].y, z = st.b2[mt][r].x + st.b2[mt][r].y;
-#pragma unroll
-            for (int d = 1; d < 4; d <<= 1) {
-                l += __shfl_xor_sync(0xffffffffu, l, d);
-                z += __shfl_xor_sync(0xffffffffu, z, d);
-            }
-            bsum[mt][r] = z;
-            if (q == 0) sc.ml[warp][16 * mt + g + 8 * r] = make_float2(st.m[mt][r], l);
+        for (int d = 4; d < 32; d <<= 1) {
+            st.l[n].x += __shfl_xor_sync(0xffffffffu, st.l[n].x, d);
+            st.l[n].y += __shfl_xor_sync(0xffffffffu, st.l[n].y, d);
+            st.b[n].x += __shfl_xor_sync(0xffffffffu, st.b[n].x, d);
+            st.b[n].y += __shfl_xor_sync(0xffffffffu, st.b[n].y, d);
         }
+        if (g == 0) {
+            sc.ml[warp][8 * n + 2 * q] = make_float2(-st.negm[n].x, st.l[n].x);
+            sc.ml[warp][8 * n + 2 * q + 1] = make_float2(-st.negm[n].y, st.l[n].y);
+        }
+    }
     __syncthreads();                                   // also: every warp is done with its ring, which becomes the merge buffer
     float* const out = reinterpret_cast<float*>(rings);             // [warps][ROWS][kRowsOutStride]
-    const float ungrid = 1.0f / st.grid;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const int row = 16 * mt + g + 8 * r;
+        for (int x = 0; x < 2; ++x) {
+            const int row = 8 * n + 2 * q + x;
             float M = kNegBig;
 #pragma unroll
             for (int k = 0; k < kRowsWarps; ++k) M = fmaxf(M, sc.ml[k][row].x);
-            const float f = fast_exp2(st.m[mt][r] - M), fg = f * ungrid, fb = f * bsum[mt][r];
+            const float f = fast_exp2(-(x ? st.negm[n].y : st.negm[n].x) - M), fb = f * (x ? st.b[n].y : st.b[n].x);
             float* dst = out + ((size_t)warp * ROWS + row) * kRowsOutStride;
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {          // column 2q + e of the groups (i, 0..3): channels 4 (2q + e + 8i) ..
-                    const float4 v = make_float4(fmaf(st.acc[mt][4 * i][2 * r + e], fg, fb), fmaf(st.acc[mt][4 * i + 1][2 * r + e], fg, fb),
-                                                 fmaf(st.acc[mt][4 * i + 2][2 * r + e], fg, fb), fmaf(st.acc[mt][4 * i + 3][2 * r + e], fg, fb));
-                    *reinterpret_cast<float4*>(dst + 4 * (2 * q + e + 8 * i)) = v;
-                }
+            for (int i = 0; i < 2; ++i)                // channels 32 i + 4 g .. + 3
+                *reinterpret_cast<float4*>(dst + 32 * i + 4 * g) =
+                    make_float4(fmaf(st.acc[n][0][2 * i + x], f, fb), fmaf(st.acc[n][1][2 * i + x], f, fb),
+                                fmaf(st.acc[n][2][2 * i + x], f, fb), fmaf(st.acc[n][3][2 * i + x], f, fb));
         }
     __syncthreads();
 
@@ -920,9 +1023,9 @@ __global__ void __launch_bounds__(kRowsThreads, MT == 1 ? 4 : 2) k_attend_rows(c
         *reinterpret_cast<uint4*>(P.O + (((size_t)b * P.nodes + node) * S.q_heads + (size_t)h * P.group + (R - node * P.group)) * kHeadDim + (tid & 7) * 8) =
             make_uint4(v[0], v[1], v[2], v[3]);
     };
-#pragma unroll
-    for (int k = 0; k < MT; ++k) {
-        const int row = 16 * k + (tid >> 3);
+    const bool mine = tid < 8 * ROWS;
+    const int row = tid >> 3;
+    if (mine) {
         float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         float M = kNegBig, L = 0.f;
 #pragma unroll
@@ -955,26 +1058,23 @@ __global__ void __launch_bounds__(kRowsThreads, MT == 1 ? 4 : 2) k_attend_rows(c
     if (!sc.last) return;
     __threadfence();
     if (tid == 0) P.part_cnt[unit] = 0u;
-#pragma unroll
-    for (int k = 0; k < MT; ++k) {
-        const int row = 16 * k + (tid >> 3);
-        const size_t rec0 = (size_t)unit * P.parts * ROWS + row;
-        float M = kNegBig, L = 0.f;
-        for (uint32_t s = 0; s < P.parts; ++s) M = fmaxf(M, __ldcg(P.part_ml + rec0 + (size_t)s * ROWS).x);
-        float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (!mine) return;
+    const size_t rec0 = (size_t)unit * P.parts * ROWS + row;
+    float M = kNegBig, L = 0.f;
+    for (uint32_t s = 0; s < P.parts; ++s) M = fmaxf(M, __ldcg(P.part_ml + rec0 + (size_t)s * ROWS).x);
+    float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-        for (uint32_t s = 0; s < P.parts; ++s) {
-            const size_t rec = rec0 + (size_t)s * ROWS;
-            const float2 ml = __ldcg(P.part_ml + rec);
-            const float4* src = reinterpret_cast<const float4*>(P.part_o + rec * kHeadDim + (tid & 7) * 8);
-            const float4 v0 = __ldcg(src), v1 = __ldcg(src + 1);
-            const float f = fast_exp2(ml.x - M);
-            L = fmaf(ml.y, f, L);
-            o[0] = fmaf(v0.x, f, o[0]); o[1] = fmaf(v0.y, f, o[1]); o[2] = fmaf(v0.z, f, o[2]); o[3] = fmaf(v0.w, f, o[3]);
-            o[4] = fmaf(v1.x, f, o[4]); o[5] = fmaf(v1.y, f, o[5]); o[6] = fmaf(v1.z, f, o[6]); o[7] = fmaf(v1.w, f, o[7]);
-        }
-        store_row(row, o, L);
+    for (uint32_t s = 0; s < P.parts; ++s) {
+        const size_t rec = rec0 + (size_t)s * ROWS;
+        const float2 ml = __ldcg(P.part_ml + rec);
+        const float4* src = reinterpret_cast<const float4*>(P.part_o + rec * kHeadDim + (tid & 7) * 8);
+        const float4 v0 = __ldcg(src), v1 = __ldcg(src + 1);
+        const float f = fast_exp2(ml.x - M);
+        L = fmaf(ml.y, f, L);
+        o[0] = fmaf(v0.x, f, o[0]); o[1] = fmaf(v0.y, f, o[1]); o[2] = fmaf(v0.z, f, o[2]); o[3] = fmaf(v0.w, f, o[3]);
+        o[4] = fmaf(v1.x, f, o[4]); o[5] = fmaf(v1.y, f, o[5]); o[6] = fmaf(v1.z, f, o[6]); o[7] = fmaf(v1.w, f, o[7]);
     }
+    store_row(row, o, L);
 }
 
 }  // namespace kvq

@@ -1105,7 +1105,7 @@ static int rows_impl(kvq_ctx* c, int layer, const void* Q, void* O, const void* 
     p.sinks = sinks;
     const int64_t seen = window > 0 ? std::min<int64_t>(c->len[layer], (int64_t)window + sinks) : c->len[layer];
     const uint64_t pairs = (uint64_t)c->batch * c->kv_heads;
-    const RowsPlan plan = rows_plan(c->sm_count, pairs, p.rows, (int)seen);
+    const RowsPlan plan = rows_plan(c->sm_count, pairs, p.rows, (int)seen, c->splits_override);
     if (pairs * plan.row_blocks * plan.parts > 0x7fffffffull) return KVQ_ERR_ARG;
     p.row_blocks = plan.row_blocks;
     p.parts = plan.parts;

@@ -8,25 +8,25 @@ namespace kvq {
 
 namespace {
 
-template <int MT, bool TREE>
+template <int NT, bool TREE>
 cudaError_t set_smem() {
     const int draft_tiles = TREE ? kMaxTreeNodes / kTileTokens : 0;
-    return cudaFuncSetAttribute(k_attend_rows<MT, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)rows_smem_bytes<MT>(draft_tiles));
+    return cudaFuncSetAttribute(k_attend_rows<NT, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)rows_smem_bytes<NT>(draft_tiles));
 }
 
-template <int MT, bool TREE>
+template <int NT, bool TREE>
 void launch(const RowsParams& p, uint64_t ctas, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas);
     cfg.blockDim = dim3(kRowsThreads);
-    cfg.dynamicSmemBytes = rows_smem_bytes<MT>(TREE ? (p.nodes + kTileTokens - 1) / kTileTokens : 0);
+    cfg.dynamicSmemBytes = rows_smem_bytes<NT>(TREE ? (p.nodes + kTileTokens - 1) / kTileTokens : 0);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];                       // may be scheduled behind the kernel ahead of it; see pdl_wait
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    cudaLaunchKernelEx(&cfg, k_attend_rows<MT, TREE>, p);
+    cudaLaunchKernelEx(&cfg, k_attend_rows<NT, TREE>, p);
 }
 
 }  // namespace
@@ -40,13 +40,18 @@ cudaError_t rows_setup() {
 }
 
 // pairs = (sequence, KV head) pairs.
-RowsPlan rows_plan(int sm_count, uint64_t pairs, int rows, int visible_tokens) {
+RowsPlan rows_plan(int sm_count, uint64_t pairs, int rows, int visible_tokens, int splits) {
     RowsPlan plan;
-    plan.mt = rows <= 16 ? 1 : 2;
-    plan.row_blocks = (uint32_t)((rows + 16 * plan.mt - 1) / (16 * plan.mt));
+    plan.nt = rows <= 8 ? 1 : 2;
+    plan.row_blocks = (uint32_t)((rows + 8 * plan.nt - 1) / (8 * plan.nt));
     const uint64_t units = pairs * plan.row_blocks;
+    if (splits > 0) {
+        plan.parts = (uint32_t)((splits + kRowsWarps - 1) / kRowsWarps);
+        while (plan.parts > 1 && units * plan.parts > rows_max_records(sm_count)) --plan.parts;
+        return plan;
+    }
     const double tiles = (double)visible_tokens / kTileTokens + 2.0;
-    const uint64_t resident = (uint64_t)sm_count * (plan.mt == 1 ? 4 : 2);
+    const uint64_t resident = (uint64_t)sm_count * rows_ctas_per_sm(plan.nt);
     // Time of a launch in tiles of one warp: waves of CTAs, each a set-up of about twelve tiles and its warps' shares;
     // parts merged through global records cost about another twelve.
     double best = 0.0;
@@ -65,10 +70,10 @@ RowsPlan rows_plan(int sm_count, uint64_t pairs, int rows, int visible_tokens) {
 void rows_launch(const RowsParams& p, const RowsPlan& plan, bool tree, uint64_t pairs, cudaStream_t st) {
     const uint64_t ctas = pairs * plan.row_blocks * plan.parts;
     if (tree) {
-        if (plan.mt == 1) launch<1, true>(p, ctas, st);
+        if (plan.nt == 1) launch<1, true>(p, ctas, st);
         else launch<2, true>(p, ctas, st);
     } else {
-        if (plan.mt == 1) launch<1, false>(p, ctas, st);
+        if (plan.nt == 1) launch<1, false>(p, ctas, st);
         else launch<2, false>(p, ctas, st);
     }
 }

@@ -18,8 +18,8 @@ struct RowsParams {
     const __half* V;
     const uint8_t* bits;           // [batch][nodes] or nullptr: fp16 rows (tree only)
     const int32_t* parents;        // [batch][nodes] (tree only)
-    float* part_o;                 // [units * parts][16 MT][64] unnormalised
-    float2* part_ml;               // [units * parts][16 MT]     (m in log2 units, l)
+    float* part_o;                 // [units * parts][8 NT][64] unnormalised
+    float2* part_ml;               // [units * parts][8 NT]     (m in log2 units, l)
     uint32_t* part_cnt;            // [units] parts delivered so far; zero between launches
     int layer, group, nodes, rows; // rows = nodes * group
     uint32_t row_blocks, parts;
@@ -39,19 +39,20 @@ struct VerifyParams {
     int nodes, vocab;
 };
 
-// How a launch is cut: 16-row blocks per unit (1 or 2), row blocks per (sequence, KV head), parts per unit.
+// How a launch is cut: blocks of eight rows per unit (1 or 2), units per (sequence, KV head), parts per unit.
 struct RowsPlan {
-    int mt = 1;
+    int nt = 1;
     uint32_t row_blocks = 1, parts = 1;
 };
-constexpr int kRowsMaxRows = 32;                       // rows of a partial record
+constexpr int kRowsMaxRows = 16;                       // rows of a partial record
 
 // Partial records (of kRowsMaxRows rows) and arrival counters a handle keeps.
-inline size_t rows_max_records(int sm_count) { return 4 * (size_t)sm_count; }
+inline size_t rows_max_records(int sm_count) { return 8 * (size_t)sm_count; }
 
 // Once per device and process image: shared-memory limits of the kernels.
 cudaError_t rows_setup();
-RowsPlan rows_plan(int sm_count, uint64_t pairs, int rows, int visible_tokens);
+// splits > 0: as many warps per unit as that (rounded up to whole CTAs, and down to what the records hold).
+RowsPlan rows_plan(int sm_count, uint64_t pairs, int rows, int visible_tokens, int splits);
 void rows_launch(const RowsParams& p, const RowsPlan& plan, bool tree, uint64_t pairs, cudaStream_t st);
 cudaError_t verify_launch(const VerifyParams& p, int batch, int sm_count, cudaStream_t st);
 
