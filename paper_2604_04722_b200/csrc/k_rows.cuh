@@ -36,10 +36,12 @@
 // grow by 2^11 or so before anything is rescaled -- with sixteen rows, a reference that followed every new maximum was
 // moved on a fifth of all tiles -- and w keeps all its bits down to 2^-18 of the row's largest.
 //
-// Work split: the tiles of a unit (of its four pools laid end to end, a tile weighted by its cost) are cut into
-// parts * 4 equal shares, one per warp.  A warp streams its share through its own ring of bulk copies, as in the decode
-// kernel; the four warps of a CTA are merged in shared memory, the CTAs of a unit (parts > 1) through global records
-// by the CTA that arrives last.  Nothing waits for another CTA.
+// Work split: the units lie end to end on an axis, every unit `ticks` long; a CTA takes `span` ticks of it, in pieces where it
+// crosses unit borders.  With as many CTAs as stay resident and equal stretches all SMs finish together, whatever the
+// number of units; many units are taken whole.  The tiles of a unit (of its four pools laid end to end, a tile weighted
+// by its cost) are cut like the axis, a piece's into four equal shares, one per warp.  A warp streams its share through
+// its own ring of bulk copies, as in the decode kernel; the four warps are merged in shared memory, the pieces of a unit
+// through global records by the CTA that arrives last.  Nothing waits for another CTA.
 //
 // Window.  Slots of a pool are handed out in position order, so a window is a suffix and the sinks a prefix of every
 // pool.  Where they start follows from the per-token index: the first token of class c at or after position p names
@@ -47,7 +49,7 @@
 // window starts; they are told apart only inside the tiles at the edge.
 //
 // Drafted rows (the tree) are quantized at their bit-width and put back together, rounded to fp16, by the CTA of the
-// last part, as fp16 tiles in shared memory that the fp16 consumer reads under a mask of ancestors.
+// last piece, as fp16 tiles in shared memory that the fp16 consumer reads under a mask of ancestors.
 #pragma once
 #include "kvq_common.cuh"
 #include "kvq_ptx.cuh"
@@ -67,17 +69,12 @@ static_assert(6 * pool_rec_bytes(0) <= kRowsStageBytes && 4 * pool_rec_bytes(1) 
               2 * pool_rec_bytes(2) <= kRowsStageBytes && pool_rec_bytes(3) <= kRowsStageBytes, "a chunk fits a stage");
 constexpr int kDraftTileBytes = 4096;                  // one fp16 tile: K units, then V units
 // What a tile of each class costs a warp, for cutting a unit into equal shares.
-__device__ constexpr uint32_t kRowsTileCost[kNumPools] = {6u, 7u, 9u, 12u};
+__device__ constexpr uint32_t kRowsTileCost[kNumPools] = {6u, 7u, 9u, 15u};
 constexpr int kWeightTop = 4;                          // log2 of a row's largest weight when its reference is set
 
-// Resident CTAs per SM that the kernel is compiled for (registers): 8 rows per unit, 16 rows per unit.
-#ifndef KVQ_ROWS_CTAS1
-#define KVQ_ROWS_CTAS1 4
-#endif
-#ifndef KVQ_ROWS_CTAS2
-#define KVQ_ROWS_CTAS2 4
-#endif
-__host__ __device__ constexpr int rows_ctas_per_sm(int nt) { return nt == 1 ? KVQ_ROWS_CTAS1 : KVQ_ROWS_CTAS2; }
+// Resident CTAs per SM that the kernel is compiled for (its registers allow; trees of more than 16 nodes take so much shared
+// memory that 16 rows per unit keep three).
+__host__ __device__ constexpr int rows_ctas_per_sm(int nt) { return nt == 4 ? 2 : 4; }
 // NT: blocks of 8 rows per unit.
 template <int NT>
 __host__ __device__ constexpr size_t rows_smem_bytes(int draft_tiles) {
@@ -231,10 +228,10 @@ __device__ __forceinline__ void logits_of(const RowsState<NT>& st, const TileLog
             y[n][s] = fma2v(make_float2(t.D[n][2 * s], t.D[n][2 * s + 1]), both(t.sk[s]),
                             fma2v(both(t.zk[s]), st.sumq[n], relative ? st.negm[n] : both(0.f)));
 }
-// From relative logits y to p = 2^y and the fp16 weights; false if a weight overflows.  (Every scale is at least 2^-24, see
-// k_side, so that p itself stays far from the end of fp32.)
+// From relative logits y to p = 2^y and the fp16 weights; returns their maxima.  (Every scale is at least 2^-24, see k_side, so
+// that p itself stays far from the end of fp32.)
 template <int NT>
-__device__ __forceinline__ bool weigh(const TileLogits<NT>& t, float2 (&y)[NT][2], uint32_t (&w)[NT][2]) {
+__device__ __forceinline__ uint32_t weigh(const TileLogits<NT>& t, float2 (&y)[NT][2], uint32_t (&w)[NT][2]) {
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -245,9 +242,10 @@ __device__ __forceinline__ bool weigh(const TileLogits<NT>& t, float2 (&y)[NT][2
     uint32_t big = max_half2(w[0][0], w[0][1]);
 #pragma unroll
     for (int n = 1; n < NT; ++n) big = max_half2(big, max_half2(w[n][0], w[n][1]));
-    // weights are not negative; a bit pattern of 0x7c00 or above is an overflow
-    return !__any_sync(0xffffffffu, (big + 0x04000400u) & 0x80008000u);
+    return big;
 }
+// Weights are not negative; a bit pattern of 0x7c00 or above is an overflow.  One vote of the warp.
+__device__ __forceinline__ bool overflows(uint32_t big) { return __any_sync(0xffffffffu, (big + 0x04000400u) & 0x80008000u); }
 // The tile's part of the sums of p and p (z + mid s) - w mid; w becomes the column operand of the V product.
 template <int NT>
 __device__ __forceinline__ void add_tile(RowsState<NT>& st, const TileLogits<NT>& t, const float2 (&p)[NT][2], uint32_t (&w)[NT][2]) {
@@ -315,15 +313,9 @@ struct RowsQuant {
     static constexpr uint32_t MASK = CLS == 0 ? 0x00030003u : CLS == 1 ? 0x000f000fu : 0x00ff00ffu;
     static constexpr float MID = (float)(1 << (BITS - 1));
 
-    // Register r of step s of the K product: channel of 16-bit lane x, and the bit its field is cut out at.
-    __device__ static constexpr int k_channel(int s, int r, int q, int x) {
-        return CLS == 0   ? 16 * q + (2 * s + r) + 8 * x
-               : CLS == 1 ? 8 * (q + 4 * (s >> 1)) + 2 * (s & 1) + r + 4 * x
-                          : 4 * (q + 4 * s) + r + 2 * x;
-    }
-    __device__ static constexpr int k_bit(int s, int r) {
-        return CLS == 0 ? 2 * ((2 * s + r) & 3) : CLS == 1 ? 4 * r : 0;
-    }
+    // Register r of step s of the K product holds, in 16-bit lane x, the code of channel
+    //   2-bit: 16 q + 2 s + r + 8 x;   4-bit: 8 (q + 4 (s >> 1)) + 2 (s & 1) + r + 4 x;   8-bit: 4 (q + 4 s) + r + 2 x
+    // cut out at bit 2 ((2 s + r) & 3), 4 r, 0 (the query's operand is laid out alike, see "column operands" below).
     // The codes of slot g + 8 i for step s, register r.
     __device__ static __forceinline__ uint32_t k_operand(const uint32_t (&kw)[NW], int i, int s, int r) {
         if (CLS == 0) {
@@ -377,8 +369,8 @@ struct RowsQuant {
             }
         }
     }
-    template <int NT>
-    __device__ static __forceinline__ void v_side(const uint8_t* rec, int lane, RowsState<NT>& st, const uint32_t (&w)[NT][2], uint32_t) {
+    // The row operands of the V product: a[j] holds the fields (prefixes, see enter_class) of channels 4 g + j and 32 + 4 g + j.
+    __device__ static __forceinline__ void v_operands(const uint8_t* rec, int lane, uint32_t (&a)[4][4], uint32_t) {
         const int g = lane >> 2, q = lane & 3;
         // V words of slots 2q, 2q + 1 (a) and 8 + 2q, 9 + 2q (b): halves of the words of slot quads q >> 1 and 2 + (q >> 1)
         uint32_t va[NW], vb[NW];
@@ -394,11 +386,8 @@ struct RowsQuant {
 #pragma unroll
             for (int f = 0; f < PER; ++f) {
                 const uint32_t prefix = ((1u << (BITS * (f + 1))) - 1u) * 0x00010001u;
-                uint32_t a[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) a[k] = f + 1 == PER ? x[k] : x[k] & prefix;
-#pragma unroll
-                for (int n = 0; n < NT; ++n) mma_f16(st.acc[n][byte * PER + f], a, w[n][0], w[n][1]);
+                for (int k = 0; k < 4; ++k) a[byte * PER + f][k] = f + 1 == PER ? x[k] : x[k] & prefix;
             }
         }
     }
@@ -406,7 +395,7 @@ struct RowsQuant {
 
 // fp16 rows: the fp16 pool, and the drafted tokens.
 struct RowsFp16 {
-    __device__ static constexpr int k_channel(int s, int r, int q, int x) { return 8 * (2 * s + r) + 2 * q + x; }
+    // Register r of step s of the K product: channels 8 (2 s + r) + 2 q + x.
 
     template <int NT>
     __device__ static __forceinline__ void k_side(const uint8_t* rec, int lane, const RowsQuery<NT>& qf, float kfactor, TileLogits<NT>& t) {
@@ -428,8 +417,7 @@ struct RowsFp16 {
     }
     // valid: bit k says that slot 2 q + (k & 1) + 8 (k >> 1) holds a row (the bytes of other slots may be anything, an Inf
     // or NaN pattern included, which a weight of zero would not silence).
-    template <int NT>
-    __device__ static __forceinline__ void v_side(const uint8_t* rec, int lane, RowsState<NT>& st, const uint32_t (&w)[NT][2], uint32_t valid) {
+    __device__ static __forceinline__ void v_operands(const uint8_t* rec, int lane, uint32_t (&a)[4][4], uint32_t valid) {
         const int g = lane >> 2, q = lane & 3;
         const uint8_t* v = rec + pool_codes_bytes(3) + (g >> 1) * kTileTokens * 16 + (g & 1) * 8;
         uint2 x[2][4];
@@ -443,19 +431,25 @@ struct RowsFp16 {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const uint32_t sel = (j & 1) ? 0x7632u : 0x5410u;
-            uint32_t a[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {              // a0, a1: slots 2q, 2q + 1 of channel groups 0, 1; a2, a3: slots 8 + 2q ..
                 const uint2 lo = x[k & 1][2 * (k >> 1)], hi = x[k & 1][2 * (k >> 1) + 1];
-                a[k] = j < 2 ? prmt(lo.x, hi.x, sel) : prmt(lo.y, hi.y, sel);
+                a[j][k] = j < 2 ? prmt(lo.x, hi.x, sel) : prmt(lo.y, hi.y, sel);
             }
-#pragma unroll
-            for (int n = 0; n < NT; ++n) mma_f16(st.acc[n][j], a, w[n][0], w[n][1]);
         }
     }
 };
+template <int NT>
+__device__ __forceinline__ void v_products(RowsState<NT>& st, const uint32_t (&a)[4][4], const uint32_t (&w)[NT][2]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) mma_f16(st.acc[n][j], a[j], w[n][0], w[n][1]);
+}
 
-// n tiles in a row that every row sees whole; stops in front of a tile with a weight that overflows.  Returns the tiles done.
+// Up to n tiles in a row that every row sees whole; stops in front of one with a weight that overflows.  Returns the tiles
+// done.  (Two tiles at a time, for more independent instructions, made the loops of the classes outgrow the innermost
+// instruction cache: 20 % slower on mixed pools.)
 template <int NT, class C>
 __device__ __forceinline__ uint32_t whole_tiles(const uint8_t* rec, uint32_t n, uint32_t step, int lane, const RowsQuery<NT>& qf,
                                                 float kfactor, RowsState<NT>& st) {
@@ -464,12 +458,14 @@ __device__ __forceinline__ uint32_t whole_tiles(const uint8_t* rec, uint32_t n, 
     for (; i < n; ++i, rec += step) {
         TileLogits<NT> t;
         C::template k_side<NT>(rec, lane, qf, kfactor, t);
+        uint32_t a[4][4];
+        C::v_operands(rec, lane, a, 15u);              // (in front of the vote: it fills the waits of the chain above)
         float2 p[NT][2];
         uint32_t w[NT][2];
         logits_of(st, t, true, p);
-        if (__builtin_expect(!weigh(t, p, w), 0)) break;
+        if (__builtin_expect(overflows(weigh(t, p, w)), 0)) break;
         add_tile(st, t, p, w);
-        C::template v_side<NT>(rec, lane, st, w, 15u);
+        v_products(st, a, w);
     }
     return i;
 }
@@ -548,7 +544,13 @@ __device__ __forceinline__ uint4 draft_row_as_stored(uint4 raw, int c) {
     return make_uint4(out[0], out[1], out[2], out[3]);
 }
 
-// grid = batch * kv_heads * parts * row_blocks, block = kRowsThreads, dynamic smem = rows_smem_bytes<NT>(draft tiles).
+// The record that CTA j writes for its piece of a unit: a CTA has at most two pieces that are not whole units, its first and
+// its last.  (The axis is shorter than 2^32: ticks * units is the number of units, or at most rows_max_units times the CTAs.)
+__device__ __forceinline__ uint32_t rows_record(const RowsParams& P, uint32_t j, uint32_t unit) {
+    return 2u * j + (j * P.span >= unit * P.ticks ? 0u : 1u);      // (it starts inside the unit, or in front of it)
+}
+
+// grid = CTAs of the plan, block = kRowsThreads, dynamic smem = rows_smem_bytes<NT>(draft tiles).
 // NT: blocks of eight rows per unit.  TREE: rows belong to drafted nodes (otherwise nodes == 1 and the row is the last
 // cached token's).
 template <int NT, bool TREE>
@@ -563,14 +565,10 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
     const StoreView& S = P.store;
 
-    uint32_t x = blockIdx.x;
-    const uint32_t rb = x % P.row_blocks;
-    x /= P.row_blocks;
-    const uint32_t part = x % P.parts, bh = x / P.parts;
-    const int b = (int)(bh / (uint32_t)S.kv_heads), h = (int)(bh - (uint32_t)b * S.kv_heads);
-    const uint32_t unit = bh * P.row_blocks + rb;
-    const bool has_draft = TREE && part + 1 == P.parts;
     const int draft_tiles = (P.nodes + kTileTokens - 1) / kTileTokens;
+    int cslot = 0;                                     // ring slot that is read next
+    uint32_t parity = 0;                               // phase parity of every ring slot (bit s: slot s)
+    bool failed = false;
 
     if (lane == 0) {
         for (int s = 0; s < kRowsStages; ++s) mbar_init(&sc.bars[warp][s], 1);
@@ -579,32 +577,196 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
     pdl_launch_dependents();
     pdl_wait();                                        // an append ahead of this launch has stored its tokens
 
+    // This CTA's stretch of the axis, in pieces: ticks [a0, a1) of unit u.  After an expired wait a warp starts no further
+    // copy, but every piece is delivered (empty), so that all arrival counters reach their totals.
+    uint32_t x = blockIdx.x * P.span;
+    const uint32_t x_end = x + P.span;
+#pragma unroll 1
+    while (x < x_end) {
+    const uint32_t unit = x / P.ticks, a0 = x - unit * P.ticks, a1 = min(P.ticks, a0 + (x_end - x));
+    x += a1 - a0;
+    const uint32_t rb = unit / P.pairs, bh = unit - rb * P.pairs;  // row blocks of a pair lie far apart: CTAs that run at the same time read the same tiles
+    const int b = (int)(bh / (uint32_t)S.kv_heads), h = (int)(bh - (uint32_t)b * S.kv_heads);
+    const bool has_draft = TREE && a1 == P.ticks;
+
+    // ---- what the piece starts from, requested together
     const uint4 fill = *reinterpret_cast<const uint4*>(P.counts + (size_t)b * 4);
+    const uint32_t first_id = lane < kNumPools ? stream_table(S, lane, P.layer, b, h)[0] : 0u;     // first block of every stream
+    // thread = (row, eight channels), up to 16 rows at a time
+    constexpr int RB = ROWS > 16 ? ROWS / 16 : 1;
+    const int row16 = tid >> 3, piece8 = tid & 7;
+    auto row_of = [&](int k) { return 16 * k + row16; };
+    auto place_of = [&](int k, int& node) -> size_t {  // of a row's eight channels in Q and O
+        const int R = (int)rb * ROWS + row_of(k);
+        node = R / P.group;
+        return (((size_t)b * P.nodes + node) * S.q_heads + (size_t)h * P.group + (R - node * P.group)) * kHeadDim + piece8 * 8;
+    };
+    auto row_used = [&](int k) { return row_of(k) < ROWS && (int)rb * ROWS + row_of(k) < P.rows; };
+    uint4 qv[RB];
+    int my_node[RB];
+#pragma unroll
+    for (int k = 0; k < RB; ++k) {
+        const size_t at = place_of(k, my_node[k]);
+        qv[k] = row_used(k) ? *reinterpret_cast<const uint4*>(P.Q + at) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    int par[2] = {-2, -2};
+    if (TREE && warp == 0) {
+        if (lane < P.nodes) par[0] = P.parents[(size_t)b * P.nodes + lane];
+        if (lane + 32 < P.nodes) par[1] = P.parents[(size_t)b * P.nodes + lane + 32];
+    }
     const int len = (int)(fill.x + fill.y + fill.z + fill.w);
 
-    // ---- the query block
-    float qmax = 0.f;
-    if (tid < 8 * ROWS) {                              // (whole warps) thread = (row, eight channels)
-        const int row = tid >> 3, piece = tid & 7;
-        const int R = (int)rb * ROWS + row;
-        const int node = R / P.group;
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (R < P.rows)
-            v = *reinterpret_cast<const uint4*>(P.Q + (((size_t)b * P.nodes + node) * S.q_heads + (size_t)h * P.group + (R - node * P.group)) * kHeadDim + piece * 8);
-        *reinterpret_cast<uint4*>(&sc.q[row][piece * 8]) = v;
-        const float2 f0 = unpack_half2(v.x), f1 = unpack_half2(v.y), f2 = unpack_half2(v.z), f3 = unpack_half2(v.w);
+    // ---- the window: where it and the sinks end in every pool (warp = class)
+    int base0 = 0;                                     // first position that the shallowest row's window holds
+    if (P.window > 0) {
+        base0 = min(max(len - P.window + (TREE ? 1 : 0), 0), len);
+        const uint32_t c = (uint32_t)warp;
+        const uint32_t n = c == 0 ? fill.x : c == 1 ? fill.y : c == 2 ? fill.z : fill.w;
+        const uint32_t* idx = S.index + ((size_t)P.layer * S.batch + b) * S.max_ctx;
+        const uint32_t start = first_slot_from(idx, base0, len, c, n, lane);
+        const uint32_t sink = P.sinks > 0 ? first_slot_from(idx, min(P.sinks, len), len, c, n, lane) : 0u;
+        unsigned long long bits = 0;
+        if (TREE) {
+            uint32_t m[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int at = base0 + 32 * k + lane;
+                m[k] = __ballot_sync(0xffffffffu, at < len && (idx[min(at, len - 1)] >> 30) == c);
+            }
+            bits = ((unsigned long long)m[1] << 32) | m[0];
+        }
+        if (lane == 0) {
+            sc.start[c] = start;
+            sc.sink[c] = sink;
+            sc.step_bits[c] = bits;
+        }
+        __syncthreads();
+    }
+    // ---- this warp's share: tile ranges of the pools, laid end to end [sinks | window] per pool; lane = pool
+    const uint32_t ring = (uint32_t)warp * kRowsStages * kRowsStageBytes;          // offset in dyn
+    RowsChunks& plan = sc.plan[warp];
+    {
+        const int c = lane & 3;
+        const uint32_t n_c = c == 0 ? fill.x : c == 1 ? fill.y : c == 2 ? fill.z : fill.w;
+        const uint32_t start = P.window > 0 ? sc.start[c] : 0u, sink = P.window > 0 ? sc.sink[c] : 0u;
+        const int nt = (int)((n_c + kTileTokens - 1) / kTileTokens);
+        int ns = (int)((sink + kTileTokens - 1) / kTileTokens), ws = (int)(start / kTileTokens);
+        if (ws <= ns) ns = ws = 0;                     // no gap
+        const int n = ns + nt - ws;
+        const float cost = (float)kRowsTileCost[c], weight = (float)n * cost;
+        float before = 0.f, total = 0.f;
+#pragma unroll
+        for (int k = 0; k < kNumPools; ++k) {
+            const float wk = __shfl_sync(0xffffffffu, weight, k);
+            before += k < c ? wk : 0.f;
+            total += wk;
+        }
+        // The end of a share and the start of the next one are the same expression of the same tick, which does not fall as
+        // the tick grows; the last share ends with the last tile.  So no tile is lost or taken twice, however this rounds.
+        const uint32_t t0 = a0 * kRowsWarps + (a1 - a0) * warp, t1 = t0 + (a1 - a0), T = P.ticks * kRowsWarps;
+        const float scale = total / (float)T, inv = 1.0f / cost;
+        const float pool_scale = (float)n / (float)T;
+        auto tiles_before = [&](uint32_t t) {
+            return t == T ? n : min(max((int)(P.by_pool ? pool_scale * (float)t : (scale * (float)t - before) * inv), 0), n);
+        };
+        const int lo = tiles_before(t0), hi = tiles_before(t1);
+        if (lane < kNumPools) {
+            sc.seg_lo[warp][2 * c] = lo;
+            sc.seg_hi[warp][2 * c] = min(hi, ns);
+            sc.seg_lo[warp][2 * c + 1] = max(lo, ns) - ns + ws;
+            sc.seg_hi[warp][2 * c + 1] = hi - ns + ws;
+            if (warp == 0) {
+                const uint32_t lo_last = P.window > 0 ? start + (TREE ? (uint32_t)__popcll(sc.step_bits[c]) : 0u) : 0u;
+                sc.cnt[c] = n_c;
+                if (P.window == 0) sc.start[c] = sc.sink[c] = 0u;
+                sc.in_sinks[c] = (int)(sink / kTileTokens);
+                sc.from[c] = (int)((lo_last + kTileTokens - 1) / kTileTokens);
+                sc.full[c] = (int)(n_c / kTileTokens);
+            }
+            if (lane == 0) {
+                plan.seg = 0;
+                plan.tile = lo;
+            }
+        }
+    }
+    float qmax = 0.f;                                  // the query block
+#pragma unroll
+    for (int k = 0; k < RB; ++k) {
+        const float2 f0 = unpack_half2(qv[k].x), f1 = unpack_half2(qv[k].y), f2 = unpack_half2(qv[k].z), f3 = unpack_half2(qv[k].w);
         float sum = ((f0.x + f0.y) + (f1.x + f1.y)) + ((f2.x + f2.y) + (f3.x + f3.y));
-        qmax = fmaxf(fmaxf(fmaxf(fabsf(f0.x), fabsf(f0.y)), fmaxf(fabsf(f1.x), fabsf(f1.y))),
-                     fmaxf(fmaxf(fabsf(f2.x), fabsf(f2.y)), fmaxf(fabsf(f3.x), fabsf(f3.y))));
+        qmax = fmaxf(qmax, fmaxf(fmaxf(fmaxf(fabsf(f0.x), fabsf(f0.y)), fmaxf(fabsf(f1.x), fabsf(f1.y))),
+                                 fmaxf(fmaxf(fabsf(f2.x), fabsf(f2.y)), fmaxf(fabsf(f3.x), fabsf(f3.y)))));
 #pragma unroll
         for (int d = 1; d < 8; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        if (piece == 0) {
-            sc.sumq[row] = sum * kLogitScale;
-            sc.node[row] = (int16_t)(R < P.rows ? node : -1);
+        if (row_of(k) < ROWS) {
+            *reinterpret_cast<uint4*>(&sc.q[row_of(k)][piece8 * 8]) = qv[k];
+            if (piece8 == 0) {
+                sc.sumq[row_of(k)] = sum * kLogitScale;
+                sc.node[row_of(k)] = (int16_t)(row_used(k) ? my_node[k] : -1);
+            }
         }
     }
     qmax = warp_max(qmax);
     if (lane == 0) sc.wmax[warp] = qmax;
+    __syncthreads();
+
+    // ---- the copies: chunks of the share in order; a chunk stays inside one 64 KB block and fits a stage
+    int planned = 0, taken = 0;
+    auto plan_more = [&]() {                           // (whole warp) the chunks up to the end of the range or of the block
+        __syncwarp();
+        const int from_seg = plan.seg, my_seg = lane & (2 * kNumPools - 1);
+        const int my_lo = my_seg == from_seg ? plan.tile : sc.seg_lo[warp][my_seg], my_hi = sc.seg_hi[warp][my_seg];
+        const uint32_t open = __ballot_sync(0xffffffffu, my_seg >= from_seg && my_lo < my_hi) & 0xffu;
+        planned = taken = 0;
+        if (open == 0) return;
+        const int seg = __ffs(open) - 1, tile = __shfl_sync(0xffffffffu, my_lo, seg), hi = __shfl_sync(0xffffffffu, my_hi, seg);
+        const int c = seg >> 1, bt = (int)block_tiles(c), tps = kRowsTps(c);
+        const uint32_t rec = (uint32_t)(c == 0 ? pool_rec_bytes(0) : c == 1 ? pool_rec_bytes(1) : c == 2 ? pool_rec_bytes(2) : pool_rec_bytes(3));
+        int blk = 0, ib = tile;
+        uint32_t id = __shfl_sync(0xffffffffu, first_id, c);
+        if (tile >= bt) {
+            blk = tile / bt;
+            ib = tile - blk * bt;
+            id = stream_table(S, c, P.layer, b, h)[blk];
+        }
+        const int in_sinks = sc.in_sinks[c], from = sc.from[c], full = sc.full[c];
+        const int piece = min(bt - ib, hi - tile);
+        planned = min(c == 3 ? piece : c == 2 ? (piece + 1) >> 1 : c == 1 ? (piece + 3) >> 2 : (piece + 5) / 6, 32);
+        const int t0 = tile + lane * tps, n = min(tps, tile + piece - t0);
+        uint32_t edge = 0;
+#pragma unroll
+        for (int i = 0; i < kRowsTps(0); ++i) edge |= i < n && !(t0 + i < full && (t0 + i >= from || t0 + i < in_sinks)) ? 1u << i : 0u;
+        const uint8_t* src = S.arena + (size_t)id * kBlockBytes + (uint32_t)(ib + lane * tps) * rec;
+        if (lane < planned)
+            plan.chunk[lane] = make_uint4((uint32_t)(uintptr_t)src, (uint32_t)((uintptr_t)src >> 32), (uint32_t)t0 | ((uint32_t)c << 30),
+                                          (uint32_t)n * rec | ((uint32_t)n << 16) | (edge << 20));
+        __syncwarp();
+        if (lane == 0) {
+            plan.seg = seg;
+            plan.tile = tile + min(piece, planned * tps);
+        }
+        __syncwarp();
+    };
+    auto feed = [&](int slot) -> int {                 // start the next copy; 0 if there is none
+        if (taken == planned) {
+            plan_more();
+            if (planned == 0) return 0;
+        }
+        if (lane == 0) {
+            const uint4 k = plan.chunk[taken];
+            const uint32_t bytes = k.w & 0xffffu;
+            mbar_arrive_expect_tx(&sc.bars[warp][slot], bytes);
+            bulk_load(dyn + ring + (uint32_t)slot * kRowsStageBytes, reinterpret_cast<const uint8_t*>((uintptr_t)k.x | ((uintptr_t)k.y << 32)), bytes,
+                      &sc.bars[warp][slot]);
+            sc.chunk[warp][slot] = make_uint2(k.z, k.w >> 16);
+        }
+        ++taken;
+        return 1;
+    };
+    int in_flight = 0;
+#pragma unroll 1
+    for (; in_flight < kRowsStages; ++in_flight)
+        if (failed || !feed((cslot + in_flight) % kRowsStages)) break;
 
     // ---- the tree: ancestors by doubling the chain of parents
     if (TREE && warp == 0) {
@@ -613,16 +775,17 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const int i = lane + 32 * k;
-            const int par = i < P.nodes ? P.parents[(size_t)b * P.nodes + i] : -2;
-            bad[k] = !(par >= -1 && par < i);
-            link[k] = bad[k] ? -1 : par;
+            bad[k] = !(par[k] >= -1 && par[k] < i);
+            link[k] = bad[k] ? -1 : par[k];
             a[k] = 1ull << i;
             sc.anc[i] = a[k];
             sc.link[i] = (int8_t)link[k];
             sc.bad[i] = (int8_t)bad[k];
         }
-        for (int round = 0; round < 6; ++round) {
+#pragma unroll 1
+        while (true) {                                 // (six rounds at most)
             __syncwarp();
+            if (!__any_sync(0xffffffffu, link[0] >= 0 || link[1] >= 0)) break;
 #pragma unroll
             for (int k = 0; k < 2; ++k)
                 if (link[k] >= 0) {
@@ -655,46 +818,18 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
             sc.vis[lane + 32 * k] = v;
         }
     }
-    // ---- the window: where it and the sinks end in every pool (warp = class)
-    int base0 = 0;                                     // first position that the shallowest row's window holds
-    if (P.window > 0) base0 = min(max(len - P.window + (TREE ? 1 : 0), 0), len);
-    {
-        const uint32_t c = (uint32_t)warp;
-        const uint32_t n = c == 0 ? fill.x : c == 1 ? fill.y : c == 2 ? fill.z : fill.w;
-        uint32_t start = 0, sink = 0;
-        unsigned long long bits = 0;
-        if (P.window > 0) {
-            const uint32_t* idx = S.index + ((size_t)P.layer * S.batch + b) * S.max_ctx;
-            start = first_slot_from(idx, base0, len, c, n, lane);
-            sink = P.sinks > 0 ? first_slot_from(idx, min(P.sinks, len), len, c, n, lane) : 0u;
-            if (TREE) {
-                uint32_t m[2];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int at = base0 + 32 * k + lane;
-                    m[k] = __ballot_sync(0xffffffffu, at < len && (idx[min(at, len - 1)] >> 30) == c);
-                }
-                bits = ((unsigned long long)m[1] << 32) | m[0];
-            }
-        }
-        if (lane == 0) {
-            sc.cnt[c] = n;
-            sc.start[c] = start;
-            sc.sink[c] = sink;
-            sc.step_bits[c] = bits;
-        }
-    }
     // ---- drafted rows as fp16 tiles
     if (has_draft) {
         const int padded = draft_tiles * kTileTokens;
+#pragma unroll 1
         for (int k = 0; k < 2 * padded; k += kRowsThreads / 8) {
-            const int i = k + (tid >> 3), piece = tid & 7;
+            const int i = k + row16;
             const bool value = i >= padded;
             const int node = value ? i - padded : i;
             uint4 raw = make_uint4(0u, 0u, 0u, 0u);
             int c = 3;
             if (node < P.nodes) {
-                raw = *reinterpret_cast<const uint4*>((value ? P.V : P.K) + (((size_t)b * P.nodes + node) * S.kv_heads + h) * kHeadDim + piece * 8);
+                raw = *reinterpret_cast<const uint4*>((value ? P.V : P.K) + (((size_t)b * P.nodes + node) * S.kv_heads + h) * kHeadDim + piece8 * 8);
                 if (P.bits) {
                     c = bits_to_class(P.bits[(size_t)b * P.nodes + node]);
                     if (c < 0) {                       // as in an append: kept as fp16, and flagged
@@ -705,13 +840,40 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
             }
             const uint4 row = draft_row_as_stored(raw, c);
             *reinterpret_cast<uint4*>(draft + (node / kTileTokens) * kDraftTileBytes + (value ? kDraftTileBytes / 2 : 0) +
-                                      (piece * kTileTokens + node % kTileTokens) * 16) = row;
+                                      (piece8 * kTileTokens + node % kTileTokens) * 16) = row;
+        }
+    }
+
+    // ---- column operands of the K product, one set per class (warp = class): q * F * 2^-k, F a power of two that puts the
+    // block's largest query value below 2^15
+    const float block_max = fmaxf(fmaxf(fmaxf(sc.wmax[0], sc.wmax[1]), fmaxf(sc.wmax[2], sc.wmax[3])), 6.103515625e-05f);
+    const int e_max = (int)(__float_as_uint(block_max) >> 23) - 127;           // -14 .. 15
+    const float F = two_to(14 - e_max);
+    {
+        // The channels and bits of the classes' K operands (RowsQuant, RowsFp16) as sums of a part each of q, r, s & 1, s >> 1 and x.
+        const int c = warp, at_q = q * (16 >> c), at_r = c == 3 ? 8 : 1, at_x = c == 0 ? 8 : c == 1 ? 4 : c == 2 ? 2 : 1;
+        const int at_s1 = c < 2 ? 2 : 16, at_s2 = c == 0 ? 4 : 32;         // of s & 1 and of s >> 1
+        const float f1 = c == 0 ? F * 0.25f : c == 1 ? F * 0.0625f : F;    // r = 1
+        const float f2 = c == 0 ? 0.0625f : 1.0f;                          // s & 1
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {                 // column g of block n
+            const __half* row = sc.q[8 * n + g] + at_q;
+#pragma unroll
+            for (int s2 = 0; s2 < 2; ++s2) {
+                uint32_t w[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {          // step s = 2 s2 + (k >> 1), register r = k & 1
+                    const __half* e = row + s2 * at_s2 + (k >> 1) * at_s1 + (k & 1) * at_r;
+                    const float f = ((k & 1) ? f1 : F) * ((k >> 1) ? f2 : 1.0f);
+                    w[k] = pack_half2(make_float2(__half2float(e[0]) * f, __half2float(e[at_x]) * f));
+                }
+                qfrag[((warp * NT + n) * 2 + s2) * 32 + lane] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
         }
     }
     __syncthreads();
-
     // ---- first window slot of every row, per class
-    if (P.window > 0)
+    if (P.window > 0) {
         for (int k = tid; k < kNumPools * ROWS; k += kRowsThreads) {
             const int c = k / ROWS, row = k - c * ROWS;
             uint32_t lo = sc.start[c];
@@ -722,131 +884,8 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
             }
             sc.lo_row[c][row] = lo;
         }
-    // ---- this warp's share: tile ranges of the pools, laid end to end [sinks | window] per pool
-    if (lane < kNumPools) {
-        const int c = lane;
-        const int nt = (int)((sc.cnt[c] + kTileTokens - 1) / kTileTokens);
-        int ns = (int)((sc.sink[c] + kTileTokens - 1) / kTileTokens), ws = (int)(sc.start[c] / kTileTokens);
-        if (ws <= ns) ns = ws = 0;                     // no gap
-        const uint32_t n = (uint32_t)(ns + nt - ws), cost = kRowsTileCost[c];
-        uint32_t before = 0, total = 0;
-#pragma unroll
-        for (int k = 0; k < kNumPools; ++k) {
-            const uint32_t wk = __shfl_sync(0xfu, n * cost, k);
-            before += k < c ? wk : 0u;
-            total += wk;
-        }
-        // floor(total * j / shares) without a 64-bit division (shares <= 256)
-        const uint32_t shares = P.parts * kRowsWarps, me = part * kRowsWarps + warp, whole = total / shares, rest = total - whole * shares;
-        const int r0 = (int)(whole * me + rest * me / shares) - (int)before;
-        const int r1 = (int)(whole * (me + 1) + rest * (me + 1) / shares) - (int)before;
-        // the same rounding for a share's end and the next one's start
-        const int lo = min(max(r0, 0) / (int)cost, (int)n);
-        const int hi = me + 1 == shares ? (int)n : min(max(r1, 0) / (int)cost, (int)n);
-        sc.seg_lo[warp][2 * c] = lo;
-        sc.seg_hi[warp][2 * c] = min(hi, ns);
-        sc.seg_lo[warp][2 * c + 1] = max(lo, ns) - ns + ws;
-        sc.seg_hi[warp][2 * c + 1] = hi - ns + ws;
+        __syncthreads();
     }
-    __syncwarp();
-
-    // ---- the copies: chunks of the share in order; a chunk stays inside one 64 KB block and fits a stage
-    const uint32_t ring = (uint32_t)warp * kRowsStages * kRowsStageBytes;          // offset in dyn
-    RowsChunks& plan = sc.plan[warp];
-    int planned = 0, taken = 0;
-    auto plan_more = [&]() {                           // (whole warp) the chunks up to the end of the range or of the block
-        __syncwarp();
-        int seg = plan.seg, tile = plan.tile;
-        planned = taken = 0;
-        while (tile >= sc.seg_hi[warp][seg]) {
-            if (++seg == 2 * kNumPools) return;
-            tile = sc.seg_lo[warp][seg];
-        }
-        const int c = seg >> 1, bt = (int)block_tiles(c), blk = tile / bt, ib = tile - blk * bt, tps = kRowsTps(c);
-        const uint32_t rec = (uint32_t)(c == 0 ? pool_rec_bytes(0) : c == 1 ? pool_rec_bytes(1) : c == 2 ? pool_rec_bytes(2) : pool_rec_bytes(3));
-        const uint8_t* src = S.arena + (size_t)stream_table(S, c, P.layer, b, h)[blk] * kBlockBytes + (uint32_t)ib * rec;
-        const int in_sinks = sc.in_sinks[c], from = sc.from[c], full = sc.full[c];
-        const int piece = min(bt - ib, sc.seg_hi[warp][seg] - tile);
-        planned = min((piece + tps - 1) / tps, 32);
-        const int t0 = tile + lane * tps, n = min(tps, tile + piece - t0);
-        uint32_t edge = 0;
-        for (int i = 0; i < n; ++i) edge |= t0 + i < full && (t0 + i >= from || t0 + i < in_sinks) ? 0u : 1u << i;
-        src += (size_t)((uint32_t)(lane * tps) * rec);
-        if (lane < planned)
-            plan.chunk[lane] = make_uint4((uint32_t)(uintptr_t)src, (uint32_t)((uintptr_t)src >> 32), (uint32_t)t0 | ((uint32_t)c << 30),
-                                          (uint32_t)n * rec | ((uint32_t)n << 16) | (edge << 20));
-        __syncwarp();
-        if (lane == 0) {
-            plan.seg = seg;
-            plan.tile = tile + min(piece, planned * tps);
-        }
-        __syncwarp();
-    };
-    auto feed = [&](int slot) -> int {                 // start the next copy; 0 if there is none
-        if (taken == planned) {
-            plan_more();
-            if (planned == 0) return 0;
-        }
-        if (lane == 0) {
-            const uint4 k = plan.chunk[taken];
-            const uint32_t bytes = k.w & 0xffffu;
-            mbar_arrive_expect_tx(&sc.bars[warp][slot], bytes);
-            bulk_load(dyn + ring + (uint32_t)slot * kRowsStageBytes, reinterpret_cast<const uint8_t*>((uintptr_t)k.x | ((uintptr_t)k.y << 32)), bytes,
-                      &sc.bars[warp][slot]);
-            sc.chunk[warp][slot] = make_uint2(k.z, k.w >> 16);
-        }
-        ++taken;
-        return 1;
-    };
-    int in_flight = 0, cslot = 0;
-    uint32_t parity = 0;
-    bool failed = false;
-    if (lane < kNumPools) {
-        const int c = lane;
-        const uint32_t lo_last = P.window > 0 ? sc.start[c] + (TREE ? (uint32_t)__popcll(sc.step_bits[c]) : 0u) : 0u;
-        if (warp == 0) {
-            sc.in_sinks[c] = (int)(sc.sink[c] / kTileTokens);
-            sc.from[c] = (int)((lo_last + kTileTokens - 1) / kTileTokens);
-            sc.full[c] = (int)(sc.cnt[c] / kTileTokens);
-        }
-        if (lane == 0) {
-            plan.seg = 0;
-            plan.tile = sc.seg_lo[warp][0];
-        }
-    }
-    __syncthreads();
-#pragma unroll 1
-    for (; in_flight < kRowsStages; ++in_flight)
-        if (!feed(in_flight)) break;
-
-    // ---- column operands of the K product, one set per class (warp = class): q * F * 2^-k, F a power of two that puts the
-    // block's largest query value below 2^15
-    const float block_max = fmaxf(fmaxf(fmaxf(sc.wmax[0], sc.wmax[1]), fmaxf(sc.wmax[2], sc.wmax[3])), 6.103515625e-05f);
-    const int e_max = (int)(__float_as_uint(block_max) >> 23) - 127;           // -14 .. 15
-    const float F = two_to(14 - e_max);
-    {
-        auto build = [&](auto channel, auto bit) {     // column g of block n: step s, register r = channels of lane q
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int s2 = 0; s2 < 2; ++s2) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int s = 2 * s2 + (k >> 1), r = k & 1;
-                        const __half* row = sc.q[8 * n + g];
-                        const float f = F * two_to(-bit(s, r));
-                        w[k] = pack_half2(make_float2(__half2float(row[channel(s, r, q, 0)]) * f, __half2float(row[channel(s, r, q, 1)]) * f));
-                    }
-                    qfrag[((warp * NT + n) * 2 + s2) * 32 + lane] = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-        };
-        if (warp == 0) build(RowsQuant<0>::k_channel, RowsQuant<0>::k_bit);
-        else if (warp == 1) build(RowsQuant<1>::k_channel, RowsQuant<1>::k_bit);
-        else if (warp == 2) build(RowsQuant<2>::k_channel, RowsQuant<2>::k_bit);
-        else build(RowsFp16::k_channel, [](int, int) { return 0; });
-    }
-    __syncthreads();
 
     // ---- the walk
     RowsState<NT> st;
@@ -869,6 +908,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
     RowsQuery<NT> qf;
     // One tile of class c in general.  There is one copy of this code for all classes, and a short loop per class for the
     // tiles in the middle (whole_tiles): the loops have to stay inside the instruction caches.
+    bool fresh = true;                                 // no reference has been set yet
     auto any_tile = [&](int c, const uint8_t* rec, bool edge, const uint32_t (&seen)[NT], uint32_t valid) {
         TileLogits<NT> t;
         if (c == 0) RowsQuant<0>::k_side<NT>(rec, lane, qf, kfactor, t);
@@ -877,17 +917,21 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
         else RowsFp16::k_side<NT>(rec, lane, qf, kfactor, t);
         float2 p[NT][2];
         uint32_t w[NT][2];
-        for (int moved = 0; moved < 2; ++moved) {
+#pragma unroll 1
+        for (bool moved = false;; moved = true) {
+            if (moved || fresh) move_references(st, t, edge, seen);
             logits_of(st, t, true, p);
             hide(edge, seen, p);
-            if (weigh(t, p, w) || moved) break;
-            move_references(st, t, edge, seen);
+            if (!overflows(weigh(t, p, w)) || moved || fresh) break;
         }
+        fresh = false;
         add_tile(st, t, p, w);
-        if (c == 0) RowsQuant<0>::v_side<NT>(rec, lane, st, w, valid);
-        else if (c == 1) RowsQuant<1>::v_side<NT>(rec, lane, st, w, valid);
-        else if (c == 2) RowsQuant<2>::v_side<NT>(rec, lane, st, w, valid);
-        else RowsFp16::v_side<NT>(rec, lane, st, w, valid);
+        uint32_t a[4][4];
+        if (c == 0) RowsQuant<0>::v_operands(rec, lane, a, valid);
+        else if (c == 1) RowsQuant<1>::v_operands(rec, lane, a, valid);
+        else if (c == 2) RowsQuant<2>::v_operands(rec, lane, a, valid);
+        else RowsFp16::v_operands(rec, lane, a, valid);
+        v_products(st, a, w);
     };
     int cls = 3;
     bool draft_left = has_draft && warp < draft_tiles; // a tile of drafted tokens per warp, at the end
@@ -912,8 +956,8 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
 #pragma unroll 1
         while (true) {
             const uint32_t run = edges ? (uint32_t)__ffs(edges) - 1u : left;
-            if (run > 0) {
-                uint32_t done;
+            if (run > 0 && !fresh) {
+                uint32_t done = 0;
                 if (c == 0) done = whole_tiles<NT, RowsQuant<0>>(rec, run, pool_rec_bytes(0), lane, qf, kfactor, st);
                 else if (c == 1) done = whole_tiles<NT, RowsQuant<1>>(rec, run, pool_rec_bytes(1), lane, qf, kfactor, st);
                 else if (c == 2) done = whole_tiles<NT, RowsQuant<2>>(rec, run, pool_rec_bytes(2), lane, qf, kfactor, st);
@@ -1012,20 +1056,20 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
     __syncthreads();
 
     // ---- this CTA's rows: thread = (row, eight channels)
-    auto store_row = [&](int row, const float (&o)[8], float L) {
-        const int R = (int)rb * ROWS + row;
-        if (R >= P.rows) return;
-        const int node = R / P.group;
+    auto store_row = [&](int k, const float (&o)[8], float L) {
+        if (!row_used(k)) return;
+        int node;
+        const size_t at = place_of(k, node);
         const float inv = L > 0.f && (!TREE || sc.vis[node]) ? 1.0f / L : 0.f;     // nothing seen, or an unused node: zeros
         uint32_t v[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = inv != 0.f ? pack_half2(make_float2(o[2 * k] * inv, o[2 * k + 1] * inv)) : 0u;
-        *reinterpret_cast<uint4*>(P.O + (((size_t)b * P.nodes + node) * S.q_heads + (size_t)h * P.group + (R - node * P.group)) * kHeadDim + (tid & 7) * 8) =
-            make_uint4(v[0], v[1], v[2], v[3]);
+        for (int e = 0; e < 4; ++e) v[e] = inv != 0.f ? pack_half2(make_float2(o[2 * e] * inv, o[2 * e + 1] * inv)) : 0u;
+        *reinterpret_cast<uint4*>(P.O + at) = make_uint4(v[0], v[1], v[2], v[3]);
     };
-    const bool mine = tid < 8 * ROWS;
-    const int row = tid >> 3;
-    if (mine) {
+#pragma unroll 1
+    for (int k = 0; k < RB; ++k) {
+        const int row = row_of(k);
+        if (row >= ROWS) break;
         float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         float M = kNegBig, L = 0.f;
 #pragma unroll
@@ -1033,48 +1077,59 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
 #pragma unroll
         for (int w = 0; w < kRowsWarps; ++w) {
             L = fmaf(sc.ml[w][row].y, fast_exp2(sc.ml[w][row].x - M), L);
-            const float4* src = reinterpret_cast<const float4*>(out + ((size_t)w * ROWS + row) * kRowsOutStride + (tid & 7) * 8);
+            const float4* src = reinterpret_cast<const float4*>(out + ((size_t)w * ROWS + row) * kRowsOutStride + piece8 * 8);
             const float4 v0 = src[0], v1 = src[1];
             o[0] += v0.x; o[1] += v0.y; o[2] += v0.z; o[3] += v0.w;
             o[4] += v1.x; o[5] += v1.y; o[6] += v1.z; o[7] += v1.w;
         }
-        if (P.parts == 1) {
-            store_row(row, o, L);
+        if (a1 - a0 == P.ticks) {
+            store_row(k, o, L);
         } else {
-            const size_t rec = ((size_t)unit * P.parts + part) * ROWS + row;
-            float4* dst = reinterpret_cast<float4*>(P.part_o + rec * kHeadDim + (tid & 7) * 8);
+            const size_t rec = (size_t)rows_record(P, blockIdx.x, unit) * ROWS + row;
+            float4* dst = reinterpret_cast<float4*>(P.part_o + rec * kHeadDim + piece8 * 8);
             dst[0] = make_float4(o[0], o[1], o[2], o[3]);
             dst[1] = make_float4(o[4], o[5], o[6], o[7]);
-            if ((tid & 7) == 0) P.part_ml[rec] = make_float2(M, L);
+            if (piece8 == 0) P.part_ml[rec] = make_float2(M, L);
         }
     }
-    if (P.parts == 1) return;
-
-    // ---- the CTA that delivers the unit's last part merges the parts, in part order
-    __threadfence();
-    __syncthreads();
-    if (tid == 0) sc.last = atomicAdd(P.part_cnt + unit, 1u) + 1u == P.parts ? 1u : 0u;
-    __syncthreads();
-    if (!sc.last) return;
-    __threadfence();
-    if (tid == 0) P.part_cnt[unit] = 0u;
-    if (!mine) return;
-    const size_t rec0 = (size_t)unit * P.parts * ROWS + row;
-    float M = kNegBig, L = 0.f;
-    for (uint32_t s = 0; s < P.parts; ++s) M = fmaxf(M, __ldcg(P.part_ml + rec0 + (size_t)s * ROWS).x);
-    float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (uint32_t s = 0; s < P.parts; ++s) {
-        const size_t rec = rec0 + (size_t)s * ROWS;
-        const float2 ml = __ldcg(P.part_ml + rec);
-        const float4* src = reinterpret_cast<const float4*>(P.part_o + rec * kHeadDim + (tid & 7) * 8);
-        const float4 v0 = __ldcg(src), v1 = __ldcg(src + 1);
-        const float f = fast_exp2(ml.x - M);
-        L = fmaf(ml.y, f, L);
-        o[0] = fmaf(v0.x, f, o[0]); o[1] = fmaf(v0.y, f, o[1]); o[2] = fmaf(v0.z, f, o[2]); o[3] = fmaf(v0.w, f, o[3]);
-        o[4] = fmaf(v1.x, f, o[4]); o[5] = fmaf(v1.y, f, o[5]); o[6] = fmaf(v1.z, f, o[6]); o[7] = fmaf(v1.w, f, o[7]);
+    if (a1 - a0 < P.ticks) {
+        // ---- the CTA that delivers the unit's last piece merges the pieces, in order
+        const uint32_t first = unit * P.ticks / P.span, pieces = ((unit + 1) * P.ticks - 1) / P.span - first + 1;
+        __syncthreads();
+        if (tid == 0) {
+            __threadfence();                           // (covers the whole CTA's records, which the barrier has ordered before it)
+            sc.last = atomicAdd(P.part_cnt + unit, 1u) + 1u == pieces ? 1u : 0u;
+            __threadfence();
+        }
+        __syncthreads();
+        if (sc.last) {
+            if (tid == 0) P.part_cnt[unit] = 0u;
+#pragma unroll 1
+            for (int k = 0; k < RB; ++k) {
+                const int row = row_of(k);
+                if (row >= ROWS) break;
+                float M = kNegBig, L = 0.f;
+                float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+                for (uint32_t s = 0; s < pieces; ++s) {
+                    const size_t rec = (size_t)rows_record(P, first + s, unit) * ROWS + row;
+                    const float2 ml = __ldcg(P.part_ml + rec);
+                    const float4* src = reinterpret_cast<const float4*>(P.part_o + rec * kHeadDim + piece8 * 8);
+                    const float4 v0 = __ldcg(src), v1 = __ldcg(src + 1);
+                    const float top = fmaxf(M, ml.x), f = fast_exp2(ml.x - top), r = fast_exp2(M - top);
+                    M = top;
+                    L = fmaf(L, r, ml.y * f);
+                    o[0] = fmaf(o[0], r, v0.x * f); o[1] = fmaf(o[1], r, v0.y * f); o[2] = fmaf(o[2], r, v0.z * f); o[3] = fmaf(o[3], r, v0.w * f);
+                    o[4] = fmaf(o[4], r, v1.x * f); o[5] = fmaf(o[5], r, v1.y * f); o[6] = fmaf(o[6], r, v1.z * f); o[7] = fmaf(o[7], r, v1.w * f);
+                }
+                store_row(k, o, L);
+            }
+        }
     }
-    store_row(row, o, L);
+    // the next piece's copies overwrite the merge buffer through the asynchronous proxy
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    }
 }
 
 }  // namespace kvq

@@ -67,9 +67,9 @@ struct kvq_ctx {
     float* part_s2 = nullptr;            //                [units][partial slots] sum of squared weights (kvq_decode_attn_var)
     float* unit_var = nullptr;           //                [units] variance of a unit's attention weights
     uint32_t* vis = nullptr;             // kvq_attend_last: visible pool fills [batch][query rows of a launch][4]
-    float* rows_o = nullptr;             // many-row attention scratch [records][kRowsMaxRows][64]
-    float2* rows_ml = nullptr;           //                            [records][kRowsMaxRows]
-    uint32_t* rows_cnt = nullptr;        //                            [records] arrival counters, zero between launches
+    float* rows_o = nullptr;             // many-row attention scratch [record rows][64]
+    float2* rows_ml = nullptr;           //                            [record rows]
+    uint32_t* rows_cnt = nullptr;        // [rows_max_units] arrival counters, zero between launches
     int splits_override = 0;
     int chunk_override = 0;              // kvq_set_append_chunk: 0 = automatic, else tokens per thread of a prefill chunk
     uint32_t* flags = nullptr;
@@ -727,10 +727,10 @@ int create_impl(kvq_ctx** out, int layers, int q_heads, int kv_heads, int head_d
     ok = ok && dev_alloc(c, &c->part_s2, sizeof(float) * max_partial_records(c)) == cudaSuccess;
     ok = ok && dev_alloc(c, &c->unit_var, sizeof(float) * units) == cudaSuccess;
     ok = ok && dev_alloc(c, &c->vis, sizeof(uint32_t) * 4 * (size_t)batch * kMaxQueryRows) == cudaSuccess;
-    const size_t rows_records = rows_max_records(c->sm_count);
-    ok = ok && dev_alloc(c, &c->rows_o, sizeof(float) * rows_records * kRowsMaxRows * kHeadDim) == cudaSuccess;
-    ok = ok && dev_alloc(c, &c->rows_ml, sizeof(float2) * rows_records * kRowsMaxRows) == cudaSuccess;
-    ok = ok && dev_alloc(c, &c->rows_cnt, sizeof(uint32_t) * rows_records) == cudaSuccess;
+    const size_t rows_records = rows_max_record_rows(c->sm_count);
+    ok = ok && dev_alloc(c, &c->rows_o, sizeof(float) * rows_records * kHeadDim) == cudaSuccess;
+    ok = ok && dev_alloc(c, &c->rows_ml, sizeof(float2) * rows_records) == cudaSuccess;
+    ok = ok && dev_alloc(c, &c->rows_cnt, sizeof(uint32_t) * rows_max_units(c->sm_count)) == cudaSuccess;
     ok = ok && dev_alloc(c, &c->d_lens, sizeof(int) * 3 * (size_t)batch * kvq_ctx::kLenSlots) == cudaSuccess;
     ok = ok && dev_alloc(c, &c->flags, sizeof(uint32_t)) == cudaSuccess;
     ok = ok && dev_alloc(c, &c->st_feats, sizeof(float) * 4 * batch) == cudaSuccess;
@@ -767,8 +767,8 @@ int create_impl(kvq_ctx** out, int layers, int q_heads, int kv_heads, int head_d
         ok = ok && cudaMemset(c->chunk_arrivals, 0, sizeof(uint32_t) * batch) == cudaSuccess;
         ok = ok && cudaMemset(c->step_cls, 0, sizeof(uint32_t) * batch) == cudaSuccess;
         ok = ok && cudaMemset(c->part_cnt, 0, sizeof(uint32_t) * units * kMaxQueryRows) == cudaSuccess;
-        ok = ok && cudaMemset(c->rows_cnt, 0, sizeof(uint32_t) * rows_records) == cudaSuccess;
-        ok = ok && rows_setup() == cudaSuccess;
+        ok = ok && cudaMemset(c->rows_cnt, 0, sizeof(uint32_t) * rows_max_units(c->sm_count)) == cudaSuccess;
+        ok = ok && rows_setup(c->device) == cudaSuccess;
         // the controller block may exceed the default 48 KB of dynamic shared memory
         const int smem_max = (int)controller_smem(kMaxHidden);
         ok = ok && cudaFuncSetAttribute(k_select_bits, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_max) == cudaSuccess;
@@ -1105,11 +1105,13 @@ static int rows_impl(kvq_ctx* c, int layer, const void* Q, void* O, const void* 
     p.sinks = sinks;
     const int64_t seen = window > 0 ? std::min<int64_t>(c->len[layer], (int64_t)window + sinks) : c->len[layer];
     const uint64_t pairs = (uint64_t)c->batch * c->kv_heads;
-    const RowsPlan plan = rows_plan(c->sm_count, pairs, p.rows, (int)seen, c->splits_override);
-    if (pairs * plan.row_blocks * plan.parts > 0x7fffffffull) return KVQ_ERR_ARG;
-    p.row_blocks = plan.row_blocks;
-    p.parts = plan.parts;
-    rows_launch(p, plan, parents != nullptr, pairs, st);
+    const RowsPlan plan = rows_plan(c->device, c->sm_count, pairs, p.rows, parents ? nodes : 0, (int)seen, c->splits_override);
+    if (plan.ctas == 0) return KVQ_ERR_ARG;
+    p.pairs = (uint32_t)pairs;
+    p.ticks = plan.ticks;
+    p.span = plan.span;
+    p.by_pool = plan.by_pool;
+    rows_launch(p, plan, parents != nullptr, st);
     c->launches += 1;
     KVQ_CUDA(c, cudaGetLastError());
     return KVQ_OK;
@@ -1602,7 +1604,7 @@ int kvq_recover(kvq_ctx* c) {
     DeviceGuard guard(c->device);
     KVQ_CUDA(c, cudaDeviceSynchronize());
     KVQ_CUDA(c, cudaMemset(c->part_cnt, 0, sizeof(uint32_t) * (size_t)c->batch * c->q_heads * kMaxQueryRows));
-    KVQ_CUDA(c, cudaMemset(c->rows_cnt, 0, sizeof(uint32_t) * rows_max_records(c->sm_count)));
+    KVQ_CUDA(c, cudaMemset(c->rows_cnt, 0, sizeof(uint32_t) * rows_max_units(c->sm_count)));
     KVQ_CUDA(c, cudaMemset(c->flags, 0, sizeof(uint32_t)));
     float* base = nullptr;
     if (c->device >= 0 && c->device < KVQ_STATIC_MAX_DEVICES) {

@@ -1,6 +1,8 @@
 // Launches of the many-row attention and of the draft verification: planning and instantiation.
 #include "kvq_rows.h"
 
+#include <algorithm>
+
 #include "k_rows.cuh"
 #include "k_verify.cuh"
 
@@ -8,10 +10,21 @@ namespace kvq {
 
 namespace {
 
+constexpr int kMaxDraftTiles = kMaxTreeNodes / kTileTokens;
+
+// CTAs of a kernel that fit an SM, by blocks of eight rows (1, 2, 4) and 16-node tiles of the tree (0: no tree).
+struct Residency {
+    int ctas[5][kMaxDraftTiles + 1] = {};
+};
+Residency g_residency[64];             // per device; written with the same values by every set-up
+
 template <int NT, bool TREE>
-cudaError_t set_smem() {
-    const int draft_tiles = TREE ? kMaxTreeNodes / kTileTokens : 0;
-    return cudaFuncSetAttribute(k_attend_rows<NT, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)rows_smem_bytes<NT>(draft_tiles));
+cudaError_t set_up_kernel(Residency& r) {
+    const int most = TREE ? kMaxDraftTiles : 0;
+    cudaError_t e = cudaFuncSetAttribute(k_attend_rows<NT, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)rows_smem_bytes<NT>(most));
+    for (int tiles = TREE ? 1 : 0; e == cudaSuccess && tiles <= most; ++tiles)
+        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&r.ctas[NT][tiles], k_attend_rows<NT, TREE>, kRowsThreads, rows_smem_bytes<NT>(tiles));
+    return e;
 }
 
 template <int NT, bool TREE>
@@ -31,50 +44,83 @@ void launch(const RowsParams& p, uint64_t ctas, cudaStream_t st) {
 
 }  // namespace
 
-cudaError_t rows_setup() {
-    cudaError_t e = set_smem<1, true>();
-    if (e == cudaSuccess) e = set_smem<2, true>();
-    if (e == cudaSuccess) e = set_smem<1, false>();
-    if (e == cudaSuccess) e = set_smem<2, false>();
+cudaError_t rows_setup(int device) {
+    if (device < 0 || device >= 64) return cudaErrorInvalidDevice;
+    Residency& r = g_residency[device];
+    cudaError_t e = set_up_kernel<1, true>(r);
+    if (e == cudaSuccess) e = set_up_kernel<2, true>(r);
+    if (e == cudaSuccess) e = set_up_kernel<4, true>(r);
+    if (e == cudaSuccess) e = set_up_kernel<1, false>(r);
+    if (e == cudaSuccess) e = set_up_kernel<2, false>(r);
+    if (e == cudaSuccess) e = set_up_kernel<4, false>(r);
     return e;
 }
 
-// pairs = (sequence, KV head) pairs.
-RowsPlan rows_plan(int sm_count, uint64_t pairs, int rows, int visible_tokens, int splits) {
+RowsPlan rows_plan(int device, int sm_count, uint64_t pairs, int rows, int tree_nodes, int visible_tokens, int splits) {
     RowsPlan plan;
-    plan.nt = rows <= 8 ? 1 : 2;
+    plan.ctas = 0;
+    const double tiles = (double)visible_tokens / kTileTokens + 2.0;
+    // 32 rows share the unpacking of a tile, but their kernel runs with half the warps and a longer set-up: worth it from
+    // about 128 tiles on (192 rows over 190 tiles: 67 us against 78 us with 16 rows per unit; 63 rows over 66 tiles: 26 against 23).
+    plan.nt = rows <= 8 ? 1 : rows <= 16 || tiles < 128.0 ? 2 : 4;
     plan.row_blocks = (uint32_t)((rows + 8 * plan.nt - 1) / (8 * plan.nt));
+    // Shares that are the same fraction of every pool keep the warps of an SM in the same loop, which the longest code profits
+    // from (8192 tokens, 32 rows: 224 us against 243 us); the others are faster with fewer changes of pool (2048 tokens of
+    // one sequence, 15 rows: 13 us against 17 us).
+    plan.by_pool = plan.nt == 4;
     const uint64_t units = pairs * plan.row_blocks;
+    if (units > 0x7fffffffull) return plan;
+    const int draft_tiles = (tree_nodes + kTileTokens - 1) / kTileTokens;
+    const int per_sm = device >= 0 && device < 64 ? std::max(1, g_residency[device].ctas[plan.nt][draft_tiles]) : 1;
+    const uint64_t resident = (uint64_t)sm_count * per_sm;
+    const uint64_t max_ctas = std::min<uint64_t>(4 * (uint64_t)sm_count, rows_max_record_rows(sm_count) / (16 * plan.nt));   // of a launch that cuts units
+    auto cut = [&](uint64_t parts) {                   // every unit into `parts` CTAs
+        if (parts == 1) plan.ctas = (uint32_t)units, plan.ticks = plan.span = 1;
+        else plan.ctas = plan.ticks = (uint32_t)(units * parts), plan.span = (uint32_t)units;
+    };
     if (splits > 0) {
-        plan.parts = (uint32_t)((splits + kRowsWarps - 1) / kRowsWarps);
-        while (plan.parts > 1 && units * plan.parts > rows_max_records(sm_count)) --plan.parts;
+        uint64_t parts = (uint64_t)((splits + kRowsWarps - 1) / kRowsWarps);
+        while (parts > 1 && units * parts > max_ctas) --parts;
+        cut(parts);
         return plan;
     }
-    const double tiles = (double)visible_tokens / kTileTokens + 2.0;
-    const uint64_t resident = (uint64_t)sm_count * rows_ctas_per_sm(plan.nt);
-    // Time of a launch in tiles of one warp: waves of CTAs, each a set-up of about twelve tiles and its warps' shares;
-    // parts merged through global records cost about another twelve.
+    // A model of the launch in us, fitted to measured sweeps over context lengths and splits: a CTA's set-up and merge, its
+    // warps' tiles -- a tile costs a warp more the more CTAs share the SM -- in as many waves as it takes.  Parts of a unit
+    // that go through global records cost a merge; CTAs with stretches that do not end at unit borders work on two units
+    // one after the other, with a second set-up.
+    const double set_up = 7.0, merge = 1.5, merge_part = 0.15;
+    const double second = plan.nt == 1 ? 8.0 : plan.nt == 2 ? 17.0 : 30.0;
+    const double tile_full = plan.nt == 1 ? 0.52 : plan.nt == 2 ? 0.65 : 0.75, tile_alone = plan.nt == 1 ? 0.4 : plan.nt == 2 ? 0.5 : 0.6;
     double best = 0.0;
-    for (uint32_t parts = 1; parts <= 64 && (parts == 1 || units * parts <= rows_max_records(sm_count)); ++parts) {
-        const double waves = (double)((units * parts + resident - 1) / resident);
-        const double share = tiles / (double)(parts * kRowsWarps);
-        const double cost = waves * (12.0 + share) + (parts > 1 ? 12.0 : 0.0);
-        if (parts == 1 || cost < best) {
+    uint64_t parts = 1;
+    for (uint64_t p = 1; p == 1 || (units * p <= max_ctas && p <= 64); ++p) {
+        const uint64_t ctas = units * p;
+        const double waves = (double)((ctas + resident - 1) / resident);
+        const double load = std::min(1.0, (double)((ctas + sm_count - 1) / sm_count) / (double)per_sm);
+        const double tile = std::max(tile_alone, tile_full * load);
+        const double cost = waves * (set_up + tiles / (double)(p * kRowsWarps) * tile) + (p > 1 ? merge + merge_part * (double)p : 0.0);
+        if (p == 1 || cost < best) {
             best = cost;
-            plan.parts = parts;
+            parts = p;
         }
+    }
+    cut(parts);
+    if (2 * units > resident && units < 4 * resident && resident <= max_ctas && units < rows_max_units(sm_count)) {
+        const double cost = set_up + second + merge + (double)units * tiles / (double)(resident * kRowsWarps) * tile_full;
+        if (cost < best) plan.ctas = plan.ticks = (uint32_t)resident, plan.span = (uint32_t)units;
     }
     return plan;
 }
 
-void rows_launch(const RowsParams& p, const RowsPlan& plan, bool tree, uint64_t pairs, cudaStream_t st) {
-    const uint64_t ctas = pairs * plan.row_blocks * plan.parts;
+void rows_launch(const RowsParams& p, const RowsPlan& plan, bool tree, cudaStream_t st) {
     if (tree) {
-        if (plan.nt == 1) launch<1, true>(p, ctas, st);
-        else launch<2, true>(p, ctas, st);
+        if (plan.nt == 1) launch<1, true>(p, plan.ctas, st);
+        else if (plan.nt == 2) launch<2, true>(p, plan.ctas, st);
+        else launch<4, true>(p, plan.ctas, st);
     } else {
-        if (plan.nt == 1) launch<1, false>(p, ctas, st);
-        else launch<2, false>(p, ctas, st);
+        if (plan.nt == 1) launch<1, false>(p, plan.ctas, st);
+        else if (plan.nt == 2) launch<2, false>(p, plan.ctas, st);
+        else launch<4, false>(p, plan.ctas, st);
     }
 }
 

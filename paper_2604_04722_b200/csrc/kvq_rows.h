@@ -18,11 +18,13 @@ struct RowsParams {
     const __half* V;
     const uint8_t* bits;           // [batch][nodes] or nullptr: fp16 rows (tree only)
     const int32_t* parents;        // [batch][nodes] (tree only)
-    float* part_o;                 // [units * parts][8 NT][64] unnormalised
-    float2* part_ml;               // [units * parts][8 NT]     (m in log2 units, l)
-    uint32_t* part_cnt;            // [units] parts delivered so far; zero between launches
+    float* part_o;                 // [2 * CTAs][8 NT][64] unnormalised
+    float2* part_ml;               // [2 * CTAs][8 NT]     (m in log2 units, l)
+    uint32_t* part_cnt;            // [units] pieces delivered so far; zero between launches
     int layer, group, nodes, rows; // rows = nodes * group
-    uint32_t row_blocks, parts;
+    uint32_t pairs;                // (sequence, KV head) pairs; unit = row block * pairs + pair
+    uint32_t ticks, span;          // ticks per unit and per CTA of the axis on which the units lie end to end
+    bool by_pool;                  // a share is the same fraction of every pool (otherwise a stretch of the pools laid end to end)
     int window, sinks;             // window == 0: everything is visible
 };
 
@@ -39,21 +41,25 @@ struct VerifyParams {
     int nodes, vocab;
 };
 
-// How a launch is cut: blocks of eight rows per unit (1 or 2), units per (sequence, KV head), parts per unit.
+// How a launch is cut: blocks of eight rows per unit (1, 2 or 4), units per (sequence, KV head), CTAs, and the axis of RowsParams.
 struct RowsPlan {
     int nt = 1;
-    uint32_t row_blocks = 1, parts = 1;
+    uint32_t row_blocks = 1, ctas = 1, ticks = 1, span = 1;
+    bool by_pool = false;
 };
-constexpr int kRowsMaxRows = 16;                       // rows of a partial record
+constexpr int kRowsMaxRows = 32;                       // rows of a unit at most
 
-// Partial records (of kRowsMaxRows rows) and arrival counters a handle keeps.
-inline size_t rows_max_records(int sm_count) { return 8 * (size_t)sm_count; }
+// What a handle keeps for launches that cut units: rows of partial records, two records for each CTA (at most four CTAs of
+// 8 rows per SM, three of 16, two of 32), and arrival counters, for at most four times as many units as there are CTAs.
+inline size_t rows_max_record_rows(int sm_count) { return 128 * (size_t)sm_count; }
+inline size_t rows_max_units(int sm_count) { return 16 * (size_t)sm_count; }
 
-// Once per device and process image: shared-memory limits of the kernels.
-cudaError_t rows_setup();
-// splits > 0: as many warps per unit as that (rounded up to whole CTAs, and down to what the records hold).
-RowsPlan rows_plan(int sm_count, uint64_t pairs, int rows, int visible_tokens, int splits);
-void rows_launch(const RowsParams& p, const RowsPlan& plan, bool tree, uint64_t pairs, cudaStream_t st);
+// For every handle: shared-memory limits of the kernels on this device, and how many of their CTAs fit an SM.
+cudaError_t rows_setup(int device);
+// pairs: (sequence, KV head) pairs; tree_nodes: 0 without a tree; splits > 0: as many warps per unit as that (rounded up to
+// whole CTAs, and down to what the records hold).  ctas == 0: too many units for a launch.
+RowsPlan rows_plan(int device, int sm_count, uint64_t pairs, int rows, int tree_nodes, int visible_tokens, int splits);
+void rows_launch(const RowsParams& p, const RowsPlan& plan, bool tree, cudaStream_t st);
 cudaError_t verify_launch(const VerifyParams& p, int batch, int sm_count, cudaStream_t st);
 
 }  // namespace kvq
