@@ -26,7 +26,7 @@
 // way, but as prefixes of their byte (c0, c0 + 4 c1, ...: the last needs no AND at all), which the accumulators undo
 // when the pool is left.  The weight w = p * s_v is rounded once to fp16 (by at most 2^-11 of its value: the rounding
 // that the fp16 operand forces).  What that does is made to act on centred codes:
-//   sum p (s c + z) = sum w (c - mid) + sum p (z + mid s),   mid = 2^(bits-1),
+//   sum p (s c + z) = sum w (c - mid) + sum p (z + mid s),   mid = (2^bits - 1) / 2,
 // with the same rounded w in both terms of (c - mid).  With channels far larger than the others in a row (keys and
 // values have such) c is near the middle of its range for all the ordinary channels, and the rounding of w would
 // otherwise act on the middle instead of on the value.  The sums of p, of p (z + mid s) and of mid w stay in fp32.
@@ -146,6 +146,11 @@ __device__ __forceinline__ uint32_t max_half2(uint32_t a, uint32_t b) {
     const __half2 m = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
     return *reinterpret_cast<const uint32_t*>(&m);
 }
+__device__ __forceinline__ float fast_rcp(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 __device__ __forceinline__ float two_to(int e) { return __int_as_float((127 + e) << 23); }
 
 // The slot of the first token of class c at a position >= p of a sequence of len tokens (n_c if there is none), for the
@@ -213,7 +218,7 @@ struct TileLogits {
     float D[NT][4];
     float sk[2], zk[2];            // scale (times the common factor of the K product) and zero-point of K
     float sv[2], zv[2];            // scale and centred zero-point of V
-    float mid;                     // the code that V is centred on
+    float mid[2];                  // the code that V is centred on
 };
 
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
@@ -254,7 +259,7 @@ __device__ __forceinline__ void add_tile(RowsState<NT>& st, const TileLogits<NT>
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             st.l[n] = add2v(st.l[n], p[n][s]);
-            st.b[n] = fma2v(unpack_half2(w[n][s]), both(-t.mid), fma2v(p[n][s], both(t.zv[s]), st.b[n]));
+            st.b[n] = fma2v(unpack_half2(w[n][s]), both(-t.mid[s]), fma2v(p[n][s], both(t.zv[s]), st.b[n]));
             w[n][s] = transpose8(w[n][s]);             // (slot g: rows 2q, 2q + 1) -> (row g: slots 2q, 2q + 1)
         }
 }
@@ -311,7 +316,6 @@ struct RowsQuant {
     static constexpr int BITS = pool_bits(CLS);
     static constexpr int NW = 2 << CLS;                // words per lane of one tensor: 2, 4, 8
     static constexpr uint32_t MASK = CLS == 0 ? 0x00030003u : CLS == 1 ? 0x000f000fu : 0x00ff00ffu;
-    static constexpr float MID = (float)(1 << (BITS - 1));
 
     // Register r of step s of the K product holds, in 16-bit lane x, the code of channel
     //   2-bit: 16 q + 2 s + r + 8 x;   4-bit: 8 (q + 4 (s >> 1)) + 2 (s & 1) + r + 4 x;   8-bit: 4 (q + 4 s) + r + 2 x
@@ -355,9 +359,9 @@ struct RowsQuant {
             // A constant row has scale zero and codes zero.  It is read with a scale of 2^-24, the smallest there is, which
             // its codes multiply by zero all the same: s (c - mid) + (z + mid s) = z.
             t.sv[s] = fmaxf(vm.x, 5.9604645e-8f);
-            t.zv[s] = fmaf(t.sv[s], MID, vm.y);
+            t.mid[s] = fminf(fmaxf(-vm.y * fast_rcp(t.sv[s]), 0.f), (float)((1 << BITS) - 1));
+            t.zv[s] = fmaf(t.sv[s], t.mid[s], vm.y);
         }
-        t.mid = MID;
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             const uint32_t a[4] = {k_operand(kw, 0, s, 0), k_operand(kw, 1, s, 0), k_operand(kw, 0, s, 1), k_operand(kw, 1, s, 1)};
@@ -413,7 +417,7 @@ struct RowsFp16 {
         }
         t.sk[0] = t.sk[1] = kfactor;
         t.sv[0] = t.sv[1] = 1.f;
-        t.zk[0] = t.zk[1] = t.zv[0] = t.zv[1] = t.mid = 0.f;
+        t.zk[0] = t.zk[1] = t.zv[0] = t.zv[1] = t.mid[0] = t.mid[1] = 0.f;
     }
     // valid: bit k says that slot 2 q + (k & 1) + 8 (k >> 1) holds a row (the bytes of other slots may be anything, an Inf
     // or NaN pattern included, which a weight of zero would not silence).

@@ -132,12 +132,14 @@ cudaError_t verify_launch(const VerifyParams& p, int batch, int sm_count, cudaSt
     cfg.gridDim = dim3((unsigned)batch * ctas);
     cfg.blockDim = dim3(kVerifyThreads);
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = ctas;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, k_verify_tree, p);
 }
 
