@@ -288,8 +288,11 @@ int kvq_attend_last(kvq_ctx* ctx, int layer, const void* Q, void* O, int n_queri
  *   window, sinks  window == 0: a node sees every cached token, its ancestors and itself.  window > 0: of those, the
  *          ones whose position is less than `window` before its own, and the tokens at positions < sinks.
  * The cache is not changed: append the accepted rows afterwards (kvq_append_ragged).  n_nodes == 0 is a no-op.  One
- * launch.  Q, K, V, O 16-byte aligned; O may not overlap the inputs.  Caches with one scale group per row only
- * (kvq_create, kvq_create_arena and their workspace forms); KVQ_ERR_ARG for the other layouts.
+ * launch; one that was captured into a graph is captured again after an append to the layer.  Q, K, V, O 16-byte
+ * aligned; O may not overlap the inputs.  The rows of a node that is not in use may hold anything, and so may cached
+ * tokens that no row sees.  A value that is not finite makes NaN of the rows that see it; if it is a cached one, also
+ * of rows of the same sequence whose window has moved past it while another row still sees it.  Caches with one scale
+ * group per row only (kvq_create, kvq_create_arena and their workspace forms); KVQ_ERR_ARG for the other layouts.
  */
 #define KVQ_MAX_TREE_NODES 64
 int kvq_attend_tree(kvq_ctx* ctx, int layer, const void* Q, const void* K, const void* V, const uint8_t* bits_opt,
@@ -322,7 +325,7 @@ int kvq_decode_attn_window(kvq_ctx* ctx, int layer, const void* Q, void* O, int 
  *   n_accepted dev int32 [batch]; path dev int32 [batch][n_nodes]: the accepted nodes from the root down, then -1;
  *   next_token dev int32 [batch]
  * 0 <= n_nodes <= KVQ_MAX_TREE_NODES (0: only the next token is drawn; tokens, parents, u_accept and path may be NULL).
- * batch == 0 is a no-op.  One launch.
+ * 1 <= vocab <= 2^30.  batch == 0 is a no-op.  One launch.
  */
 int kvq_verify_tree(const float* target, const float* draft_opt, const int32_t* tokens, const int32_t* parents, int batch,
                     int n_nodes, int vocab, const float* u_accept, const float* u_next, int32_t* n_accepted,

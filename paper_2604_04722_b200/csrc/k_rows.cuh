@@ -6,7 +6,7 @@
 //
 // The decode kernel (k_decode.cuh) gives every (sequence, query head) its own walk over the cache, which is right for
 // one row.  Here the rows of a tree and the heads of a group share a walk: a unit is (sequence, KV head, block of up
-// to 8 or 16 rows), row = node * group + head, and both products run on the fp16 matrix instructions with the rows as
+// to 8, 16 or 32 rows), row = node * group + head, and both products run on the fp16 matrix instructions with the rows as
 // the 8 columns (mma.sync m16n8k16, fp32 accumulation):
 //   S[slot][row] = sum_i c_i q_i            16 rows = the slots of a tile
 //   O[channel][row] += sum_slot c w         16 rows = channels, four products for the 64 of a head
@@ -22,14 +22,14 @@
 // power 2^-k is undone on the query's side.  Both factors are exact (the query is only scaled by powers of two), so a
 // logit
 //   y = log2(e)/8 * (s_k * sum_i q_i c_i + z_k * sum_i q_i)
-// carries fp32 accumulation error only.  V codes are cut out the same
-// way, but as prefixes of their byte (c0, c0 + 4 c1, ...: the last needs no AND at all), which the accumulators undo
-// when the pool is left.  The weight w = p * s_v is rounded once to fp16 (by at most 2^-11 of its value: the rounding
+// carries fp32 accumulation error only.  V codes are cut out the same way, but as prefixes of their byte (c0, c0 + 4 c1,
+// ...: the last needs no AND at all), which the accumulators undo when the pool is left.  The weight w = p * s_v is rounded once to fp16 (by at most 2^-11 of its value: the rounding
 // that the fp16 operand forces).  What that does is made to act on centred codes:
-//   sum p (s c + z) = sum w (c - mid) + sum p (z + mid s),   mid = (2^bits - 1) / 2,
-// with the same rounded w in both terms of (c - mid).  With channels far larger than the others in a row (keys and
-// values have such) c is near the middle of its range for all the ordinary channels, and the rounding of w would
-// otherwise act on the middle instead of on the value.  The sums of p, of p (z + mid s) and of mid w stay in fp32.
+//   sum p (s c + z) = sum w (c - mid) + sum p (z + mid s),   mid = -z / s, inside [0, 2^bits - 1], per token
+// with the same rounded w in both terms of (c - mid).  mid is the code of the value zero, so the rounding of w acts on
+// the value and not on its distance from the row's minimum, which is far larger for the ordinary channels of a row with
+// one large one (values have such): outputs over 500 to 8000 mixed tokens are off by 2.8e-4 to 3.1e-4 (relative, whole
+// tensors), of which the rounding to fp16 alone makes 2.1e-4.  The sums of p, of p (z + mid s) and of mid w stay in fp32.
 //
 // Softmax reference.  p = 2^(y - m), m kept per row and warp.  m is no running maximum: it is moved only when some w
 // overflows fp16 (one vote per tile decides), and then to where the row's largest w of the tile is 2^4.  So logits may
@@ -187,6 +187,7 @@ struct RowsScratch {
     unsigned long long vis[kMaxTreeNodes];             // those of them that it sees (0: the node is not used)
     unsigned long long step_bits[kNumPools];           // class c among the 64 positions after the first window start
     unsigned long long used;                           // nodes that are used
+    unsigned long long poison;                         // drafted values that are not finite
     alignas(16) RowsChunks plan[kRowsWarps];
     uint2 chunk[kRowsWarps][kRowsStages];              // what a stage holds: z, and w >> 16, of its chunk
     int in_sinks[kNumPools], from[kNumPools], full[kNumPools];     // tiles that every row sees whole: [0, in_sinks), [from, full)
@@ -419,9 +420,9 @@ struct RowsFp16 {
         t.sv[0] = t.sv[1] = 1.f;
         t.zk[0] = t.zk[1] = t.zv[0] = t.zv[1] = t.mid[0] = t.mid[1] = 0.f;
     }
-    // valid: bit k says that slot 2 q + (k & 1) + 8 (k >> 1) holds a row (the bytes of other slots may be anything, an Inf
-    // or NaN pattern included, which a weight of zero would not silence).
-    __device__ static __forceinline__ void v_operands(const uint8_t* rec, int lane, uint32_t (&a)[4][4], uint32_t valid) {
+    // slots: those of the tile that are read (the bytes of the others may be anything, an Inf or NaN pattern included, which
+    // a weight of zero would not silence).
+    __device__ static __forceinline__ void v_operands(const uint8_t* rec, int lane, uint32_t (&a)[4][4], uint32_t slots) {
         const int g = lane >> 2, q = lane & 3;
         const uint8_t* v = rec + pool_codes_bytes(3) + (g >> 1) * kTileTokens * 16 + (g & 1) * 8;
         uint2 x[2][4];
@@ -430,7 +431,7 @@ struct RowsFp16 {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int slot = 2 * q + (k & 1) + 8 * (k >> 1);
-                x[i][k] = (valid >> k) & 1u ? *reinterpret_cast<const uint2*>(v + (i * 4 * kTileTokens + slot) * 16) : make_uint2(0u, 0u);
+                x[i][k] = (slots >> slot) & 1u ? *reinterpret_cast<const uint2*>(v + (i * 4 * kTileTokens + slot) * 16) : make_uint2(0u, 0u);
             }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -463,7 +464,7 @@ __device__ __forceinline__ uint32_t whole_tiles(const uint8_t* rec, uint32_t n, 
         TileLogits<NT> t;
         C::template k_side<NT>(rec, lane, qf, kfactor, t);
         uint32_t a[4][4];
-        C::v_operands(rec, lane, a, 15u);              // (in front of the vote: it fills the waits of the chain above)
+        C::v_operands(rec, lane, a, 0xffffu);              // (in front of the vote: it fills the waits of the chain above)
         float2 p[NT][2];
         uint32_t w[NT][2];
         logits_of(st, t, true, p);
@@ -506,6 +507,11 @@ __device__ __forceinline__ void leave_class(RowsState<NT>& st, int c) {
 
 // ---------------------------------------------------------------- the kernel
 
+__device__ __forceinline__ bool finite_half8(uint4 v) {
+    // (an exponent of all ones carries into the sign bit)
+    const auto carry = [](uint32_t w) { return (w & 0x7fff7fffu) + 0x04000400u; };
+    return !((carry(v.x) | carry(v.y) | carry(v.z) | carry(v.w)) & 0x80008000u);
+}
 // One drafted row, eight channels per lane of an eight-lane group, as the store would give it back (the row quantizer of
 // Eq. 24, then code * scale + zero-point), rounded to fp16.
 __device__ __forceinline__ uint4 draft_row_as_stored(uint4 raw, int c) {
@@ -698,8 +704,10 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
     for (int k = 0; k < RB; ++k) {
         const float2 f0 = unpack_half2(qv[k].x), f1 = unpack_half2(qv[k].y), f2 = unpack_half2(qv[k].z), f3 = unpack_half2(qv[k].w);
         float sum = ((f0.x + f0.y) + (f1.x + f1.y)) + ((f2.x + f2.y) + (f3.x + f3.y));
-        qmax = fmaxf(qmax, fmaxf(fmaxf(fmaxf(fabsf(f0.x), fabsf(f0.y)), fmaxf(fabsf(f1.x), fabsf(f1.y))),
-                                 fmaxf(fmaxf(fabsf(f2.x), fabsf(f2.y)), fmaxf(fabsf(f3.x), fabsf(f3.y)))));
+        // (an unused node's row may hold anything: what is not finite must not set the scale of the others)
+        const float top = fmaxf(fmaxf(fmaxf(fabsf(f0.x), fabsf(f0.y)), fmaxf(fabsf(f1.x), fabsf(f1.y))),
+                                fmaxf(fmaxf(fabsf(f2.x), fabsf(f2.y)), fmaxf(fabsf(f3.x), fabsf(f3.y))));
+        qmax = fmaxf(qmax, top <= 65504.f ? top : 0.f);
 #pragma unroll
         for (int d = 1; d < 8; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         if (row_of(k) < ROWS) {
@@ -712,6 +720,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
     }
     qmax = warp_max(qmax);
     if (lane == 0) sc.wmax[warp] = qmax;
+    if (has_draft && tid == 0) sc.poison = 0ull;
     __syncthreads();
 
     // ---- the copies: chunks of the share in order; a chunk stays inside one 64 KB block and fits a stage
@@ -842,7 +851,14 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
                     }
                 }
             }
-            const uint4 row = draft_row_as_stored(raw, c);
+            uint4 row = draft_row_as_stored(raw, c);
+            // A value row that is not finite is left out of the products, where a weight of zero would not silence it for the
+            // nodes that do not see it; those that see it become NaN at the end.
+            const uint32_t lanes = 0xffu << (lane & 24);
+            if (value && (__ballot_sync(0xffffffffu, !finite_half8(row)) & lanes)) {
+                row = make_uint4(0u, 0u, 0u, 0u);
+                if (piece8 == 0 && node < P.nodes) atomicOr(&sc.poison, 1ull << node);
+            }
             *reinterpret_cast<uint4*>(draft + (node / kTileTokens) * kDraftTileBytes + (value ? kDraftTileBytes / 2 : 0) +
                                       (piece8 * kTileTokens + node % kTileTokens) * 16) = row;
         }
@@ -913,12 +929,18 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
     // One tile of class c in general.  There is one copy of this code for all classes, and a short loop per class for the
     // tiles in the middle (whole_tiles): the loops have to stay inside the instruction caches.
     bool fresh = true;                                 // no reference has been set yet
-    auto any_tile = [&](int c, const uint8_t* rec, bool edge, const uint32_t (&seen)[NT], uint32_t valid) {
+    auto any_tile = [&](int c, const uint8_t* rec, bool edge, const uint32_t (&seen)[NT], uint32_t slots) {
         TileLogits<NT> t;
         if (c == 0) RowsQuant<0>::k_side<NT>(rec, lane, qf, kfactor, t);
         else if (c == 1) RowsQuant<1>::k_side<NT>(rec, lane, qf, kfactor, t);
         else if (c == 2) RowsQuant<2>::k_side<NT>(rec, lane, qf, kfactor, t);
         else RowsFp16::k_side<NT>(rec, lane, qf, kfactor, t);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+            if (!((slots >> (g + 8 * s)) & 1u)) {      // what a slot carries that is not read may be Inf or NaN
+                t.sv[s] = 1.f;
+                t.zv[s] = t.mid[s] = 0.f;
+            }
         float2 p[NT][2];
         uint32_t w[NT][2];
 #pragma unroll 1
@@ -931,10 +953,10 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
         fresh = false;
         add_tile(st, t, p, w);
         uint32_t a[4][4];
-        if (c == 0) RowsQuant<0>::v_operands(rec, lane, a, valid);
-        else if (c == 1) RowsQuant<1>::v_operands(rec, lane, a, valid);
-        else if (c == 2) RowsQuant<2>::v_operands(rec, lane, a, valid);
-        else RowsFp16::v_operands(rec, lane, a, valid);
+        if (c == 0) RowsQuant<0>::v_operands(rec, lane, a, slots);
+        else if (c == 1) RowsQuant<1>::v_operands(rec, lane, a, slots);
+        else if (c == 2) RowsQuant<2>::v_operands(rec, lane, a, slots);
+        else RowsFp16::v_operands(rec, lane, a, slots);
         v_products(st, a, w);
     };
     int cls = 3;
@@ -972,16 +994,13 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
                 s0 += done * kTileTokens;
                 edges >>= done;
             }
-            uint32_t seen[NT] = {}, valid = 15u;
+            uint32_t seen[NT] = {}, slots = 0xffffu;
             const bool edge = edges & 1u;
             if (edge) {                                // the pool's last tile, one where a window starts or the sinks end, a drafted one
                 const uint32_t use = drafted ? (uint32_t)(sc.used >> (16 * warp)) : 0u, cnt = sc.cnt[c], sink = sc.sink[c];
-                valid = 0;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t at = 2 * q + (k & 1) + 8 * (k >> 1);
-                    valid |= (drafted ? (use >> at) & 1u : s0 + at < cnt) ? 1u << k : 0u;
-                }
+                // those that some row sees: up to the end of the pool, from the shallowest row's window on or in the sinks
+                const auto below = [&](uint32_t end) { return end <= s0 ? 0u : (1u << min(end - s0, 16u)) - 1u; };
+                slots = drafted ? use & 0xffffu : below(cnt) & (~below(sc.start[c]) | below(sink));
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -997,7 +1016,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
                         }
                     }
             }
-            any_tile(c, rec, edge, seen, valid);
+            any_tile(c, rec, edge, seen, slots);
             if (--left == 0) break;
             rec += step;
             s0 += kTileTokens;
@@ -1021,6 +1040,15 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
             parity ^= 1u << cslot;
             cslot = cslot + 1 == kRowsStages ? 0 : cslot + 1;
             --in_flight;
+        }
+    }
+
+    if (has_draft && sc.poison != 0ull) {              // rows that see a drafted value that is not finite
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int n0 = sc.node[8 * n + 2 * q], n1 = sc.node[8 * n + 2 * q + 1];
+            if (n0 >= 0 && (sc.vis[n0] & sc.poison)) st.l[n].x = NAN;
+            if (n1 >= 0 && (sc.vis[n1] & sc.poison)) st.l[n].y = NAN;
         }
     }
 
@@ -1064,7 +1092,8 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
         if (!row_used(k)) return;
         int node;
         const size_t at = place_of(k, node);
-        const float inv = L > 0.f && (!TREE || sc.vis[node]) ? 1.0f / L : 0.f;     // nothing seen, or an unused node: zeros
+        // nothing seen, or an unused node: zeros (a NaN stays one)
+        const float inv = L != 0.f && (!TREE || sc.vis[node]) ? 1.0f / L : 0.f;
         uint32_t v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = inv != 0.f ? pack_half2(make_float2(o[2 * e] * inv, o[2 * e + 1] * inv)) : 0u;

@@ -1138,7 +1138,7 @@ int kvq_decode_attn_window(kvq_ctx* c, int layer, const void* Q, void* O, int wi
 int kvq_verify_tree(const float* target, const float* draft_opt, const int32_t* tokens, const int32_t* parents, int batch,
                     int n_nodes, int vocab, const float* u_accept, const float* u_next, int32_t* n_accepted, int32_t* path,
                     int32_t* next_token, void* stream) {
-    if (batch < 0 || n_nodes < 0 || n_nodes > KVQ_MAX_TREE_NODES || vocab < 1) return KVQ_ERR_ARG;
+    if (batch < 0 || n_nodes < 0 || n_nodes > KVQ_MAX_TREE_NODES || vocab < 1 || vocab > (1 << 30)) return KVQ_ERR_ARG;
     if (batch == 0) return KVQ_OK;
     if (!target || !u_next || !n_accepted || !next_token || batch > (1 << 24)) return KVQ_ERR_ARG;
     if (n_nodes > 0 && (!tokens || !parents || !u_accept || !path)) return KVQ_ERR_ARG;

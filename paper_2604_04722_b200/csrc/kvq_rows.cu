@@ -45,8 +45,8 @@ void launch(const RowsParams& p, uint64_t ctas, cudaStream_t st) {
 }  // namespace
 
 cudaError_t rows_setup(int device) {
-    if (device < 0 || device >= 64) return cudaErrorInvalidDevice;
-    Residency& r = g_residency[device];
+    Residency other;
+    Residency& r = device >= 0 && device < 64 ? g_residency[device] : other;
     cudaError_t e = set_up_kernel<1, true>(r);
     if (e == cudaSuccess) e = set_up_kernel<2, true>(r);
     if (e == cudaSuccess) e = set_up_kernel<4, true>(r);

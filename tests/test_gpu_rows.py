@@ -258,6 +258,65 @@ def test_garbage_in_unused_nodes_stays_out(gu, oracle):
         assert np.array_equal(got, want)
 
 
+@pytest.mark.parametrize("junk", [np.nan, np.inf, -65504.0])
+def test_queries_of_unused_nodes_stay_out(gu, oracle, junk):
+    """Their rows share blocks with rows in use."""
+    with Case(gu, oracle, 24, 2, 6, 2, [60, 60]) as c:
+        Q, t = c.queries(13), c.tree(13, "ragged")
+        for b in range(2):
+            for i, ch in enumerate(rr.chains(t[3][b])):
+                if ch is None:
+                    Q[b, i] = np.float16(junk)
+        clean = Q.copy()
+        for b in range(2):
+            for i, ch in enumerate(rr.chains(t[3][b])):
+                if ch is None:
+                    clean[b, i] = 0
+        c.check(c.run_tree(Q, t), clean, tree=t)
+
+
+@pytest.mark.parametrize("splits", [1, 5, 16, 64])
+def test_explicit_splits(gu, oracle, splits):
+    from paper_2604_04722_b200 import binding as kq
+    with Case(gu, oracle, 25, 2, 6, 2, [700, 650]) as c:
+        kq.kvq_set_splits(c.g.ctx, splits)
+        for T in (1, 6, 30):
+            Q, t = c.queries(T), c.tree(T)
+            c.check(c.run_tree(Q, t), Q, tree=t)
+        Q1 = c.queries(1)
+        c.check(c.run_window(Q1, 400, 4), Q1, 400, 4)
+
+
+@pytest.mark.parametrize("B,Hq,H,n,T", [(40, 32, 32, 300, 1), (13, 30, 10, 900, 9), (3, 32, 32, 2300, 12), (20, 32, 32, 60, 3)])
+def test_many_units(gu, oracle, B, Hq, H, n, T):
+    """More units than CTAs fit the device: whole units, and stretches of the axis that cross unit borders.  Three sequences
+    of the batch are compared."""
+    rng = np.random.default_rng(n)
+    import torch
+    from paper_2604_04722_b200 import binding as kq
+    with Case(gu, oracle, n, B, Hq, H, [n] * B) as c:
+        Q, t = c.queries(T), c.tree(T)
+        got, Q1 = c.run_tree(Q, t, n - 30, 2), c.queries(1)
+        got1 = c.run_window(Q1, n - 7, 3)
+        for b in (0, B // 2, B - 1):
+            part = oracle.OracleCache(1, Hq, H)
+            part.append(c.K[b:b + 1], c.V[b:b + 1], c.bits[b:b + 1])
+            sub = tuple(x[b:b + 1] for x in t)
+            for out, q, kw in ((got, Q, dict(window=n - 30, sinks=2, tree=sub)), (got1, Q1, dict(window=n - 7, sinks=3))):
+                want, bound = rr.attention(oracle, part, [n], q[b:b + 1], Hq // H, **kw)
+                assert np.all(np.abs(out[b:b + 1].astype(np.float64).reshape(want.shape) - want) <= bound)
+
+
+def test_long_ragged_batch_over_the_whole_axis(gu, oracle):
+    """Lengths from nothing to long, so that some stretches of the axis are empty."""
+    with Case(gu, oracle, 26, 6, 6, 2, [2500, 0, 1, 2100, 16, 900]) as c:
+        for T in (2, 8, 40):
+            Q, t = c.queries(T), c.tree(T, "ragged")
+            c.check(c.run_tree(Q, t), Q, tree=t)
+        Q1 = c.queries(1)
+        c.check(c.run_window(Q1, 2000, 4), Q1, 2000, 4)
+
+
 def test_stale_blocks_of_an_earlier_cache_stay_out(gu, oracle):
     """Blocks that held huge fp16 rows are handed out again after a reset."""
     import torch
@@ -274,6 +333,63 @@ def test_stale_blocks_of_an_earlier_cache_stay_out(gu, oracle):
         c.check(c.run_tree(Q, t), Q, tree=t)
         Q1 = c.queries(1)
         c.check(c.run_window(Q1, 9, 1), Q1, 9, 1)
+
+
+@pytest.mark.parametrize("b", [2, 4, 8, 16])
+@pytest.mark.parametrize("pattern", [0x7c00, 0xffff])
+def test_slots_without_a_token_may_hold_any_bytes(gu, oracle, b, pattern):
+    """Blocks that held rows of Inf or NaN patterns, whatever the pool that gets them next."""
+    from paper_2604_04722_b200 import binding as kq
+    with Case(gu, oracle, b, 1, 2, 1, [21], bits=lambda m: np.full(m, b)) as c:
+        kq.kvq_reset(c.g.ctx)
+        junk = np.full((1, 100, 1, 64), pattern, np.uint16).view(np.float16)
+        c.g.append(0, junk, junk, np.full((1, 100), 16, np.uint8))
+        kq.kvq_reset(c.g.ctx)
+        c.g.append(0, c.K, c.V, c.bits)
+        Q, t = c.queries(3), c.tree(3)
+        c.check(c.run_tree(Q, t), Q, tree=t)
+        Q1 = c.queries(1)
+        c.check(c.run_window(Q1, 9, 1), Q1, 9, 1)
+
+
+@pytest.mark.parametrize("b", [2, 4, 8, 16])
+@pytest.mark.parametrize("bad", [np.inf, np.nan])
+def test_cached_tokens_that_nobody_sees_may_hold_anything(gu, oracle, b, bad):
+    with Case(gu, oracle, b, 1, 4, 2, [150], bits=lambda m: np.full(m, b)) as c:
+        Q1, Q, t = c.queries(1), c.queries(7), c.tree(7, "star")
+        at = slice(5, 150 - 41)                        # neither among 5 sinks nor in a window of 40
+        dirty = Case(gu, oracle, b, 1, 4, 2, [0], bits=lambda m: np.full(m, b))
+        dirty.g.close()
+        dirty.g = gu.GpuCache(1, 1, 4, 2, 300)
+        K, V = c.K.copy(), c.V.copy()
+        K[:, at], V[:, at] = bad, bad
+        dirty.g.append(0, K, V, c.bits)
+        # The append lets a quantized row that is not finite reach the codes of a neighbour; the attention is held to what
+        # is stored.
+        _, _, kc, vc, km, vm = dirty.g.export(0, 0, 150)
+        seen = np.r_[0:5, 109:150]
+        for mine, stored in ((c.cache.kc, kc), (c.cache.vc, vc), (c.cache.km, km), (c.cache.vm, vm)):
+            mine[:, seen] = stored[:, seen].reshape(mine[:, seen].shape)
+        c.check(dirty.run_window(Q1, 40, 5), Q1, 40, 5)
+        c.check(dirty.run_tree(Q, t, 41, 5), Q, 41, 5, t)
+        dirty.g.close()
+
+
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
+def test_a_drafted_row_that_is_not_finite_concerns_its_descendants_only(gu, oracle, bad):
+    with Case(gu, oracle, 27, 1, 6, 2, [70]) as c:
+        T, hit = 22, (3, 17)
+        Q, (K, V, bits, par) = c.queries(T), c.tree(T)
+        bits[0, list(hit)] = 16
+        want, bound = rr.attention(oracle, c.cache, c.lens, Q, 3, tree=(K.copy(), V.copy(), bits, par))
+        V[0, list(hit), :, 5] = bad
+        K[0, 17] = bad
+        got = c.run_tree(Q, (K, V, bits, par))
+        for i, ch in enumerate(rr.chains(par[0])):
+            if set(ch) & set(hit):
+                assert not np.any(np.isfinite(got[0, i]))
+            else:
+                assert np.all(np.abs(got[0, i].astype(np.float64) - want[0, i]) <= bound[0, i])
 
 
 def test_bad_bits_are_flagged_and_kept_as_fp16(gu, oracle):
