@@ -40,8 +40,9 @@
 // crosses unit borders.  With as many CTAs as stay resident and equal stretches all SMs finish together, whatever the
 // number of units; many units are taken whole.  The tiles of a unit (of its four pools laid end to end, a tile weighted
 // by its cost) are cut like the axis, a piece's into four equal shares, one per warp.  A warp streams its share through
-// its own ring of bulk copies, as in the decode kernel; the four warps are merged in shared memory, the pieces of a unit
-// through global records by the CTA that arrives last.  Nothing waits for another CTA.
+// its own ring of bulk copies, as in the decode kernel; the four warps are merged in shared memory.  Two to eight CTAs
+// of a unit that are resident together are a cluster and merge out of each other's shared memory; other pieces of a unit
+// go through global records and are merged by the CTA that arrives last, so that nothing there waits for another CTA.
 //
 // Window.  Slots of a pool are handed out in position order, so a window is a suffix and the sinks a prefix of every
 // pool.  Where they start follows from the per-token index: the first token of class c at or after position p names
@@ -54,7 +55,7 @@
 #include "kvq_common.cuh"
 #include "kvq_ptx.cuh"
 #include "kvq_rows.h"
-#include <type_traits>
+#include <cooperative_groups.h>
 
 namespace kvq {
 
@@ -150,6 +151,23 @@ __device__ __forceinline__ float fast_rcp(float x) {
     float y;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// Shared memory of CTA `rank` of the cluster, at the address that `at` is in this CTA's.
+__device__ __forceinline__ float2 ld_cluster_f2(uint32_t at, uint32_t rank) {
+    float2 v;
+    asm volatile("{ .reg .b32 a;\n mapa.shared::cluster.u32 a, %2, %3;\n ld.shared::cluster.v2.f32 {%0, %1}, [a]; }"
+                 : "=f"(v.x), "=f"(v.y)
+                 : "r"(at), "r"(rank)
+                 : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t at, uint32_t rank) {
+    float4 v;
+    asm volatile("{ .reg .b32 a;\n mapa.shared::cluster.u32 a, %4, %5;\n ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a]; }"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(at), "r"(rank)
+                 : "memory");
+    return v;
 }
 __device__ __forceinline__ float two_to(int e) { return __int_as_float((127 + e) << 23); }
 
@@ -1117,6 +1135,12 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
         }
         if (a1 - a0 == P.ticks) {
             store_row(k, o, L);
+        } else if (P.cluster > 1) {                    // left in this CTA's shared memory, where warp 0's part was
+            float4* dst = reinterpret_cast<float4*>(out + (size_t)row * kRowsOutStride + piece8 * 8);
+            dst[0] = make_float4(o[0], o[1], o[2], o[3]);
+            dst[1] = make_float4(o[4], o[5], o[6], o[7]);
+            __syncwarp();                              // (a row belongs to eight lanes of a warp)
+            if (piece8 == 0) sc.ml[0][row] = make_float2(M, L);
         } else {
             const size_t rec = (size_t)rows_record(P, blockIdx.x, unit) * ROWS + row;
             float4* dst = reinterpret_cast<float4*>(P.part_o + rec * kHeadDim + piece8 * 8);
@@ -1125,7 +1149,39 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
             if (piece8 == 0) P.part_ml[rec] = make_float2(M, L);
         }
     }
-    if (a1 - a0 < P.ticks) {
+    if (P.cluster > 1) {
+        // ---- the CTAs of a unit are a cluster: each merges some of the rows out of the shared memory of all
+        namespace cg = cooperative_groups;
+        cg::cluster_group cluster = cg::this_cluster();
+        const uint32_t rank = blockIdx.x % P.cluster;
+        cluster.sync();
+#pragma unroll 1
+        for (int k = 0; k < RB; ++k) {
+            const int row = row_of(k);
+            if (row >= ROWS) break;
+            if ((uint32_t)row % P.cluster != rank) continue;
+            const uint32_t ml_at = smem_addr(&sc.ml[0][row]), o_at = smem_addr(out + (size_t)row * kRowsOutStride + piece8 * 8);
+            float2 ml[kRowsMaxCluster];
+            float M = kNegBig, L = 0.f;
+            float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (uint32_t s = 0; s < kRowsMaxCluster; ++s) {
+                ml[s] = s < P.cluster ? ld_cluster_f2(ml_at, s) : make_float2(kNegBig, 0.f);
+                M = fmaxf(M, ml[s].x);
+            }
+#pragma unroll
+            for (uint32_t s = 0; s < kRowsMaxCluster; ++s)
+                if (s < P.cluster) {
+                    const float4 v0 = ld_cluster_f4(o_at, s), v1 = ld_cluster_f4(o_at + 16, s);
+                    const float f = fast_exp2(ml[s].x - M);
+                    L = fmaf(ml[s].y, f, L);
+                    o[0] = fmaf(v0.x, f, o[0]); o[1] = fmaf(v0.y, f, o[1]); o[2] = fmaf(v0.z, f, o[2]); o[3] = fmaf(v0.w, f, o[3]);
+                    o[4] = fmaf(v1.x, f, o[4]); o[5] = fmaf(v1.y, f, o[5]); o[6] = fmaf(v1.z, f, o[6]); o[7] = fmaf(v1.w, f, o[7]);
+                }
+            store_row(k, o, L);
+        }
+        cluster.sync();                                // nobody leaves while its shared memory is read
+    } else if (a1 - a0 < P.ticks) {
         // ---- the CTA that delivers the unit's last piece merges the pieces, in order
         const uint32_t first = unit * P.ticks / P.span, pieces = ((unit + 1) * P.ticks - 1) / P.span - first + 1;
         __syncthreads();

@@ -1110,6 +1110,7 @@ static int rows_impl(kvq_ctx* c, int layer, const void* Q, void* O, const void* 
     p.pairs = (uint32_t)pairs;
     p.ticks = plan.ticks;
     p.span = plan.span;
+    p.cluster = plan.cluster;
     p.by_pool = plan.by_pool;
     rows_launch(p, plan, parents != nullptr, st);
     c->launches += 1;

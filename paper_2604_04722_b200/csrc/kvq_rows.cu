@@ -12,34 +12,51 @@ namespace {
 
 constexpr int kMaxDraftTiles = kMaxTreeNodes / kTileTokens;
 
-// CTAs of a kernel that fit an SM, by blocks of eight rows (1, 2, 4) and 16-node tiles of the tree (0: no tree).
+// CTAs of a kernel that fit an SM, and clusters of c of them that fit the device, by blocks of eight rows (1, 2, 4) and
+// 16-node tiles of the tree (0: no tree).
 struct Residency {
     int ctas[5][kMaxDraftTiles + 1] = {};
+    int clusters[5][kMaxDraftTiles + 1][kRowsMaxCluster + 1] = {};
 };
 Residency g_residency[64];             // per device; written with the same values by every set-up
+
+// A launch of `ctas` CTAs in clusters of `cluster`.
+struct Launch {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    Launch(uint64_t ctas, uint32_t cluster, size_t smem, cudaStream_t st) {
+        cfg.gridDim = dim3((unsigned)ctas);
+        cfg.blockDim = dim3(kRowsThreads);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = st;
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // may be scheduled behind the kernel ahead of it; see pdl_wait
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = cluster;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = cluster > 1 ? 2 : 1;
+    }
+};
 
 template <int NT, bool TREE>
 cudaError_t set_up_kernel(Residency& r) {
     const int most = TREE ? kMaxDraftTiles : 0;
     cudaError_t e = cudaFuncSetAttribute(k_attend_rows<NT, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)rows_smem_bytes<NT>(most));
-    for (int tiles = TREE ? 1 : 0; e == cudaSuccess && tiles <= most; ++tiles)
+    for (int tiles = TREE ? 1 : 0; e == cudaSuccess && tiles <= most; ++tiles) {
         e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&r.ctas[NT][tiles], k_attend_rows<NT, TREE>, kRowsThreads, rows_smem_bytes<NT>(tiles));
+        for (uint32_t c = 2; e == cudaSuccess && c <= kRowsMaxCluster; ++c) {
+            Launch l(c, c, rows_smem_bytes<NT>(tiles), nullptr);
+            e = cudaOccupancyMaxActiveClusters(&r.clusters[NT][tiles][c], k_attend_rows<NT, TREE>, &l.cfg);
+        }
+    }
     return e;
 }
 
 template <int NT, bool TREE>
 void launch(const RowsParams& p, uint64_t ctas, cudaStream_t st) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)ctas);
-    cfg.blockDim = dim3(kRowsThreads);
-    cfg.dynamicSmemBytes = rows_smem_bytes<NT>(TREE ? (p.nodes + kTileTokens - 1) / kTileTokens : 0);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];                       // may be scheduled behind the kernel ahead of it; see pdl_wait
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    cudaLaunchKernelEx(&cfg, k_attend_rows<NT, TREE>, p);
+    Launch l(ctas, p.cluster, rows_smem_bytes<NT>(TREE ? (p.nodes + kTileTokens - 1) / kTileTokens : 0), st);
+    cudaLaunchKernelEx(&l.cfg, k_attend_rows<NT, TREE>, p);
 }
 
 }  // namespace
@@ -71,12 +88,20 @@ RowsPlan rows_plan(int device, int sm_count, uint64_t pairs, int rows, int tree_
     const uint64_t units = pairs * plan.row_blocks;
     if (units > 0x7fffffffull) return plan;
     const int draft_tiles = (tree_nodes + kTileTokens - 1) / kTileTokens;
-    const int per_sm = device >= 0 && device < 64 ? std::max(1, g_residency[device].ctas[plan.nt][draft_tiles]) : 1;
+    const Residency* fit = device >= 0 && device < 64 ? &g_residency[device] : nullptr;
+    const int per_sm = fit ? std::max(1, fit->ctas[plan.nt][draft_tiles]) : 1;
     const uint64_t resident = (uint64_t)sm_count * per_sm;
     const uint64_t max_ctas = std::min<uint64_t>(4 * (uint64_t)sm_count, rows_max_record_rows(sm_count) / (16 * plan.nt));   // of a launch that cuts units
+    // Up to eight CTAs of a unit merge as a cluster, through shared memory (2048 tokens, one sequence, 8 parts: 12.7 us against
+    // 14.2 us through global records), if all of the launch are resident at once: clusters that wait for room for all their
+    // CTAs cost more than that (40 clusters of 7 over 3000 tokens: 45 us against 28 us).
+    auto cluster_of = [&](uint64_t parts) {
+        return fit && parts >= 2 && parts <= kRowsMaxCluster && units <= (uint64_t)fit->clusters[plan.nt][draft_tiles][parts] ? (uint32_t)parts : 1u;
+    };
     auto cut = [&](uint64_t parts) {                   // every unit into `parts` CTAs
         if (parts == 1) plan.ctas = (uint32_t)units, plan.ticks = plan.span = 1;
         else plan.ctas = plan.ticks = (uint32_t)(units * parts), plan.span = (uint32_t)units;
+        plan.cluster = cluster_of(parts);
     };
     if (splits > 0) {
         uint64_t parts = (uint64_t)((splits + kRowsWarps - 1) / kRowsWarps);
@@ -86,9 +111,9 @@ RowsPlan rows_plan(int device, int sm_count, uint64_t pairs, int rows, int tree_
     }
     // A model of the launch in us, fitted to measured sweeps over context lengths and splits: a CTA's set-up and merge, its
     // warps' tiles -- a tile costs a warp more the more CTAs share the SM -- in as many waves as it takes.  Parts of a unit
-    // that go through global records cost a merge; CTAs with stretches that do not end at unit borders work on two units
+    // cost a merge, more of them more if they go through global records; CTAs with stretches that do not end at unit borders work on two units
     // one after the other, with a second set-up.
-    const double set_up = 7.0, merge = 1.5, merge_part = 0.15;
+    const double set_up = 7.0, crowded = 0.5, merge = plan.nt == 1 ? 1.5 : 2.2, merge_part = 0.15;
     const double second = plan.nt == 1 ? 8.0 : plan.nt == 2 ? 17.0 : 30.0;
     const double tile_full = plan.nt == 1 ? 0.52 : plan.nt == 2 ? 0.65 : 0.75, tile_alone = plan.nt == 1 ? 0.4 : plan.nt == 2 ? 0.5 : 0.6;
     double best = 0.0;
@@ -98,7 +123,7 @@ RowsPlan rows_plan(int device, int sm_count, uint64_t pairs, int rows, int tree_
         const double waves = (double)((ctas + resident - 1) / resident);
         const double load = std::min(1.0, (double)((ctas + sm_count - 1) / sm_count) / (double)per_sm);
         const double tile = std::max(tile_alone, tile_full * load);
-        const double cost = waves * (set_up + tiles / (double)(p * kRowsWarps) * tile) + (p > 1 ? merge + merge_part * (double)p : 0.0);
+        const double cost = waves * (set_up + crowded * load + tiles / (double)(p * kRowsWarps) * tile) + (p > 1 ? merge + (cluster_of(p) > 1 ? 0.0 : merge_part * (double)p) : 0.0);
         if (p == 1 || cost < best) {
             best = cost;
             parts = p;
@@ -106,8 +131,8 @@ RowsPlan rows_plan(int device, int sm_count, uint64_t pairs, int rows, int tree_
     }
     cut(parts);
     if (2 * units > resident && units < 4 * resident && resident <= max_ctas && units < rows_max_units(sm_count)) {
-        const double cost = set_up + second + merge + (double)units * tiles / (double)(resident * kRowsWarps) * tile_full;
-        if (cost < best) plan.ctas = plan.ticks = (uint32_t)resident, plan.span = (uint32_t)units;
+        const double cost = set_up + crowded + second + merge + (double)units * tiles / (double)(resident * kRowsWarps) * tile_full;
+        if (cost < best) plan.ctas = plan.ticks = (uint32_t)resident, plan.span = (uint32_t)units, plan.cluster = 1;
     }
     return plan;
 }

@@ -24,6 +24,7 @@ struct RowsParams {
     int layer, group, nodes, rows; // rows = nodes * group
     uint32_t pairs;                // (sequence, KV head) pairs; unit = row block * pairs + pair
     uint32_t ticks, span;          // ticks per unit and per CTA of the axis on which the units lie end to end
+    uint32_t cluster;              // > 1: the CTAs of a unit, in exact parts, are a cluster and merge through shared memory
     bool by_pool;                  // a share is the same fraction of every pool (otherwise a stretch of the pools laid end to end)
     int window, sinks;             // window == 0: everything is visible
 };
@@ -44,9 +45,10 @@ struct VerifyParams {
 // How a launch is cut: blocks of eight rows per unit (1, 2 or 4), units per (sequence, KV head), CTAs, and the axis of RowsParams.
 struct RowsPlan {
     int nt = 1;
-    uint32_t row_blocks = 1, ctas = 1, ticks = 1, span = 1;
+    uint32_t row_blocks = 1, ctas = 1, ticks = 1, span = 1, cluster = 1;
     bool by_pool = false;
 };
+constexpr uint32_t kRowsMaxCluster = 8;                // CTAs of a unit that merge through shared memory at most
 constexpr int kRowsMaxRows = 32;                       // rows of a unit at most
 
 // What a handle keeps for launches that cut units: rows of partial records, two records for each CTA (at most four CTAs of
