@@ -41,7 +41,8 @@
 // number of units; many units are taken whole.  The tiles of a unit (of its four pools laid end to end, a tile weighted
 // by its cost) are cut like the axis, a piece's into four equal shares, one per warp.  A warp streams its share through
 // its own ring of bulk copies, as in the decode kernel; the four warps are merged in shared memory.  Two to eight CTAs
-// of a unit that are resident together are a cluster and merge out of each other's shared memory; other pieces of a unit
+// of a unit that are resident together are a cluster: each sends its rows to the CTAs that merge them, which is one barrier
+// of the cluster (2048 tokens, one sequence, 8 parts: 11.2 us against 14.2 us through global memory).  Other pieces of a unit
 // go through global records and are merged by the CTA that arrives last, so that nothing there waits for another CTA.
 //
 // Window.  Slots of a pool are handed out in position order, so a window is a suffix and the sinks a prefix of every
@@ -55,7 +56,6 @@
 #include "kvq_common.cuh"
 #include "kvq_ptx.cuh"
 #include "kvq_rows.h"
-#include <cooperative_groups.h>
 
 namespace kvq {
 
@@ -70,7 +70,7 @@ static_assert(6 * pool_rec_bytes(0) <= kRowsStageBytes && 4 * pool_rec_bytes(1) 
               2 * pool_rec_bytes(2) <= kRowsStageBytes && pool_rec_bytes(3) <= kRowsStageBytes, "a chunk fits a stage");
 constexpr int kDraftTileBytes = 4096;                  // one fp16 tile: K units, then V units
 // What a tile of each class costs a warp, for cutting a unit into equal shares.
-__device__ constexpr uint32_t kRowsTileCost[kNumPools] = {6u, 7u, 9u, 15u};
+__device__ constexpr float kRowsTileCost[kNumPools] = {6.f, 7.f, 9.f, 15.f};
 constexpr int kWeightTop = 4;                          // log2 of a row's largest weight when its reference is set
 
 // Resident CTAs per SM that the kernel is compiled for (its registers allow; trees of more than 16 nodes take so much shared
@@ -78,9 +78,15 @@ constexpr int kWeightTop = 4;                          // log2 of a row's larges
 __host__ __device__ constexpr int rows_ctas_per_sm(int nt) { return nt == 4 ? 2 : 4; }
 // NT: blocks of 8 rows per unit.
 template <int NT>
-__host__ __device__ constexpr size_t rows_smem_bytes(int draft_tiles) {
+__host__ __device__ constexpr size_t rows_smem_bytes(int draft_tiles, uint32_t cluster) {
     return (size_t)kRowsWarps * kRowsStages * kRowsStageBytes + (size_t)kNumPools * NT * 2 * 32 * 16 +
-           (size_t)draft_tiles * kDraftTileBytes;
+           (size_t)draft_tiles * kDraftTileBytes +
+           (cluster > 1 ? (size_t)((8 * NT + cluster - 1) / cluster) * cluster * kRowsOutStride * sizeof(float) : 0);
+}
+// An upper bound over all clusters.
+template <int NT>
+__host__ __device__ constexpr size_t rows_smem_limit(int draft_tiles) {
+    return rows_smem_bytes<NT>(draft_tiles, 1) + (8 * NT + kRowsMaxCluster - 1) * kRowsOutStride * sizeof(float);
 }
 static_assert(kRowsWarps * kRowsMaxRows * kRowsOutStride * 4 <= kRowsWarps * kRowsStages * kRowsStageBytes,
               "the merge buffer lives in the rings");
@@ -152,23 +158,15 @@ __device__ __forceinline__ float fast_rcp(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// Shared memory of CTA `rank` of the cluster, at the address that `at` is in this CTA's.
-__device__ __forceinline__ float2 ld_cluster_f2(uint32_t at, uint32_t rank) {
-    float2 v;
-    asm volatile("{ .reg .b32 a;\n mapa.shared::cluster.u32 a, %2, %3;\n ld.shared::cluster.v2.f32 {%0, %1}, [a]; }"
-                 : "=f"(v.x), "=f"(v.y)
-                 : "r"(at), "r"(rank)
+// Stores to the shared memory of CTA `rank` of the cluster, at the address that `at` is in this CTA's.
+__device__ __forceinline__ void st_cluster(uint32_t at, uint32_t rank, float4 v) {
+    asm volatile("{ .reg .b32 a;\n mapa.shared::cluster.u32 a, %0, %1;\n st.shared::cluster.v4.f32 [a], {%2, %3, %4, %5}; }" ::"r"(at), "r"(rank),
+                 "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w)
                  : "memory");
-    return v;
 }
-__device__ __forceinline__ float4 ld_cluster_f4(uint32_t at, uint32_t rank) {
-    float4 v;
-    asm volatile("{ .reg .b32 a;\n mapa.shared::cluster.u32 a, %4, %5;\n ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a]; }"
-                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                 : "r"(at), "r"(rank)
-                 : "memory");
-    return v;
-}
+// The two halves of a barrier of the cluster.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ float two_to(int e) { return __int_as_float((127 + e) << 23); }
 
 // The slot of the first token of class c at a position >= p of a sequence of len tokens (n_c if there is none), for the
@@ -214,10 +212,11 @@ struct RowsScratch {
     uint32_t lo_row[kNumPools][ROWS];               // first window slot of every row
     float2 ml[kRowsWarps][ROWS];
     float sumq[ROWS];                               // log2(e)/8 * sum_i q_i
-    float wmax[kRowsWarps];
+    float wmax[kRowsWarps], load[kRowsWarps];
     int16_t node[ROWS];                             // node of a row, -1 behind the last
     int8_t link[kMaxTreeNodes], bad[kMaxTreeNodes];
     uint32_t last;
+    int draft_tile[kRowsWarps];
     alignas(16) __half q[ROWS][kRowsQStride];
 };
 
@@ -590,6 +589,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
     uint4* const qfrag = reinterpret_cast<uint4*>(dyn + (size_t)kRowsWarps * kRowsStages * kRowsStageBytes);   // [class][NT][2][32]
     const uint32_t draft_at = (uint32_t)((size_t)kRowsWarps * kRowsStages * kRowsStageBytes + (size_t)kNumPools * NT * 2 * 32 * 16);
     uint8_t* const draft = dyn + draft_at;
+    float* const inbox = reinterpret_cast<float*>(draft + (size_t)(TREE ? (P.nodes + kTileTokens - 1) / kTileTokens : 0) * kDraftTileBytes);   // [rows of this CTA][CTAs][kRowsOutStride]
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
     const StoreView& S = P.store;
 
@@ -602,6 +602,8 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
         for (int s = 0; s < kRowsStages; ++s) mbar_init(&sc.bars[warp][s], 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    __syncwarp();
+    if (P.cluster > 1) cluster_arrive();               // (before another CTA's memory is written, all of them have to be there)
     pdl_launch_dependents();
     pdl_wait();                                        // an append ahead of this launch has stored its tokens
 
@@ -615,7 +617,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
     x += a1 - a0;
     const uint32_t rb = unit / P.pairs, bh = unit - rb * P.pairs;  // row blocks of a pair lie far apart: CTAs that run at the same time read the same tiles
     const int b = (int)(bh / (uint32_t)S.kv_heads), h = (int)(bh - (uint32_t)b * S.kv_heads);
-    const bool has_draft = TREE && a1 == P.ticks;
+    const bool has_end = a1 == P.ticks, has_draft = TREE && has_end;
 
     // ---- what the piece starts from, requested together
     const uint4 fill = *reinterpret_cast<const uint4*>(P.counts + (size_t)b * 4);
@@ -624,18 +626,18 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
     constexpr int RB = ROWS > 16 ? ROWS / 16 : 1;
     const int row16 = tid >> 3, piece8 = tid & 7;
     auto row_of = [&](int k) { return 16 * k + row16; };
-    auto place_of = [&](int k, int& node) -> size_t {  // of a row's eight channels in Q and O
-        const int R = (int)rb * ROWS + row_of(k);
+    auto place_of = [&](int row, int& node) -> size_t {                // of a row's eight channels in Q and O
+        const int R = (int)rb * ROWS + row;
         node = R / P.group;
         return (((size_t)b * P.nodes + node) * S.q_heads + (size_t)h * P.group + (R - node * P.group)) * kHeadDim + piece8 * 8;
     };
-    auto row_used = [&](int k) { return row_of(k) < ROWS && (int)rb * ROWS + row_of(k) < P.rows; };
+    auto row_used = [&](int row) { return row < ROWS && (int)rb * ROWS + row < P.rows; };
     uint4 qv[RB];
     int my_node[RB];
 #pragma unroll
     for (int k = 0; k < RB; ++k) {
-        const size_t at = place_of(k, my_node[k]);
-        qv[k] = row_used(k) ? *reinterpret_cast<const uint4*>(P.Q + at) : make_uint4(0u, 0u, 0u, 0u);
+        const size_t at = place_of(row_of(k), my_node[k]);
+        qv[k] = row_used(row_of(k)) ? *reinterpret_cast<const uint4*>(P.Q + at) : make_uint4(0u, 0u, 0u, 0u);
     }
     int par[2] = {-2, -2};
     if (TREE && warp == 0) {
@@ -681,7 +683,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
         int ns = (int)((sink + kTileTokens - 1) / kTileTokens), ws = (int)(start / kTileTokens);
         if (ws <= ns) ns = ws = 0;                     // no gap
         const int n = ns + nt - ws;
-        const float cost = (float)kRowsTileCost[c], weight = (float)n * cost;
+        const float cost = c == 0 ? kRowsTileCost[0] : c == 1 ? kRowsTileCost[1] : c == 2 ? kRowsTileCost[2] : kRowsTileCost[3], weight = (float)n * cost;
         float before = 0.f, total = 0.f;
 #pragma unroll
         for (int k = 0; k < kNumPools; ++k) {
@@ -689,15 +691,28 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
             before += k < c ? wk : 0.f;
             total += wk;
         }
-        // The end of a share and the start of the next one are the same expression of the same tick, which does not fall as
-        // the tick grows; the last share ends with the last tile.  So no tile is lost or taken twice, however this rounds.
-        const uint32_t t0 = a0 * kRowsWarps + (a1 - a0) * warp, t1 = t0 + (a1 - a0), T = P.ticks * kRowsWarps;
-        const float scale = total / (float)T, inv = 1.0f / cost;
-        const float pool_scale = (float)n / (float)T;
-        auto tiles_before = [&](uint32_t t) {
-            return t == T ? n : min(max((int)(P.by_pool ? pool_scale * (float)t : (scale * (float)t - before) * inv), 0), n);
+        // Positions on the pools laid end to end, in units of cost.  Drafted rows cost the last piece of the unit about as much
+        // as so many tiles, which stand for them behind the last pool (with an equal share that piece came last: 512 tokens,
+        // 8 nodes, 8 parts: 10.1 us against 9.4 us).  The end of a share and the start of the next one are
+        // the same expression of the same tick, which does not fall as the tick grows; the last share ends with the last tile.
+        // So no tile is lost or taken twice, however this rounds.
+        const float drafts = TREE ? 60.f + 20.f * (float)draft_tiles : 0.f, per_tick = (total + drafts) * fast_rcp((float)P.ticks);
+        const float x0 = fminf((float)a0 * per_tick, total), x1 = has_end ? total : fminf((float)a1 * per_tick, total);
+        const float per_pool = n > 0 ? (float)n * fast_rcp(total) : 0.f, inv = fast_rcp(cost);
+        // (where a share is the same fraction of every pool, the last one has the pools' last, ragged tiles, which take longer)
+        const float quarter = 0.25f * (x1 - x0 + (P.by_pool && has_end && n > 0 ? total * fast_rcp((float)n) : 0.f));
+        auto tiles_before = [&](int share) {           // tiles of the pool in front of warp `share`'s
+            if (share == kRowsWarps && has_end) return n;
+            const float at = share == kRowsWarps ? x1 : fminf(x0 + quarter * (float)share, x1);
+            return min(max((int)(P.by_pool ? at * per_pool : (at - before) * inv), 0), n);
         };
-        const int lo = tiles_before(t0), hi = tiles_before(t1);
+        const int lo = tiles_before(warp), hi = tiles_before(warp + 1);
+        if (TREE) {                                    // what the warp's share costs it
+            float load = (float)(hi - lo) * cost;
+            load += __shfl_xor_sync(0xffffffffu, load, 1);
+            load += __shfl_xor_sync(0xffffffffu, load, 2);
+            if (lane == 0) sc.load[warp] = load;
+        }
         if (lane < kNumPools) {
             sc.seg_lo[warp][2 * c] = lo;
             sc.seg_hi[warp][2 * c] = min(hi, ns);
@@ -732,7 +747,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
             *reinterpret_cast<uint4*>(&sc.q[row_of(k)][piece8 * 8]) = qv[k];
             if (piece8 == 0) {
                 sc.sumq[row_of(k)] = sum * kLogitScale;
-                sc.node[row_of(k)] = (int16_t)(row_used(k) ? my_node[k] : -1);
+                sc.node[row_of(k)] = (int16_t)(row_used(row_of(k)) ? my_node[k] : -1);
             }
         }
     }
@@ -978,7 +993,14 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
         v_products(st, a, w);
     };
     int cls = 3;
-    bool draft_left = has_draft && warp < draft_tiles; // a tile of drafted tokens per warp, at the end
+    bool draft_left = false;                           // a tile of drafted tokens per warp, at the end: the warps with the least to do first
+    if (has_draft) {
+        const float load = sc.load[lane & 3], mine = __shfl_sync(0xffffffffu, load, warp);
+        const int tile = __popc(__ballot_sync(0xffffffffu, load < mine || (load == mine && (lane & 3) < warp)) & 15u);
+        draft_left = tile < draft_tiles;
+        if (lane == 0) sc.draft_tile[warp] = tile;
+        __syncwarp();
+    }
     load_queries(3, qf);
     while ((in_flight > 0 || draft_left) && !failed) {
         const bool drafted = in_flight == 0;
@@ -994,7 +1016,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
             failed = !__all_sync(0xffffffffu, mbar_wait(&sc.bars[warp][cslot], (parity >> cslot) & 1u));
             if (failed) break;
         }
-        const uint8_t* rec = dyn + (drafted ? draft_at + (uint32_t)warp * kDraftTileBytes : ring + (uint32_t)cslot * kRowsStageBytes);
+        const uint8_t* rec = dyn + (drafted ? draft_at + (uint32_t)sc.draft_tile[warp] * kDraftTileBytes : ring + (uint32_t)cslot * kRowsStageBytes);
         const uint32_t step = (uint32_t)(c == 0 ? pool_rec_bytes(0) : c == 1 ? pool_rec_bytes(1) : c == 2 ? pool_rec_bytes(2) : pool_rec_bytes(3));
         uint32_t left = ck.y & 15u, edges = ck.y >> 4, s0 = (ck.x & 0x3fffffffu) * kTileTokens;
 #pragma unroll 1
@@ -1015,7 +1037,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
             uint32_t seen[NT] = {}, slots = 0xffffu;
             const bool edge = edges & 1u;
             if (edge) {                                // the pool's last tile, one where a window starts or the sinks end, a drafted one
-                const uint32_t use = drafted ? (uint32_t)(sc.used >> (16 * warp)) : 0u, cnt = sc.cnt[c], sink = sc.sink[c];
+                const uint32_t use = drafted ? (uint32_t)(sc.used >> (16 * sc.draft_tile[warp])) : 0u, cnt = sc.cnt[c], sink = sc.sink[c];
                 // those that some row sees: up to the end of the pool, from the shallowest row's window on or in the sinks
                 const auto below = [&](uint32_t end) { return end <= s0 ? 0u : (1u << min(end - s0, 16u)) - 1u; };
                 slots = drafted ? use & 0xffffu : below(cnt) & (~below(sc.start[c]) | below(sink));
@@ -1025,7 +1047,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
                     for (int x = 0; x < 2; ++x) {      // row 2q + x
                         const int row = 8 * n + 2 * q + x, node = sc.node[row];
                         const uint32_t lo = P.window > 0 ? sc.lo_row[c][row] : 0u;
-                        const uint32_t vis = drafted && node >= 0 ? (uint32_t)(sc.vis[node] >> (16 * warp)) : 0u;
+                        const uint32_t vis = drafted && node >= 0 ? (uint32_t)(sc.vis[node] >> (16 * sc.draft_tile[warp])) : 0u;
 #pragma unroll
                         for (int s = 0; s < 2; ++s) {
                             const uint32_t at = g + 8 * s, slot = s0 + at;
@@ -1106,10 +1128,11 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
     __syncthreads();
 
     // ---- this CTA's rows: thread = (row, eight channels)
-    auto store_row = [&](int k, const float (&o)[8], float L) {
-        if (!row_used(k)) return;
+    if (P.cluster > 1) cluster_wait();
+    auto store_row = [&](int row, const float (&o)[8], float L) {
+        if (!row_used(row)) return;
         int node;
-        const size_t at = place_of(k, node);
+        const size_t at = place_of(row, node);
         // nothing seen, or an unused node: zeros (a NaN stays one)
         const float inv = L != 0.f && (!TREE || sc.vis[node]) ? 1.0f / L : 0.f;
         uint32_t v[4];
@@ -1134,13 +1157,12 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
             o[4] += v1.x; o[5] += v1.y; o[6] += v1.z; o[7] += v1.w;
         }
         if (a1 - a0 == P.ticks) {
-            store_row(k, o, L);
-        } else if (P.cluster > 1) {                    // left in this CTA's shared memory, where warp 0's part was
-            float4* dst = reinterpret_cast<float4*>(out + (size_t)row * kRowsOutStride + piece8 * 8);
-            dst[0] = make_float4(o[0], o[1], o[2], o[3]);
-            dst[1] = make_float4(o[4], o[5], o[6], o[7]);
-            __syncwarp();                              // (a row belongs to eight lanes of a warp)
-            if (piece8 == 0) sc.ml[0][row] = make_float2(M, L);
+            store_row(row, o, L);
+        } else if (P.cluster > 1) {                    // to the CTA that merges this row
+            const uint32_t at = smem_addr(inbox + ((size_t)(row / P.cluster) * P.cluster + blockIdx.x % P.cluster) * kRowsOutStride), to = row % P.cluster;
+            st_cluster(at + piece8 * 32, to, make_float4(o[0], o[1], o[2], o[3]));
+            st_cluster(at + piece8 * 32 + 16, to, make_float4(o[4], o[5], o[6], o[7]));
+            if (piece8 == 0) st_cluster(at + kHeadDim * 4, to, make_float4(M, L, 0.f, 0.f));
         } else {
             const size_t rec = (size_t)rows_record(P, blockIdx.x, unit) * ROWS + row;
             float4* dst = reinterpret_cast<float4*>(P.part_o + rec * kHeadDim + piece8 * 8);
@@ -1150,37 +1172,27 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
         }
     }
     if (P.cluster > 1) {
-        // ---- the CTAs of a unit are a cluster: each merges some of the rows out of the shared memory of all
-        namespace cg = cooperative_groups;
-        cg::cluster_group cluster = cg::this_cluster();
-        const uint32_t rank = blockIdx.x % P.cluster;
-        cluster.sync();
-#pragma unroll 1
-        for (int k = 0; k < RB; ++k) {
-            const int row = row_of(k);
-            if (row >= ROWS) break;
-            if ((uint32_t)row % P.cluster != rank) continue;
-            const uint32_t ml_at = smem_addr(&sc.ml[0][row]), o_at = smem_addr(out + (size_t)row * kRowsOutStride + piece8 * 8);
-            float2 ml[kRowsMaxCluster];
+        // ---- the CTAs of a unit are a cluster: each merges the rows that it has been sent
+        cluster_arrive();
+        cluster_wait();
+        const int row = (int)(row16 * P.cluster + blockIdx.x % P.cluster);
+        if (row < ROWS) {
+            const float* const from = inbox + (size_t)row16 * P.cluster * kRowsOutStride;
             float M = kNegBig, L = 0.f;
             float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (uint32_t s = 0; s < kRowsMaxCluster; ++s) {
-                ml[s] = s < P.cluster ? ld_cluster_f2(ml_at, s) : make_float2(kNegBig, 0.f);
-                M = fmaxf(M, ml[s].x);
+            for (uint32_t s = 0; s < P.cluster; ++s) M = fmaxf(M, from[s * kRowsOutStride + kHeadDim]);
+#pragma unroll 2
+            for (uint32_t s = 0; s < P.cluster; ++s) {
+                const float2 ml = *reinterpret_cast<const float2*>(from + s * kRowsOutStride + kHeadDim);
+                const float4* src = reinterpret_cast<const float4*>(from + s * kRowsOutStride + piece8 * 8);
+                const float4 v0 = src[0], v1 = src[1];
+                const float f = fast_exp2(ml.x - M);
+                L = fmaf(ml.y, f, L);
+                o[0] = fmaf(v0.x, f, o[0]); o[1] = fmaf(v0.y, f, o[1]); o[2] = fmaf(v0.z, f, o[2]); o[3] = fmaf(v0.w, f, o[3]);
+                o[4] = fmaf(v1.x, f, o[4]); o[5] = fmaf(v1.y, f, o[5]); o[6] = fmaf(v1.z, f, o[6]); o[7] = fmaf(v1.w, f, o[7]);
             }
-#pragma unroll
-            for (uint32_t s = 0; s < kRowsMaxCluster; ++s)
-                if (s < P.cluster) {
-                    const float4 v0 = ld_cluster_f4(o_at, s), v1 = ld_cluster_f4(o_at + 16, s);
-                    const float f = fast_exp2(ml[s].x - M);
-                    L = fmaf(ml[s].y, f, L);
-                    o[0] = fmaf(v0.x, f, o[0]); o[1] = fmaf(v0.y, f, o[1]); o[2] = fmaf(v0.z, f, o[2]); o[3] = fmaf(v0.w, f, o[3]);
-                    o[4] = fmaf(v1.x, f, o[4]); o[5] = fmaf(v1.y, f, o[5]); o[6] = fmaf(v1.z, f, o[6]); o[7] = fmaf(v1.w, f, o[7]);
-                }
-            store_row(k, o, L);
+            store_row(row, o, L);
         }
-        cluster.sync();                                // nobody leaves while its shared memory is read
     } else if (a1 - a0 < P.ticks) {
         // ---- the CTA that delivers the unit's last piece merges the pieces, in order
         const uint32_t first = unit * P.ticks / P.span, pieces = ((unit + 1) * P.ticks - 1) / P.span - first + 1;
@@ -1211,7 +1223,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
                     o[0] = fmaf(o[0], r, v0.x * f); o[1] = fmaf(o[1], r, v0.y * f); o[2] = fmaf(o[2], r, v0.z * f); o[3] = fmaf(o[3], r, v0.w * f);
                     o[4] = fmaf(o[4], r, v1.x * f); o[5] = fmaf(o[5], r, v1.y * f); o[6] = fmaf(o[6], r, v1.z * f); o[7] = fmaf(o[7], r, v1.w * f);
                 }
-                store_row(k, o, L);
+                store_row(row, o, L);
             }
         }
     }

@@ -42,11 +42,11 @@ struct Launch {
 template <int NT, bool TREE>
 cudaError_t set_up_kernel(Residency& r) {
     const int most = TREE ? kMaxDraftTiles : 0;
-    cudaError_t e = cudaFuncSetAttribute(k_attend_rows<NT, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)rows_smem_bytes<NT>(most));
+    cudaError_t e = cudaFuncSetAttribute(k_attend_rows<NT, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)rows_smem_limit<NT>(most));
     for (int tiles = TREE ? 1 : 0; e == cudaSuccess && tiles <= most; ++tiles) {
-        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&r.ctas[NT][tiles], k_attend_rows<NT, TREE>, kRowsThreads, rows_smem_bytes<NT>(tiles));
+        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&r.ctas[NT][tiles], k_attend_rows<NT, TREE>, kRowsThreads, rows_smem_bytes<NT>(tiles, 1));
         for (uint32_t c = 2; e == cudaSuccess && c <= kRowsMaxCluster; ++c) {
-            Launch l(c, c, rows_smem_bytes<NT>(tiles), nullptr);
+            Launch l(c, c, rows_smem_bytes<NT>(tiles, c), nullptr);
             e = cudaOccupancyMaxActiveClusters(&r.clusters[NT][tiles][c], k_attend_rows<NT, TREE>, &l.cfg);
         }
     }
@@ -55,7 +55,7 @@ cudaError_t set_up_kernel(Residency& r) {
 
 template <int NT, bool TREE>
 void launch(const RowsParams& p, uint64_t ctas, cudaStream_t st) {
-    Launch l(ctas, p.cluster, rows_smem_bytes<NT>(TREE ? (p.nodes + kTileTokens - 1) / kTileTokens : 0), st);
+    Launch l(ctas, p.cluster, rows_smem_bytes<NT>(TREE ? (p.nodes + kTileTokens - 1) / kTileTokens : 0, p.cluster), st);
     cudaLaunchKernelEx(&l.cfg, k_attend_rows<NT, TREE>, p);
 }
 
@@ -92,9 +92,9 @@ RowsPlan rows_plan(int device, int sm_count, uint64_t pairs, int rows, int tree_
     const int per_sm = fit ? std::max(1, fit->ctas[plan.nt][draft_tiles]) : 1;
     const uint64_t resident = (uint64_t)sm_count * per_sm;
     const uint64_t max_ctas = std::min<uint64_t>(4 * (uint64_t)sm_count, rows_max_record_rows(sm_count) / (16 * plan.nt));   // of a launch that cuts units
-    // Up to eight CTAs of a unit merge as a cluster, through shared memory (2048 tokens, one sequence, 8 parts: 12.7 us against
-    // 14.2 us through global records), if all of the launch are resident at once: clusters that wait for room for all their
-    // CTAs cost more than that (40 clusters of 7 over 3000 tokens: 45 us against 28 us).
+    // Up to eight CTAs of a unit merge as a cluster, through shared memory, if all of the launch are resident at once: 2048
+    // tokens of one sequence in 8 parts take 11.2 us, and 14.2 us through global records; but 40 clusters of 7 of which some
+    // wait for room for all their CTAs took 45 us instead of 28 us.
     auto cluster_of = [&](uint64_t parts) {
         return fit && parts >= 2 && parts <= kRowsMaxCluster && units <= (uint64_t)fit->clusters[plan.nt][draft_tiles][parts] ? (uint32_t)parts : 1u;
     };
@@ -114,7 +114,7 @@ RowsPlan rows_plan(int device, int sm_count, uint64_t pairs, int rows, int tree_
     // cost a merge, more of them more if they go through global records; CTAs with stretches that do not end at unit borders work on two units
     // one after the other, with a second set-up.
     const double set_up = 7.0, crowded = 0.5, merge = plan.nt == 1 ? 1.5 : 2.2, merge_part = 0.15;
-    const double second = plan.nt == 1 ? 8.0 : plan.nt == 2 ? 17.0 : 30.0;
+    const double second = plan.nt == 1 ? 8.0 : plan.nt == 2 ? 17.0 : 45.0;
     const double tile_full = plan.nt == 1 ? 0.52 : plan.nt == 2 ? 0.65 : 0.75, tile_alone = plan.nt == 1 ? 0.4 : plan.nt == 2 ? 0.5 : 0.6;
     double best = 0.0;
     uint64_t parts = 1;
