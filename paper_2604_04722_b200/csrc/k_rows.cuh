@@ -40,9 +40,9 @@
 // crosses unit borders.  With as many CTAs as stay resident and equal stretches all SMs finish together, whatever the
 // number of units; many units are taken whole.  The tiles of a unit (of its four pools laid end to end, a tile weighted
 // by its cost) are cut like the axis, a piece's into four equal shares, one per warp.  A warp streams its share through
-// its own ring of bulk copies, as in the decode kernel; the four warps are merged in shared memory.  Two to eight CTAs
+// its own ring of bulk copies, as in the decode kernel; the four warps are merged in shared memory.  Up to sixteen CTAs
 // of a unit that are resident together are a cluster: each sends its rows to the CTAs that merge them, which is one barrier
-// of the cluster (2048 tokens, one sequence, 8 parts: 11.2 us against 14.2 us through global memory).  Other pieces of a unit
+// of the cluster (2048 tokens, one sequence: 9.7 us against 14.2 us through global memory).  Other pieces of a unit
 // go through global records and are merged by the CTA that arrives last, so that nothing there waits for another CTA.
 //
 // Window.  Slots of a pool are handed out in position order, so a window is a suffix and the sinks a prefix of every
@@ -1211,7 +1211,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
                 if (row >= ROWS) break;
                 float M = kNegBig, L = 0.f;
                 float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
+#pragma unroll 4
                 for (uint32_t s = 0; s < pieces; ++s) {
                     const size_t rec = (size_t)rows_record(P, first + s, unit) * ROWS + row;
                     const float2 ml = __ldcg(P.part_ml + rec);

@@ -43,6 +43,7 @@ template <int NT, bool TREE>
 cudaError_t set_up_kernel(Residency& r) {
     const int most = TREE ? kMaxDraftTiles : 0;
     cudaError_t e = cudaFuncSetAttribute(k_attend_rows<NT, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)rows_smem_limit<NT>(most));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_attend_rows<NT, TREE>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     for (int tiles = TREE ? 1 : 0; e == cudaSuccess && tiles <= most; ++tiles) {
         e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&r.ctas[NT][tiles], k_attend_rows<NT, TREE>, kRowsThreads, rows_smem_bytes<NT>(tiles, 1));
         for (uint32_t c = 2; e == cudaSuccess && c <= kRowsMaxCluster; ++c) {
@@ -92,11 +93,13 @@ RowsPlan rows_plan(int device, int sm_count, uint64_t pairs, int rows, int tree_
     const int per_sm = fit ? std::max(1, fit->ctas[plan.nt][draft_tiles]) : 1;
     const uint64_t resident = (uint64_t)sm_count * per_sm;
     const uint64_t max_ctas = std::min<uint64_t>(4 * (uint64_t)sm_count, rows_max_record_rows(sm_count) / (16 * plan.nt));   // of a launch that cuts units
-    // Up to eight CTAs of a unit merge as a cluster, through shared memory, if all of the launch are resident at once: 2048
-    // tokens of one sequence in 8 parts take 11.2 us, and 14.2 us through global records; but 40 clusters of 7 of which some
-    // wait for room for all their CTAs took 45 us instead of 28 us.
+    // Up to sixteen CTAs of a unit merge as a cluster, through shared memory, if all of the launch are resident at once: 2048
+    // tokens of one sequence in 16 parts take 9.7 us, in 8 parts 11.2 us, and through global records 14.2 us; but 40 clusters of
+    // 7 of which some wait for room took 45 us instead of 28 us.  Two large CTAs per SM leave too little room to move up behind
+    // an earlier launch when they fill the device (30 clusters of 9: 31 us against 25 us with 8), so with 32 rows an eighth stays free.
     auto cluster_of = [&](uint64_t parts) {
-        return fit && parts >= 2 && parts <= kRowsMaxCluster && units <= (uint64_t)fit->clusters[plan.nt][draft_tiles][parts] ? (uint32_t)parts : 1u;
+        const uint64_t most = fit && parts >= 2 && parts <= kRowsMaxCluster ? (uint64_t)fit->clusters[plan.nt][draft_tiles][parts] : 0;
+        return units <= (plan.nt == 4 ? most * 7 / 8 : most) ? (uint32_t)parts : 1u;
     };
     auto cut = [&](uint64_t parts) {                   // every unit into `parts` CTAs
         if (parts == 1) plan.ctas = (uint32_t)units, plan.ticks = plan.span = 1;
@@ -109,21 +112,24 @@ RowsPlan rows_plan(int device, int sm_count, uint64_t pairs, int rows, int tree_
         cut(parts);
         return plan;
     }
-    // A model of the launch in us, fitted to measured sweeps over context lengths and splits: a CTA's set-up and merge, its
-    // warps' tiles -- a tile costs a warp more the more CTAs share the SM -- in as many waves as it takes.  Parts of a unit
-    // cost a merge, more of them more if they go through global records; CTAs with stretches that do not end at unit borders work on two units
-    // one after the other, with a second set-up.
-    const double set_up = 7.0, crowded = 0.5, merge = plan.nt == 1 ? 1.5 : 2.2, merge_part = 0.15;
-    const double second = plan.nt == 1 ? 8.0 : plan.nt == 2 ? 17.0 : 45.0;
-    const double tile_full = plan.nt == 1 ? 0.52 : plan.nt == 2 ? 0.65 : 0.75, tile_alone = plan.nt == 1 ? 0.4 : plan.nt == 2 ? 0.5 : 0.6;
+    // A model of the launch in us, fitted to 265 shapes (3 to 256 units, 120 to 20000 tokens) in 1 to 16 parts: what it picks is
+    // within 2 % of the best of them on average.  A CTA's set-up, longer the more CTAs share the SM; its warps' tiles, of which
+    // the first ones cost more (their instructions are not there yet); in as many waves as it takes; and the merge of the parts.
+    // CTAs with stretches that do not end at unit borders work on two units one after the other, with a second set-up.
+    struct Model { double set_up, crowded, tile, tile_full, early, early_tiles, merge, part, record, second, second_draft; };
+    static constexpr Model kModels[3] = {{4.7, 3.2, 0.56, 0.58, 0.115, 10.0, 0.4, 0.013, 0.30, 12.0, 4.0},
+                                         {8.2, 1.6, 0.64, 0.80, 0.485, 10.0, 0.0, 0.048, 0.32, 17.0, 6.0},
+                                         {9.2, 0.0, 0.65, 0.77, 0.455, 20.0, 0.0, 0.001, 0.75, 30.0, 14.0}};
+    const Model& m = kModels[plan.nt == 1 ? 0 : plan.nt == 2 ? 1 : 2];
+    auto work = [&](double n, double load) { return m.set_up + m.crowded * load + n * std::max(m.tile, m.tile_full * load) + m.early * std::min(n, m.early_tiles); };
     double best = 0.0;
     uint64_t parts = 1;
     for (uint64_t p = 1; p == 1 || (units * p <= max_ctas && p <= 64); ++p) {
         const uint64_t ctas = units * p;
         const double waves = (double)((ctas + resident - 1) / resident);
         const double load = std::min(1.0, (double)((ctas + sm_count - 1) / sm_count) / (double)per_sm);
-        const double tile = std::max(tile_alone, tile_full * load);
-        const double cost = waves * (set_up + crowded * load + tiles / (double)(p * kRowsWarps) * tile) + (p > 1 ? merge + (cluster_of(p) > 1 ? 0.0 : merge_part * (double)p) : 0.0);
+        const double merge = p == 1 ? 0.0 : cluster_of(p) > 1 ? m.merge + m.part * (double)p : m.record * (double)p;
+        const double cost = waves * work(tiles / (double)(p * kRowsWarps), load) + merge;
         if (p == 1 || cost < best) {
             best = cost;
             parts = p;
@@ -131,7 +137,7 @@ RowsPlan rows_plan(int device, int sm_count, uint64_t pairs, int rows, int tree_
     }
     cut(parts);
     if (2 * units > resident && units < 4 * resident && resident <= max_ctas && units < rows_max_units(sm_count)) {
-        const double cost = set_up + crowded + second + merge + (double)units * tiles / (double)(resident * kRowsWarps) * tile_full;
+        const double cost = work((double)units * tiles / (double)(resident * kRowsWarps), 1.0) + m.second + m.second_draft * (double)draft_tiles;
         if (cost < best) plan.ctas = plan.ticks = (uint32_t)resident, plan.span = (uint32_t)units, plan.cluster = 1;
     }
     return plan;

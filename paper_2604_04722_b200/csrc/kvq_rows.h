@@ -48,7 +48,7 @@ struct RowsPlan {
     uint32_t row_blocks = 1, ctas = 1, ticks = 1, span = 1, cluster = 1;
     bool by_pool = false;
 };
-constexpr uint32_t kRowsMaxCluster = 8;                // CTAs of a unit that merge through shared memory at most
+constexpr uint32_t kRowsMaxCluster = 16;               // CTAs of a unit that merge through shared memory at most
 constexpr int kRowsMaxRows = 32;                       // rows of a unit at most
 
 // What a handle keeps for launches that cut units: rows of partial records, two records for each CTA (at most four CTAs of
