@@ -74,73 +74,101 @@ cudaError_t rows_setup(int device) {
     return e;
 }
 
-RowsPlan rows_plan(int device, int sm_count, uint64_t pairs, int rows, int tree_nodes, int visible_tokens, int splits) {
+namespace {
+
+// A model of a launch in us: a CTA's set-up, longer the more CTAs share the SM and the more 16-node tiles of drafted rows it
+// stages; its warps' tiles, which slow each other down; in as many waves as it takes; then the merge of a unit's parts, by a
+// cluster or through records.  CTAs with stretches that do not end at unit borders work on two units one after the other, with
+// a second set-up.  Fitted to 457 shapes (3 to 512 units, 120 to 20000 tokens) in 1 to 16 parts: what it picks is within 2 % of
+// the best of them on average.
+struct LaunchModel {
+    double set_up, crowded, draft, tile, tile_full, merge, part, record, second, second_draft;
+};
+constexpr LaunchModel kLaunchModels[3] = {{4.7, 2.8, 1.2, 0.56, 0.58, 0.4, 0.01, 0.30, 12.0, 4.0},     // 8, 16 and 32 rows per unit
+                                          {6.1, 1.7, 1.6, 0.80, 0.80, 0.0, 0.02, 0.30, 11.0, 12.0},
+                                          {11.6, 1.75, 1.4, 0.787, 0.77, 0.0, 0.0, 0.48, 24.0, 14.0}};
+
+struct Shape {
+    const Residency* fit;
+    int sm_count, draft_tiles, splits;
+    uint64_t pairs;
+    int rows;
+    double tiles;
+};
+
+// The plan with blocks of 8 nt rows, and what the model says.
+RowsPlan plan_blocks(const Shape& w, int nt, double& best) {
     RowsPlan plan;
     plan.ctas = 0;
-    const double tiles = (double)visible_tokens / kTileTokens + 2.0;
-    // 32 rows share the unpacking of a tile, but their kernel runs with half the warps and a longer set-up: worth it from
-    // about 128 tiles on (192 rows over 190 tiles: 67 us against 78 us with 16 rows per unit; 63 rows over 66 tiles: 26 against 23).
-    plan.nt = rows <= 8 ? 1 : rows <= 16 || tiles < 128.0 ? 2 : 4;
-    plan.row_blocks = (uint32_t)((rows + 8 * plan.nt - 1) / (8 * plan.nt));
+    plan.nt = nt;
+    plan.row_blocks = (uint32_t)((w.rows + 8 * nt - 1) / (8 * nt));
     // Shares that are the same fraction of every pool keep the warps of an SM in the same loop, which the longest code profits
     // from (8192 tokens, 32 rows: 224 us against 243 us); the others are faster with fewer changes of pool (2048 tokens of
     // one sequence, 15 rows: 13 us against 17 us).
-    plan.by_pool = plan.nt == 4;
-    const uint64_t units = pairs * plan.row_blocks;
+    plan.by_pool = nt == 4;
+    best = 1e30;
+    const uint64_t units = w.pairs * plan.row_blocks;
     if (units > 0x7fffffffull) return plan;
-    const int draft_tiles = (tree_nodes + kTileTokens - 1) / kTileTokens;
-    const Residency* fit = device >= 0 && device < 64 ? &g_residency[device] : nullptr;
-    const int per_sm = fit ? std::max(1, fit->ctas[plan.nt][draft_tiles]) : 1;
-    const uint64_t resident = (uint64_t)sm_count * per_sm;
-    const uint64_t max_ctas = std::min<uint64_t>(4 * (uint64_t)sm_count, rows_max_record_rows(sm_count) / (16 * plan.nt));   // of a launch that cuts units
+    const int per_sm = w.fit ? std::max(1, w.fit->ctas[nt][w.draft_tiles]) : 1;
+    const uint64_t resident = (uint64_t)w.sm_count * per_sm;
+    const uint64_t max_ctas = std::min<uint64_t>(4 * (uint64_t)w.sm_count, rows_max_record_rows(w.sm_count) / (16 * nt));   // of a launch that cuts units
     // Up to sixteen CTAs of a unit merge as a cluster, through shared memory, if all of the launch are resident at once: 2048
     // tokens of one sequence in 16 parts take 9.7 us, in 8 parts 11.2 us, and through global records 14.2 us; but 40 clusters of
     // 7 of which some wait for room took 45 us instead of 28 us.  Two large CTAs per SM leave too little room to move up behind
     // an earlier launch when they fill the device (30 clusters of 9: 31 us against 25 us with 8), so with 32 rows an eighth stays free.
     auto cluster_of = [&](uint64_t parts) {
-        const uint64_t most = fit && parts >= 2 && parts <= kRowsMaxCluster ? (uint64_t)fit->clusters[plan.nt][draft_tiles][parts] : 0;
-        return units <= (plan.nt == 4 ? most * 7 / 8 : most) ? (uint32_t)parts : 1u;
+        const uint64_t most = w.fit && parts >= 2 && parts <= kRowsMaxCluster ? (uint64_t)w.fit->clusters[nt][w.draft_tiles][parts] : 0;
+        return units <= (nt == 4 ? most * 7 / 8 : most) ? (uint32_t)parts : 1u;
     };
-    auto cut = [&](uint64_t parts) {                   // every unit into `parts` CTAs
-        if (parts == 1) plan.ctas = (uint32_t)units, plan.ticks = plan.span = 1;
-        else plan.ctas = plan.ticks = (uint32_t)(units * parts), plan.span = (uint32_t)units;
-        plan.cluster = cluster_of(parts);
-    };
-    if (splits > 0) {
-        uint64_t parts = (uint64_t)((splits + kRowsWarps - 1) / kRowsWarps);
-        while (parts > 1 && units * parts > max_ctas) --parts;
-        cut(parts);
-        return plan;
-    }
-    // A model of the launch in us, fitted to 265 shapes (3 to 256 units, 120 to 20000 tokens) in 1 to 16 parts: what it picks is
-    // within 2 % of the best of them on average.  A CTA's set-up, longer the more CTAs share the SM; its warps' tiles, of which
-    // the first ones cost more (their instructions are not there yet); in as many waves as it takes; and the merge of the parts.
-    // CTAs with stretches that do not end at unit borders work on two units one after the other, with a second set-up.
-    struct Model { double set_up, crowded, tile, tile_full, early, early_tiles, merge, part, record, second, second_draft; };
-    static constexpr Model kModels[3] = {{4.7, 3.2, 0.56, 0.58, 0.115, 10.0, 0.4, 0.013, 0.30, 12.0, 4.0},
-                                         {8.2, 1.6, 0.64, 0.80, 0.485, 10.0, 0.0, 0.048, 0.32, 17.0, 6.0},
-                                         {9.2, 0.0, 0.65, 0.77, 0.455, 20.0, 0.0, 0.001, 0.75, 30.0, 14.0}};
-    const Model& m = kModels[plan.nt == 1 ? 0 : plan.nt == 2 ? 1 : 2];
-    auto work = [&](double n, double load) { return m.set_up + m.crowded * load + n * std::max(m.tile, m.tile_full * load) + m.early * std::min(n, m.early_tiles); };
-    double best = 0.0;
-    uint64_t parts = 1;
-    for (uint64_t p = 1; p == 1 || (units * p <= max_ctas && p <= 64); ++p) {
-        const uint64_t ctas = units * p;
+    const LaunchModel& m = kLaunchModels[nt == 1 ? 0 : nt == 2 ? 1 : 2];
+    const double per_cta = m.set_up + m.draft * w.draft_tiles;
+    auto cost_of = [&](uint64_t parts) {
+        const uint64_t ctas = units * parts;
         const double waves = (double)((ctas + resident - 1) / resident);
-        const double load = std::min(1.0, (double)((ctas + sm_count - 1) / sm_count) / (double)per_sm);
-        const double merge = p == 1 ? 0.0 : cluster_of(p) > 1 ? m.merge + m.part * (double)p : m.record * (double)p;
-        const double cost = waves * work(tiles / (double)(p * kRowsWarps), load) + merge;
-        if (p == 1 || cost < best) {
-            best = cost;
-            parts = p;
+        const double load = std::min(1.0, (double)((ctas + w.sm_count - 1) / w.sm_count) / (double)per_sm);
+        const double merge = parts == 1 ? 0.0 : cluster_of(parts) > 1 ? m.merge + m.part * (double)parts : m.record * (double)parts;
+        return waves * (per_cta + m.crowded * load + w.tiles / (double)(parts * kRowsWarps) * std::max(m.tile, m.tile_full * load)) + merge;
+    };
+    uint64_t parts = 1;
+    if (w.splits > 0) {
+        parts = (uint64_t)((w.splits + kRowsWarps - 1) / kRowsWarps);
+        while (parts > 1 && units * parts > max_ctas) --parts;
+        best = cost_of(parts);
+    } else {
+        for (uint64_t p = 1; p == 1 || (units * p <= max_ctas && p <= 64); ++p) {
+            const double cost = cost_of(p);
+            if (cost < best) best = cost, parts = p;
         }
     }
-    cut(parts);
-    if (2 * units > resident && units < 4 * resident && resident <= max_ctas && units < rows_max_units(sm_count)) {
-        const double cost = work((double)units * tiles / (double)(resident * kRowsWarps), 1.0) + m.second + m.second_draft * (double)draft_tiles;
-        if (cost < best) plan.ctas = plan.ticks = (uint32_t)resident, plan.span = (uint32_t)units, plan.cluster = 1;
+    if (parts == 1) plan.ctas = (uint32_t)units, plan.ticks = plan.span = 1;
+    else plan.ctas = plan.ticks = (uint32_t)(units * parts), plan.span = (uint32_t)units;
+    plan.cluster = cluster_of(parts);
+    if (w.splits == 0 && 2 * units > resident && units < 4 * resident && resident <= max_ctas && units < rows_max_units(w.sm_count)) {
+        const double cost = per_cta + m.crowded + (double)units * w.tiles / (double)(resident * kRowsWarps) * m.tile_full + m.second + m.second_draft * w.draft_tiles;
+        if (cost < best) best = cost, plan.ctas = plan.ticks = (uint32_t)resident, plan.span = (uint32_t)units, plan.cluster = 1;
     }
     return plan;
+}
+
+}  // namespace
+
+RowsPlan rows_plan(int device, int sm_count, uint64_t pairs, int rows, int tree_nodes, int visible_tokens, int splits) {
+    Shape w;
+    w.fit = device >= 0 && device < 64 ? &g_residency[device] : nullptr;
+    w.sm_count = sm_count;
+    w.draft_tiles = (tree_nodes + kTileTokens - 1) / kTileTokens;
+    w.splits = splits;
+    w.pairs = pairs;
+    w.rows = rows;
+    w.tiles = (double)visible_tokens / kTileTokens + 2.0;
+    double cost, cost4;
+    const RowsPlan plan = plan_blocks(w, rows <= 8 ? 1 : 2, cost);
+    if (rows <= 16) return plan;
+    // 32 rows share the unpacking of a tile, but their kernel runs with half the warps and a longer set-up: faster where 16 rows
+    // per unit need more waves (256 pairs of 20 rows over 1500 tokens: 37 us against 75 us; 3 pairs of 60 rows over 3000: 19
+    // against 12).
+    const RowsPlan plan4 = plan_blocks(w, 4, cost4);
+    return cost4 < cost ? plan4 : plan;
 }
 
 void rows_launch(const RowsParams& p, const RowsPlan& plan, bool tree, cudaStream_t st) {
