@@ -28,8 +28,14 @@
 //   sum p (s c + z) = sum w (c - mid) + sum p (z + mid s),   mid = -z / s, inside [0, 2^bits - 1], per token
 // with the same rounded w in both terms of (c - mid).  mid is the code of the value zero, so the rounding of w acts on
 // the value and not on its distance from the row's minimum, which is far larger for the ordinary channels of a row with
-// one large one (values have such): outputs over 500 to 8000 mixed tokens are off by 2.8e-4 to 3.1e-4 (relative, whole
-// tensors), of which the rounding to fp16 alone makes 2.1e-4.  The sums of p, of p (z + mid s) and of mid w stay in fp32.
+// one large one (values have such).  The sums of p, of p (z + mid s) and of mid w stay in fp32.
+//
+// The matrix instruction truncates its sums, towards zero and below the largest possible product of its operands, which for
+// subnormal codes is far above the real ones.  Sums of codes 0 .. 2^bits - 1 all lose in the same direction, and next to outputs
+// that average out over many tokens that is no small loss: 8000 tokens of 2 bits were off by 6.5e-4 (relative, whole tensors),
+// 60000 mixed ones in one CTA by 1.1e-3.  So the codes enter as c - (2^bits - 1) / 2 (rounded down for even slots and up for odd
+// ones, which mid takes back): 3.0e-4 at any length, of which the rounding of the outputs to fp16 makes 2.1e-4.  The 16
+// subtractions per tile take 0 to 5 % of the time (32768 tokens, 16 rows: 399 us against 379 us).
 //
 // Softmax reference.  p = 2^(y - m), m kept per row and warp.  m is no running maximum: it is moved only when some w
 // overflows fp16 (one vote per tile decides), and then to where the row's largest w of the tile is 2^4.  So logits may
@@ -152,6 +158,10 @@ __device__ __forceinline__ float2 unpack_half2(uint32_t v) { return __half22floa
 __device__ __forceinline__ uint32_t max_half2(uint32_t a, uint32_t b) {
     const __half2 m = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
     return *reinterpret_cast<const uint32_t*>(&m);
+}
+__device__ __forceinline__ uint32_t sub_half2(uint32_t a, uint32_t b) {
+    const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&d);
 }
 __device__ __forceinline__ float fast_rcp(float x) {
     float y;
@@ -332,6 +342,8 @@ __device__ __forceinline__ uint32_t query_word(const uint4& v, int k) { return k
 template <int CLS>
 struct RowsQuant {
     static constexpr int BITS = pool_bits(CLS);
+    // The middle of the codes for even slots (low half) and odd ones: (2^BITS - 1) / 2 on average.
+    static constexpr uint32_t kMiddle = ((1u << (BITS - 1)) - 1u) | ((1u << (BITS - 1)) << 16);
     static constexpr int NW = 2 << CLS;                // words per lane of one tensor: 2, 4, 8
     static constexpr uint32_t MASK = CLS == 0 ? 0x00030003u : CLS == 1 ? 0x000f000fu : 0x00ff00ffu;
 
@@ -379,6 +391,7 @@ struct RowsQuant {
             t.sv[s] = fmaxf(vm.x, 5.9604645e-8f);
             t.mid[s] = fminf(fmaxf(-vm.y * fast_rcp(t.sv[s]), 0.f), (float)((1 << BITS) - 1));
             t.zv[s] = fmaf(t.sv[s], t.mid[s], vm.y);
+            t.mid[s] -= (g & 1) ? (float)(kMiddle >> 16) : (float)(kMiddle & 0xffffu);
         }
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
@@ -408,8 +421,9 @@ struct RowsQuant {
 #pragma unroll
             for (int f = 0; f < PER; ++f) {
                 const uint32_t prefix = ((1u << (BITS * (f + 1))) - 1u) * 0x00010001u;
+                const uint32_t ones = ((1u << (BITS * (f + 1))) - 1u) / ((1u << BITS) - 1u);   // 1 + 2^BITS + ..., a one per field
 #pragma unroll
-                for (int k = 0; k < 4; ++k) a[byte * PER + f][k] = f + 1 == PER ? x[k] : x[k] & prefix;
+                for (int k = 0; k < 4; ++k) a[byte * PER + f][k] = sub_half2(f + 1 == PER ? x[k] : x[k] & prefix, kMiddle * ones);
             }
         }
     }

@@ -50,6 +50,7 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_tree(const VerifyPara
     __shared__ double s_sums[2][kVerifyMaxCluster * kVerifyWarps];         // sums of all warps of the cluster, in vocabulary order; two passes alternate
     __shared__ double s_r[32 * kVerifyKeep];                               // the final draw's part of the row
 
+    cluster.barrier_arrive();                          // (before another CTA's memory is written, all of them have to be there)
     pdl_launch_dependents();
     pdl_wait();                                        // the kernel ahead in the stream may be the one that wrote the probabilities
 
@@ -170,6 +171,7 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_tree(const VerifyPara
 #pragma unroll 1
         for (int v = lo + lane + 32 * kVerifyKeep; v < hi; v += 32) sum += far_entry(v);
         sum = warp_sum_f64(sum);
+        if (pass == 0) cluster.barrier_wait();
         ++pass;
         if (lane < ctas) *cluster.map_shared_rank(&s_sums[pass & 1][rank * kVerifyWarps + warp], lane) = sum;
         cluster.sync();

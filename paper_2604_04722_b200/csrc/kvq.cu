@@ -221,6 +221,7 @@ void free_all(kvq_ctx* c) {
 }
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 // The device's address for a page-locked host buffer, or nullptr if `p` is not one (pageable memory, or an
 // address the kernels' 16-byte accesses could not use).
@@ -1124,7 +1125,8 @@ int kvq_attend_tree(kvq_ctx* c, int layer, const void* Q, const void* K, const v
     if (check_layer(c, layer) != KVQ_OK || n_nodes < 0 || n_nodes > KVQ_MAX_TREE_NODES || window < 0 || sinks < 0) return KVQ_ERR_ARG;
     if (c->groups != 1) return KVQ_ERR_ARG;            // the kernel reads the fragment layout of one scale group per row
     if (n_nodes == 0) return KVQ_OK;
-    if (!Q || !K || !V || !parents || !O || !aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O)) return KVQ_ERR_ARG;
+    if (!Q || !K || !V || !parents || !O || !aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned4(parents))
+        return KVQ_ERR_ARG;
     return rows_impl(c, layer, Q, O, K, V, bits_opt, parents, n_nodes, window, sinks, static_cast<cudaStream_t>(stream));
 }
 
@@ -1143,6 +1145,9 @@ int kvq_verify_tree(const float* target, const float* draft_opt, const int32_t* 
     if (batch == 0) return KVQ_OK;
     if (!target || !u_next || !n_accepted || !next_token || batch > (1 << 24)) return KVQ_ERR_ARG;
     if (n_nodes > 0 && (!tokens || !parents || !u_accept || !path)) return KVQ_ERR_ARG;
+    for (const void* ptr : {(const void*)target, (const void*)draft_opt, (const void*)u_next, (const void*)n_accepted, (const void*)next_token})
+        if (!aligned4(ptr)) return KVQ_ERR_ARG;
+    if (n_nodes > 0 && !(aligned4(tokens) && aligned4(parents) && aligned4(u_accept) && aligned4(path))) return KVQ_ERR_ARG;
     int device = 0, sm_count = 0;
     if (cudaGetDevice(&device) != cudaSuccess ||
         cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, device) != cudaSuccess)

@@ -2,6 +2,7 @@
 #include "kvq_rows.h"
 
 #include <algorithm>
+#include <atomic>
 
 #include "k_rows.cuh"
 #include "k_verify.cuh"
@@ -17,8 +18,9 @@ constexpr int kMaxDraftTiles = kMaxTreeNodes / kTileTokens;
 struct Residency {
     int ctas[5][kMaxDraftTiles + 1] = {};
     int clusters[5][kMaxDraftTiles + 1][kRowsMaxCluster + 1] = {};
+    std::atomic<bool> known{false};
 };
-Residency g_residency[64];             // per device; written with the same values by every set-up
+Residency g_residency[64];             // per device; asked for once
 
 // A launch of `ctas` CTAs in clusters of `cluster`.
 struct Launch {
@@ -44,7 +46,7 @@ cudaError_t set_up_kernel(Residency& r) {
     const int most = TREE ? kMaxDraftTiles : 0;
     cudaError_t e = cudaFuncSetAttribute(k_attend_rows<NT, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)rows_smem_limit<NT>(most));
     if (e == cudaSuccess) e = cudaFuncSetAttribute(k_attend_rows<NT, TREE>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    for (int tiles = TREE ? 1 : 0; e == cudaSuccess && tiles <= most; ++tiles) {
+    for (int tiles = TREE ? 1 : 0; e == cudaSuccess && !r.known && tiles <= most; ++tiles) {
         e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&r.ctas[NT][tiles], k_attend_rows<NT, TREE>, kRowsThreads, rows_smem_bytes<NT>(tiles, 1));
         for (uint32_t c = 2; e == cudaSuccess && c <= kRowsMaxCluster; ++c) {
             Launch l(c, c, rows_smem_bytes<NT>(tiles, c), nullptr);
@@ -71,6 +73,7 @@ cudaError_t rows_setup(int device) {
     if (e == cudaSuccess) e = set_up_kernel<1, false>(r);
     if (e == cudaSuccess) e = set_up_kernel<2, false>(r);
     if (e == cudaSuccess) e = set_up_kernel<4, false>(r);
+    if (e == cudaSuccess) r.known = true;
     return e;
 }
 

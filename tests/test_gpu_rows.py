@@ -317,6 +317,19 @@ def test_long_ragged_batch_over_the_whole_axis(gu, oracle):
         c.check(c.run_window(Q1, 2000, 4), Q1, 2000, 4)
 
 
+def test_long_caches_keep_the_precision_of_short_ones(gu, oracle):
+    """60000 tokens in one CTA.  The roundings of the weights to fp16 are independent and each is uniform within 2^-11 of its
+    value at most, so next to the outputs, which are the same sums of values of random sign, they are off by 2^-11 / sqrt(3) in
+    the mean square; the rounding of the output is as much again at most: together 4.0e-4, whatever the length."""
+    from paper_2604_04722_b200 import binding as kq
+    with Case(gu, oracle, 28, 1, 3, 1, [60000]) as c:
+        kq.kvq_set_splits(c.g.ctx, 4)
+        Q, t = c.queries(4), c.tree(4)
+        got = c.run_tree(Q, t).astype(np.float64)
+        want, _ = rr.attention(oracle, c.cache, c.lens, Q, 3, tree=t)
+        assert np.linalg.norm(got - want) <= 2.0 ** -11 * (2 / 3) ** .5 * np.linalg.norm(want)
+
+
 def test_stale_blocks_of_an_earlier_cache_stay_out(gu, oracle):
     """Blocks that held huge fp16 rows are handed out again after a reset."""
     import torch
@@ -486,6 +499,9 @@ def test_refusals(gu, oracle):
             with pytest.raises(kq.KvqError) as e:
                 tree(**bad)
             assert e.value.code == kq.KVQ_ERR_ARG, bad
+        with pytest.raises(kq.KvqError) as e:          # int32 at an odd address
+            tree(par=torch.zeros(20, dtype=torch.int8, device=gu.DEV)[1:17])
+        assert e.value.code == kq.KVQ_ERR_ARG
         O.fill_(3.0)
         tree(n=0, Q=None)                              # nothing to do
         assert torch.all(O == 3.0)

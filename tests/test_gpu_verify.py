@@ -68,6 +68,15 @@ def test_verification(gu, fixed, V, B, T):
     _check(x, _run(gu, x, fixed), fixed)
 
 
+@pytest.mark.parametrize("fixed", [False, True])
+@pytest.mark.parametrize("B,V", [(1, 65536), (2, 65537), (1, 150001), (40, 20003)])
+def test_vocabularies_that_no_lane_keeps_whole(gu, B, V, fixed):
+    """More entries than the registers of the sequence's CTAs hold (65536 at the full width, 8192 at a width of one): the rest of a
+    row is read again for every sum."""
+    x = _inputs(V, B, 6, V)
+    _check(x, _run(gu, x, fixed), fixed)
+
+
 @pytest.mark.parametrize("B", [40, 80, 200, 700])
 def test_many_sequences(gu, B):
     """Every cluster width that the launch picks."""

@@ -94,3 +94,18 @@ def test_refusals_without_a_device():
                 dict(parents=None), dict(u=None), dict(u_next=None), dict(acc=None), dict(path=None), dict(nxt=None)):
         assert verify(**bad) == binding.KVQ_ERR_ARG, bad
     assert verify(batch=0, target=None) == binding.KVQ_OK
+
+
+def test_odd_addresses_and_sizes_are_refused_without_a_device():
+    from paper_2604_04722_b200 import build, binding
+    build.build()
+    L = binding.lib()
+    names = ("target", "draft", "tokens", "parents", "u", "u_next", "acc", "path", "nxt")
+
+    def verify(vocab=8, **odd):
+        p = {**dict.fromkeys(names, 16), **odd}
+        return L.kvq_verify_tree(p["target"], p["draft"], p["tokens"], p["parents"], 1, 2, vocab, p["u"], p["u_next"], p["acc"],
+                                 p["path"], p["nxt"], None)
+    for name in names:
+        assert verify(**{name: 18}) == binding.KVQ_ERR_ARG, name
+    assert verify(vocab=2 ** 30 + 1) == binding.KVQ_ERR_ARG
