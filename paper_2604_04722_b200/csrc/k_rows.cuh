@@ -23,18 +23,20 @@
 // logit
 //   y = log2(e)/8 * (s_k * sum_i q_i c_i + z_k * sum_i q_i)
 // carries fp32 accumulation error only.  V codes are cut out the same way, but as prefixes of their byte (c0, c0 + 4 c1,
-// ...: the last needs no AND at all), which the accumulators undo when the pool is left.  The weight w = p * s_v is rounded once to fp16 (by at most 2^-11 of its value: the rounding
-// that the fp16 operand forces).  What that does is made to act on centred codes:
+// ...), which the accumulators undo when the pool is left.  The weight w = p * s_v is rounded once to fp16 (by at most 2^-11
+// of its value: the rounding that the fp16 operand forces).  What that does is made to act on centred codes:
 //   sum p (s c + z) = sum w (c - mid) + sum p (z + mid s),   mid = -z / s, inside [0, 2^bits - 1], per token
 // with the same rounded w in both terms of (c - mid).  mid is the code of the value zero, so the rounding of w acts on
 // the value and not on its distance from the row's minimum, which is far larger for the ordinary channels of a row with
-// one large one (values have such).  The sums of p, of p (z + mid s) and of mid w stay in fp32.
+// one large one (values have such).  The sums of p, of p (z + mid s) and of mid w stay in fp32.  With the middle of the codes
+// in the place of mid the kernel is 7 % faster and off by 3.0e-4 to 3.5e-4 instead of 2.4e-4 to 2.6e-4 (relative, whole tensors
+// of outputs over 2000 to 8000 tokens; the rounding of exact outputs to fp16 is 2.1e-4 of that).
 //
 // The matrix instruction truncates its sums, towards zero and below the largest possible product of its operands, which for
 // subnormal codes is far above the real ones.  Sums of codes 0 .. 2^bits - 1 all lose in the same direction, and next to outputs
 // that average out over many tokens that is no small loss: 8000 tokens of 2 bits were off by 6.5e-4 (relative, whole tensors),
 // 60000 mixed ones in one CTA by 1.1e-3.  So the codes enter as c - (2^bits - 1) / 2 (rounded down for even slots and up for odd
-// ones, which mid takes back): 3.0e-4 at any length, of which the rounding of the outputs to fp16 makes 2.1e-4.  The 16
+// ones, which mid takes back): 3.0e-4 at any length.  The 16
 // subtractions per tile take 0 to 5 % of the time (32768 tokens, 16 rows: 399 us against 379 us).
 //
 // Softmax reference.  p = 2^(y - m), m kept per row and warp.  m is no running maximum: it is moved only when some w
@@ -484,8 +486,7 @@ __device__ __forceinline__ void v_products(RowsState<NT>& st, const uint32_t (&a
 }
 
 // Up to n tiles in a row that every row sees whole; stops in front of one with a weight that overflows.  Returns the tiles
-// done.  (Two tiles at a time, for more independent instructions, made the loops of the classes outgrow the innermost
-// instruction cache: 20 % slower on mixed pools.)
+// done.  
 template <int NT, class C>
 __device__ __forceinline__ uint32_t whole_tiles(const uint8_t* rec, uint32_t n, uint32_t step, int lane, const RowsQuery<NT>& qf,
                                                 float kfactor, RowsState<NT>& st) {
@@ -591,6 +592,14 @@ __device__ __forceinline__ uint32_t rows_record(const RowsParams& P, uint32_t j,
     return 2u * j + (j * P.span >= unit * P.ticks ? 0u : 1u);      // (it starts inside the unit, or in front of it)
 }
 
+// What bounds it.  Long caches: the issue of its instructions, about 240 per tile with 16 rows, in dependent chains that four
+// warps per scheduler do not hide (8192 tokens, 16 rows: a scheduler issues in 53 % of its active cycles, ALU 36 %, matrix pipe
+// 28 %, exponentials 23 %).  16 sequences x 32 heads x 32768 tokens, 1.26 GB of packed rows: 16 rows 399 us (3.2 TB/s of them,
+// 0.48 of the copy bandwidth), one row over a window of 8192 86 us (3.7 TB/s); 32 rows over 8192 tokens, 0.42 GB, 232 us, 148
+// Tflop/s.  Pools of 16 bits alone are bound by memory.  Short caches: the chain of round trips (fills, index, block table,
+// rows, merge) and instructions that are not in the caches yet, 6 to 10 us.  Two tiles at a time, for more independent
+// instructions, outgrew the innermost instruction cache (20 % slower on mixed pools).
+//
 // grid = CTAs of the plan, block = kRowsThreads, dynamic smem = rows_smem_bytes<NT>(draft tiles).
 // NT: blocks of eight rows per unit.  TREE: rows belong to drafted nodes (otherwise nodes == 1 and the row is the last
 // cached token's).
