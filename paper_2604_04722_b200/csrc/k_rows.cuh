@@ -544,8 +544,8 @@ __device__ __forceinline__ bool finite_half8(uint4 v) {
     const auto carry = [](uint32_t w) { return (w & 0x7fff7fffu) + 0x04000400u; };
     return !((carry(v.x) | carry(v.y) | carry(v.z) | carry(v.w)) & 0x80008000u);
 }
-// One drafted row, eight channels per lane of an eight-lane group, as the store would give it back (the row quantizer of
-// Eq. 24, then code * scale + zero-point), rounded to fp16.
+// One drafted row of finite values, eight channels per lane of an eight-lane group, as the store would give it back (the row
+// quantizer of Eq. 24, then code * scale + zero-point), rounded to fp16.
 __device__ __forceinline__ uint4 draft_row_as_stored(uint4 raw, int c) {
     float x[8];
     const uint32_t rw[4] = {raw.x, raw.y, raw.z, raw.w};
@@ -908,12 +908,18 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
                 }
             }
             uint4 row = draft_row_as_stored(raw, c);
-            // A value row that is not finite is left out of the products, where a weight of zero would not silence it for the
-            // nodes that do not see it; those that see it become NaN at the end.
+            // What the row quantizer makes of a row that is not finite is asked of the row as it came: its minimum and maximum
+            // skip NaN, and its clamp makes numbers of the others.  Such a row has no finite value at 2, 4 or 8 bits (its scale
+            // or its zero-point is not finite), so its key is NaN; at 16 it stays what it is.  A value row is left out of the products,
+            // where a weight of zero would not silence it for the nodes that do not see it; those that see it become
+            // NaN at the end.
             const uint32_t lanes = 0xffu << (lane & 24);
-            if (value && (__ballot_sync(0xffffffffu, !finite_half8(row)) & lanes)) {
-                row = make_uint4(0u, 0u, 0u, 0u);
-                if (piece8 == 0 && node < P.nodes) atomicOr(&sc.poison, 1ull << node);
+            if (__ballot_sync(0xffffffffu, !finite_half8(raw)) & lanes) {
+                if (c != 3) row = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
+                if (value) {
+                    row = make_uint4(0u, 0u, 0u, 0u);
+                    if (piece8 == 0 && node < P.nodes) atomicOr(&sc.poison, 1ull << node);
+                }
             }
             *reinterpret_cast<uint4*>(draft + (node / kTileTokens) * kDraftTileBytes + (value ? kDraftTileBytes / 2 : 0) +
                                       (piece8 * kTileTokens + node % kTileTokens) * 16) = row;

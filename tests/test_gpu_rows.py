@@ -520,3 +520,51 @@ def test_refusals(gu, oracle):
                 with pytest.raises(kq.KvqError) as e:
                     call()
                 assert e.value.code == kq.KVQ_ERR_ARG
+
+
+@pytest.mark.parametrize("b", [2, 4, 8])
+@pytest.mark.parametrize("where", ["K", "V"])
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
+def test_one_bad_channel_of_a_drafted_row_that_is_stored_quantized(gu, oracle, b, where, bad):
+    """Such a row has no finite values (its scale or its zero-point is not finite): those who see it become NaN, whatever the
+    width, and nobody else does."""
+    with Case(gu, oracle, 30 + b, 2, 6, 2, [70, 33]) as c:
+        T, hit = 22, (3, 17)
+        Q, (K, V, bits, par) = c.queries(T), c.tree(T)
+        bits[:, list(hit)] = b
+        want, bound = rr.attention(oracle, c.cache, c.lens, Q, 3, tree=(K.copy(), V.copy(), bits, par))
+        (K if where == "K" else V)[:, list(hit), :, 5] = bad
+        got = c.run_tree(Q, (K, V, bits, par))
+        for s in range(2):
+            for i, ch in enumerate(rr.chains(par[s])):
+                if set(ch) & set(hit):
+                    assert np.all(np.isnan(got[s, i])), (s, i)
+                else:
+                    assert np.all(np.abs(got[s, i].astype(np.float64) - want[s, i]) <= bound[s, i]), (s, i)
+
+
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
+@pytest.mark.parametrize("with_bits", [False, True])
+def test_one_bad_channel_of_a_drafted_key_that_stays_fp16(gu, oracle, bad, with_bits):
+    """The softmax as it stands: a logit of minus infinity has the weight zero, any other that is not finite makes NaN."""
+    with Case(gu, oracle, 36, 1, 6, 2, [70]) as c:
+        T, hit = 22, 3
+        Q, (K, V, bits, par) = c.queries(T), c.tree(T, with_bits=with_bits)
+        if with_bits:
+            bits[0, hit] = 16
+        want, bound = rr.attention(oracle, c.cache, c.lens, Q, 3, tree=(K.copy(), V.copy(), bits, par))
+        past = par.copy()                              # the same tree with that node out of everybody's chain
+        past[0, par[0] == hit] = par[0, hit]
+        without, bound_without = rr.attention(oracle, c.cache, c.lens, Q, 3, tree=(K.copy(), V.copy(), bits, past))
+        K[0, hit, :, 5] = bad
+        got = c.run_tree(Q, (K, V, bits, par))
+        zero = Q[0, :, :, 5].astype(np.float64) * bad == -np.inf
+        assert np.isnan(bad) or (np.any(zero) and not np.all(zero))
+        for i, ch in enumerate(rr.chains(par[0])):
+            for h in range(6):
+                if hit not in ch:
+                    assert np.all(np.abs(got[0, i, h].astype(np.float64) - want[0, i, h]) <= bound[0, i, h])
+                elif not zero[i, h]:
+                    assert np.all(np.isnan(got[0, i, h])), (i, h)
+                elif i != hit:
+                    assert np.all(np.abs(got[0, i, h].astype(np.float64) - without[0, i, h]) <= bound_without[0, i, h]), (i, h)
