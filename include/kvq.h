@@ -284,12 +284,12 @@ int kvq_attend_last(kvq_ctx* ctx, int layer, const void* Q, void* O, int n_queri
  *   bits_opt dev uint8 [batch][n_nodes], values in {2,4,8,16}, or NULL.  The rows take part in the attention as they
  *          would be stored at that bit-width (Eq. 24, then code * scale + zero-point, rounded once to fp16), so that a
  *          chain of finite nodes gives what appending them and kvq_attend_last give; NULL: as fp16 rows.  Any other value
- *          counts as 16 and sets KVQ_FLAG_BAD_BITS.
+ *          counts as 16 and, for a node in use, sets KVQ_FLAG_BAD_BITS.
  *   window, sinks  window == 0: a node sees every cached token, its ancestors and itself.  window > 0: of those, the
  *          ones whose position is less than `window` before its own, and the tokens at positions < sinks.
  * The cache is not changed: append the accepted rows afterwards (kvq_append_ragged).  n_nodes == 0 is a no-op.  One
  * launch; one that was captured into a graph is captured again after an append to the layer.  Q, K, V, O 16-byte
- * aligned; O may not overlap the inputs.  The rows of a node that is not in use may hold anything, and so may cached
+ * aligned; O may not overlap the inputs.  The rows and the bit-width of a node that is not in use may hold anything, and so may cached
  * tokens that no row sees.  A drafted value that is not finite makes NaN of the rows that see it, at every bit-width (but
  * a key that is kept as fp16 and gives a row the logit minus infinity has the weight zero there).  So does one that a
  * cached row holds as it is stored, and that also in rows of the same sequence whose window has moved past it while

@@ -216,6 +216,7 @@ struct RowsScratch {
     unsigned long long step_bits[kNumPools];           // class c among the 64 positions after the first window start
     unsigned long long used;                           // nodes that are used
     unsigned long long poison;                         // drafted values that are not finite
+    unsigned long long odd_bits;                       // nodes with a bit-width outside {2,4,8,16}
     alignas(16) RowsChunks plan[kRowsWarps];
     uint2 chunk[kRowsWarps][kRowsStages];              // what a stage holds: z, and w >> 16, of its chunk
     int in_sinks[kNumPools], from[kNumPools], full[kNumPools];     // tiles that every row sees whole: [0, in_sinks), [from, full)
@@ -776,7 +777,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
     }
     qmax = warp_max(qmax);
     if (lane == 0) sc.wmax[warp] = qmax;
-    if (has_draft && tid == 0) sc.poison = 0ull;
+    if (has_draft && tid == 0) sc.poison = sc.odd_bits = 0ull;
     __syncthreads();
 
     // ---- the copies: chunks of the share in order; a chunk stays inside one 64 KB block and fits a stage
@@ -901,8 +902,8 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
                 raw = *reinterpret_cast<const uint4*>((value ? P.V : P.K) + (((size_t)b * P.nodes + node) * S.kv_heads + h) * kHeadDim + piece8 * 8);
                 if (P.bits) {
                     c = bits_to_class(P.bits[(size_t)b * P.nodes + node]);
-                    if (c < 0) {                       // as in an append: kept as fp16, and flagged
-                        atomicOr(S.flags, 1u);
+                    if (c < 0) {                       // as in an append: kept as fp16, and flagged (if the node is in use, see below)
+                        if (piece8 == 0) atomicOr(&sc.odd_bits, 1ull << node);
                         c = 3;
                     }
                 }
@@ -954,6 +955,7 @@ __global__ void __launch_bounds__(kRowsThreads, rows_ctas_per_sm(NT)) k_attend_r
         }
     }
     __syncthreads();
+    if (has_draft && tid == 0 && (sc.odd_bits & sc.used)) atomicOr(S.flags, 1u);
     // ---- first window slot of every row, per class
     if (P.window > 0) {
         for (int k = tid; k < kNumPools * ROWS; k += kRowsThreads) {

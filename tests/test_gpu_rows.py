@@ -568,3 +568,26 @@ def test_one_bad_channel_of_a_drafted_key_that_stays_fp16(gu, oracle, bad, with_
                     assert np.all(np.isnan(got[0, i, h])), (i, h)
                 elif i != hit:
                     assert np.all(np.abs(got[0, i, h].astype(np.float64) - without[0, i, h]) <= bound_without[0, i, h]), (i, h)
+
+
+@pytest.mark.parametrize("junk", [0, 3, 255])
+def test_bit_widths_of_unused_nodes_may_be_anything(gu, oracle, junk):
+    """A padded tree is no error: no flag (run_tree asserts that), no change.  A node in use with the same width is one."""
+    import torch
+    from paper_2604_04722_b200 import binding as kq
+    with Case(gu, oracle, 31, 2, 6, 2, [50, 0]) as c:
+        Q, (K, V, bits, par) = c.queries(40), c.tree(40, "ragged")
+        par[0, 4], par[1, 7] = 4, 100                  # not an earlier node, and their descendants with them
+        want = c.run_tree(Q, (K, V, bits, par))
+        unused = np.array([[ch is None for ch in rr.chains(par[b])] for b in range(2)])
+        assert np.any(unused[:, :32]) and np.any(unused[:, 32:])
+        padded = np.where(unused, np.uint8(junk), bits)
+        assert np.array_equal(c.run_tree(Q, (K, V, padded, par)), want)
+        for i in (0, 33):                              # one in use in each half of the nodes
+            spoiled = padded.copy()
+            par[1, i] = -1
+            spoiled[1, i] = junk
+            O = torch.zeros(Q.shape, dtype=torch.float16, device=gu.DEV)
+            kq.kvq_attend_tree(c.g.ctx, 0, gu.dev(Q.view(np.uint16)), gu.dev(K.view(np.uint16)), gu.dev(V.view(np.uint16)),
+                               gu.dev(spoiled), gu.dev(par), 40, O)
+            assert kq.kvq_device_status(c.g.ctx) == 1  # KVQ_FLAG_BAD_BITS
