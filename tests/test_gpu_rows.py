@@ -591,3 +591,21 @@ def test_bit_widths_of_unused_nodes_may_be_anything(gu, oracle, junk):
             kq.kvq_attend_tree(c.g.ctx, 0, gu.dev(Q.view(np.uint16)), gu.dev(K.view(np.uint16)), gu.dev(V.view(np.uint16)),
                                gu.dev(spoiled), gu.dev(par), 40, O)
             assert kq.kvq_device_status(c.g.ctx) == 1  # KVQ_FLAG_BAD_BITS
+
+
+@pytest.mark.parametrize("junk", [65504.0, np.inf, np.nan])
+@pytest.mark.parametrize("window", [0, 50])
+def test_large_queries_of_unused_nodes_cost_the_others_no_bits(gu, oracle, junk, window):
+    """Small queries over large keys, next to unused rows of the largest values: the same bits as with zeros there."""
+    with Case(gu, oracle, 32, 2, 6, 2, [90, 75], spread=2.0 ** 10) as c:
+        Q, (K, V, bits, par) = c.queries(13), c.tree(13, "ragged")
+        par[0, 2] = 2                                  # and its descendants
+        Q = (Q.astype(np.float32) * 2.0 ** -10).astype(np.float16)
+        unused = np.array([[ch is None for ch in rr.chains(par[b])] for b in range(2)])
+        Q[unused] = 0
+        want = c.run_tree(Q, (K, V, bits, par), window)
+        c.check(want, Q, window, tree=(K, V, bits, par))
+        Q[unused] = np.float16(junk)
+        got = c.run_tree(Q, (K, V, bits, par), window)
+        assert np.array_equal(got, want)
+        assert np.all(got[unused] == 0)
