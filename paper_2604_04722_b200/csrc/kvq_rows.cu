@@ -2,10 +2,10 @@
 #include "kvq_rows.h"
 
 #include <algorithm>
-#include <atomic>
 
 #include "k_rows.cuh"
 #include "k_verify.cuh"
+#include "once_per_device.h"
 
 namespace kvq {
 
@@ -18,9 +18,8 @@ constexpr int kMaxDraftTiles = kMaxTreeNodes / kTileTokens;
 struct Residency {
     int ctas[5][kMaxDraftTiles + 1] = {};
     int clusters[5][kMaxDraftTiles + 1][kRowsMaxCluster + 1] = {};
-    std::atomic<bool> known{false};
 };
-Residency g_residency[64];             // per device; asked for once
+OncePerDevice<Residency> g_residency;
 
 // A launch of `ctas` CTAs in clusters of `cluster`.
 struct Launch {
@@ -42,11 +41,16 @@ struct Launch {
 };
 
 template <int NT, bool TREE>
-cudaError_t set_up_kernel(Residency& r) {
-    const int most = TREE ? kMaxDraftTiles : 0;
-    cudaError_t e = cudaFuncSetAttribute(k_attend_rows<NT, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)rows_smem_limit<NT>(most));
+cudaError_t set_limits() {
+    cudaError_t e = cudaFuncSetAttribute(k_attend_rows<NT, TREE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)rows_smem_limit<NT>(TREE ? kMaxDraftTiles : 0));
     if (e == cudaSuccess) e = cudaFuncSetAttribute(k_attend_rows<NT, TREE>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    for (int tiles = TREE ? 1 : 0; e == cudaSuccess && !r.known && tiles <= most; ++tiles) {
+    return e;
+}
+
+template <int NT, bool TREE>
+cudaError_t ask_residency(Residency& r) {
+    cudaError_t e = cudaSuccess;
+    for (int tiles = TREE ? 1 : 0; e == cudaSuccess && tiles <= (TREE ? kMaxDraftTiles : 0); ++tiles) {
         e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&r.ctas[NT][tiles], k_attend_rows<NT, TREE>, kRowsThreads, rows_smem_bytes<NT>(tiles, 1));
         for (uint32_t c = 2; e == cudaSuccess && c <= kRowsMaxCluster; ++c) {
             Launch l(c, c, rows_smem_bytes<NT>(tiles, c), nullptr);
@@ -65,16 +69,17 @@ void launch(const RowsParams& p, uint64_t ctas, cudaStream_t st) {
 }  // namespace
 
 cudaError_t rows_setup(int device) {
-    Residency other;
-    Residency& r = device >= 0 && device < 64 ? g_residency[device] : other;
-    cudaError_t e = set_up_kernel<1, true>(r);
-    if (e == cudaSuccess) e = set_up_kernel<2, true>(r);
-    if (e == cudaSuccess) e = set_up_kernel<4, true>(r);
-    if (e == cudaSuccess) e = set_up_kernel<1, false>(r);
-    if (e == cudaSuccess) e = set_up_kernel<2, false>(r);
-    if (e == cudaSuccess) e = set_up_kernel<4, false>(r);
-    if (e == cudaSuccess) r.known = true;
-    return e;
+    cudaError_t e = cudaSuccess;
+    for (cudaError_t (*set)() : {set_limits<1, true>, set_limits<2, true>, set_limits<4, true>, set_limits<1, false>, set_limits<2, false>, set_limits<4, false>})
+        if (e == cudaSuccess) e = set();
+    if (e != cudaSuccess) return e;
+    return g_residency.make(device, [](Residency& r) {
+        cudaError_t err = cudaSuccess;
+        for (cudaError_t (*ask)(Residency&) : {ask_residency<1, true>, ask_residency<2, true>, ask_residency<4, true>, ask_residency<1, false>,
+                                               ask_residency<2, false>, ask_residency<4, false>})
+            if (err == cudaSuccess) err = ask(r);
+        return err;
+    });
 }
 
 namespace {
@@ -157,7 +162,7 @@ RowsPlan plan_blocks(const Shape& w, int nt, double& best) {
 
 RowsPlan rows_plan(int device, int sm_count, uint64_t pairs, int rows, int tree_nodes, int visible_tokens, int splits) {
     Shape w;
-    w.fit = device >= 0 && device < 64 ? &g_residency[device] : nullptr;
+    w.fit = g_residency.of(device);
     w.sm_count = sm_count;
     w.draft_tiles = (tree_nodes + kTileTokens - 1) / kTileTokens;
     w.splits = splits;
