@@ -67,7 +67,7 @@ struct kvq_ctx {
     float* part_s2 = nullptr;            //                [units][partial slots] sum of squared weights (kvq_decode_attn_var)
     float* unit_var = nullptr;           //                [units] variance of a unit's attention weights
     uint32_t* vis = nullptr;             // kvq_attend_last: visible pool fills [batch][query rows of a launch][4]
-    float* rows_o = nullptr;             // many-row attention scratch [record rows][64]
+    float* rows_o = nullptr;             // many-row attention scratch [record rows][64] (one scale group per row only)
     float2* rows_ml = nullptr;           //                            [record rows]
     uint32_t* rows_cnt = nullptr;        // [rows_max_units] arrival counters, zero between launches
     int splits_override = 0;
@@ -728,10 +728,12 @@ int create_impl(kvq_ctx** out, int layers, int q_heads, int kv_heads, int head_d
     ok = ok && dev_alloc(c, &c->part_s2, sizeof(float) * max_partial_records(c)) == cudaSuccess;
     ok = ok && dev_alloc(c, &c->unit_var, sizeof(float) * units) == cudaSuccess;
     ok = ok && dev_alloc(c, &c->vis, sizeof(uint32_t) * 4 * (size_t)batch * kMaxQueryRows) == cudaSuccess;
-    const size_t rows_records = rows_max_record_rows(c->sm_count);
-    ok = ok && dev_alloc(c, &c->rows_o, sizeof(float) * rows_records * kHeadDim) == cudaSuccess;
-    ok = ok && dev_alloc(c, &c->rows_ml, sizeof(float2) * rows_records) == cudaSuccess;
-    ok = ok && dev_alloc(c, &c->rows_cnt, sizeof(uint32_t) * rows_max_units(c->sm_count)) == cudaSuccess;
+    if (scale_groups == 1) {                           // the other layouts refuse the calls that use these
+        const size_t rows_records = rows_max_record_rows(c->sm_count);
+        ok = ok && dev_alloc(c, &c->rows_o, sizeof(float) * rows_records * kHeadDim) == cudaSuccess;
+        ok = ok && dev_alloc(c, &c->rows_ml, sizeof(float2) * rows_records) == cudaSuccess;
+        ok = ok && dev_alloc(c, &c->rows_cnt, sizeof(uint32_t) * rows_max_units(c->sm_count)) == cudaSuccess;
+    }
     ok = ok && dev_alloc(c, &c->d_lens, sizeof(int) * 3 * (size_t)batch * kvq_ctx::kLenSlots) == cudaSuccess;
     ok = ok && dev_alloc(c, &c->flags, sizeof(uint32_t)) == cudaSuccess;
     ok = ok && dev_alloc(c, &c->st_feats, sizeof(float) * 4 * batch) == cudaSuccess;
@@ -768,8 +770,10 @@ int create_impl(kvq_ctx** out, int layers, int q_heads, int kv_heads, int head_d
         ok = ok && cudaMemset(c->chunk_arrivals, 0, sizeof(uint32_t) * batch) == cudaSuccess;
         ok = ok && cudaMemset(c->step_cls, 0, sizeof(uint32_t) * batch) == cudaSuccess;
         ok = ok && cudaMemset(c->part_cnt, 0, sizeof(uint32_t) * units * kMaxQueryRows) == cudaSuccess;
-        ok = ok && cudaMemset(c->rows_cnt, 0, sizeof(uint32_t) * rows_max_units(c->sm_count)) == cudaSuccess;
-        ok = ok && rows_setup(c->device) == cudaSuccess;
+        if (scale_groups == 1) {
+            ok = ok && cudaMemset(c->rows_cnt, 0, sizeof(uint32_t) * rows_max_units(c->sm_count)) == cudaSuccess;
+            ok = ok && rows_setup(c->device) == cudaSuccess;
+        }
         // the controller block may exceed the default 48 KB of dynamic shared memory
         const int smem_max = (int)controller_smem(kMaxHidden);
         ok = ok && cudaFuncSetAttribute(k_select_bits, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_max) == cudaSuccess;
@@ -1610,7 +1614,7 @@ int kvq_recover(kvq_ctx* c) {
     DeviceGuard guard(c->device);
     KVQ_CUDA(c, cudaDeviceSynchronize());
     KVQ_CUDA(c, cudaMemset(c->part_cnt, 0, sizeof(uint32_t) * (size_t)c->batch * c->q_heads * kMaxQueryRows));
-    KVQ_CUDA(c, cudaMemset(c->rows_cnt, 0, sizeof(uint32_t) * rows_max_units(c->sm_count)));
+    if (c->rows_cnt) KVQ_CUDA(c, cudaMemset(c->rows_cnt, 0, sizeof(uint32_t) * rows_max_units(c->sm_count)));
     KVQ_CUDA(c, cudaMemset(c->flags, 0, sizeof(uint32_t)));
     float* base = nullptr;
     if (c->device >= 0 && c->device < KVQ_STATIC_MAX_DEVICES) {

@@ -56,7 +56,7 @@ constexpr int kRowsMaxRows = 32;                       // rows of a unit at most
 inline size_t rows_max_record_rows(int sm_count) { return 128 * (size_t)sm_count; }
 inline size_t rows_max_units(int sm_count) { return 16 * (size_t)sm_count; }
 
-// For every handle: shared-memory limits of the kernels on this device, and how many of their CTAs fit an SM.
+// For every handle with one scale group per row: shared-memory limits of the kernels on this device, and how many of their CTAs fit an SM.
 cudaError_t rows_setup(int device);
 // pairs: (sequence, KV head) pairs; tree_nodes: 0 without a tree; splits > 0: as many warps per unit as that (rounded up to
 // whole CTAs, and down to what the records hold).  ctas == 0: too many units for a launch.

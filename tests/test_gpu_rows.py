@@ -609,3 +609,20 @@ def test_large_queries_of_unused_nodes_cost_the_others_no_bits(gu, oracle, junk,
         got = c.run_tree(Q, (K, V, bits, par), window)
         assert np.array_equal(got, want)
         assert np.all(got[unused] == 0)
+
+
+def test_layouts_that_refuse_these_calls_hold_no_memory_for_them(gu):
+    """The partial records (256 bytes for each of 128 rows per SM, and their counters) are part of handles with one scale group."""
+    import torch
+    from paper_2604_04722_b200 import binding as kq
+    records = torch.cuda.get_device_properties(0).multi_processor_count * 128 * 256
+    arena = 40 * 65536
+    need = [kq.kvq_workspace_bytes(1, 2, 1, 64, 64, 1, arena, groups) for groups in (1, 2)]
+    assert need[0] - need[1] >= records
+    handles = [kq.kvq_create_arena(1, 2, 1, 64, 64, 1, arena), kq.kvq_create_grouped(1, 2, 1, 64, 64, 1, arena, 2),
+               kq.kvq_create_perchannel(1, 2, 1, 64, 64, 1, arena)]
+    held = [kq.kvq_device_bytes(h) for h in handles]
+    assert held[0] - held[1] >= records and held[0] - held[2] >= records - 2 ** 16   # (waiting rows of per-channel keys)
+    for h in handles:
+        kq.kvq_recover(h)
+        kq.kvq_destroy(h)
