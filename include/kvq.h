@@ -315,7 +315,8 @@ int kvq_decode_attn_window(kvq_ctx* ctx, int layer, const void* Q, void* O, int 
  *   target    dev fp32 [batch][n_nodes + 1][vocab]: the target's next-token probabilities after the last cached token
  *             (row 0) and after node i (row i + 1); finite, not negative
  *   draft_opt dev fp32, same shape: the distributions the children of row 0 / of node i were drawn from, each child on
- *             its own; or NULL: the drafted tokens are fixed guesses
+ *             its own (finite, not negative; the row of a node without children may hold anything); or NULL: the
+ *             drafted tokens are fixed guesses
  *   tokens, parents  dev int32 [batch][n_nodes]; parents as in kvq_attend_tree.  A token outside [0, vocab) is turned down
  *   u_accept  dev fp32 [batch][n_nodes], u_next dev fp32 [batch]: uniform numbers in [0, 1)
  * From the root, the children of the node reached so far are tested in index order.  Child i with token x is accepted

@@ -112,8 +112,10 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_tree(const VerifyPara
     int n_accepted = 0;
     bool pending = false;                              // Z is out of date: a rejection has not been followed by its sum yet
     uint32_t pass = 0;
-    // r(v) of the current row from p(v) and q(v) (zero for fixed guesses), as far as fixed guesses were not turned down
-    auto residual = [&](float p, float q) -> double { return fmax((double)p - c * (double)q, 0.0); };
+    // r(v) of the current row from p(v) and q(v) (zero for fixed guesses), as far as fixed guesses were not turned down.  Where no
+    // child was turned down q takes no part: a node without children has no draft distribution, and its row may hold anything
+    // (zero times what is not finite would be NaN).
+    auto residual = [&](float p, float q) -> double { return fmax((double)p - (c != 0.0 ? c * (double)q : 0.0), 0.0); };
     auto turned_down = [&](int v) -> bool {
         if (P.draft) return false;
         for (unsigned long long m = tried; m; m &= m - 1ull)

@@ -239,3 +239,27 @@ def test_a_speculative_step_from_draft_to_append(gu, oracle):
             oc.append(*(a[None] for a in store[b]))
             want, bound = rr.attention(oracle, oc, [len(store[b][0])], Q1[b:b + 1], 3, 40, 4)
             assert np.all(np.abs(O1[b:b + 1].cpu().numpy().astype(np.float64) - want) <= bound)
+
+
+@pytest.fixture(scope="module")
+def drafted():
+    return {(V, near): _inputs(V, 6, 9, V, near=near) for V in (50, 5003, 70001) for near in (0.0, 0.7)}
+
+
+@pytest.mark.parametrize("junk", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("V", [50, 5003, 70001])
+def test_draft_rows_that_nothing_was_drawn_from_may_hold_anything(gu, drafted, junk, V):
+    """A node without children has no draft distribution, nor has the root of a tree without a node in use.  (The largest
+    vocabulary is more than a sequence's registers hold.)"""
+    for near in (0.0, 0.7):                            # draft and target equal: leaves are reached
+        x = {k: v.copy() for k, v in drafted[V, near].items()}
+        x["parents"][0] = -2                           # no node in use: the next token comes from row 0 of the target
+        x["parents"][1] = np.arange(9) - 1             # a chain that is accepted as a whole
+        x["u"][1] = 0
+        for b in range(6):
+            drawn = {int(p) + 1 for i, p in enumerate(x["parents"][b]) if -1 <= p < i}
+            for row in set(range(10)) - drawn:
+                x["draft"][b, row] = junk
+        got = _run(gu, x)
+        _check(x, got)
+        assert got[0][0] == 0 and got[0][1] == 9 and np.all(got[2] >= 0)
