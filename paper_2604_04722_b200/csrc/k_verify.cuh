@@ -28,7 +28,6 @@
 
 namespace kvq {
 
-constexpr int kMaxVerifyNodes = 64;
 constexpr int kVerifyThreads = 512, kVerifyWarps = kVerifyThreads / 32;
 constexpr int kVerifyMaxCluster = 8;
 constexpr int kVerifyKeep = 16;            // vocabulary entries of a row (of each distribution) that a lane keeps
@@ -46,8 +45,8 @@ __global__ void __launch_bounds__(kVerifyThreads) k_verify_tree(const VerifyPara
     const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int b = (int)blockIdx.x / ctas;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    __shared__ int s_tok[kMaxVerifyNodes];
-    __shared__ float s_u[kMaxVerifyNodes], s_p[kMaxVerifyNodes], s_q[kMaxVerifyNodes];
+    __shared__ int s_tok[kMaxTreeNodes];
+    __shared__ float s_u[kMaxTreeNodes], s_p[kMaxTreeNodes], s_q[kMaxTreeNodes];
     __shared__ double s_sums[2][kVerifyMaxCluster * kVerifyWarps];         // sums of all warps of the cluster, in vocabulary order; two passes alternate
     __shared__ double s_r[32 * kVerifyKeep];                               // the final draw's part of the row
 

@@ -153,6 +153,7 @@ constexpr int kProfMaxCalls = 1024;
 #ifndef KVQ_APPEND_TOKENS_PER_THREAD
 #define KVQ_APPEND_TOKENS_PER_THREAD 2
 #endif
+static_assert(KVQ_MAX_TREE_NODES == kMaxTreeNodes, "the header states what the kernels hold");
 static_assert(KVQ_APPEND_TOKENS_PER_THREAD >= 1 && KVQ_APPEND_TOKENS_PER_THREAD <= kMaxTokensPerThread, "chunk size");
 #ifndef KVQ_OVERLAP_LAUNCHES
 #define KVQ_OVERLAP_LAUNCHES 1

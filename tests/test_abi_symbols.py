@@ -40,6 +40,13 @@ def test_every_declared_symbol_is_exported_and_bound(kvq_lib):
         assert name in names, "binding has %s which the header does not declare" % name
 
 
+def test_limits_of_the_header_and_of_the_binding_agree():
+    from paper_2604_04722_b200 import binding
+    text = open(HEADER).read()
+    for name in ("KVQ_MAX_TREE_NODES", "KVQ_STATIC_MAX_PARTIALS", "KVQ_EXPORT_ROW_BYTES"):
+        assert int(re.search(r"#define\s+%s\s+(\d+)" % name, text).group(1)) == getattr(binding, name)
+
+
 def test_host_side_argument_checks_need_no_device(kvq_lib):
     h = ctypes.c_void_p()
     assert kvq_lib.kvq_create(None, 1, 1, 1, 64, 16, 1) == -1
