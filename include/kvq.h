@@ -305,7 +305,9 @@ int kvq_attend_tree(kvq_ctx* ctx, int layer, const void* Q, const void* K, const
  * cached tokens (its own included) and the first `sinks` ones, O = Softmax(q K^T / 8) V over those.  Q, O: dev fp16
  * [batch][q_heads][64], 16-byte aligned.  window >= 1, sinks >= 0 (both may exceed the length).  A sequence of a
  * ragged layer that holds nothing gets a zero row; KVQ_ERR_EMPTY if none holds a token.  Reads the packed rows inside
- * the window and the sinks only.  One launch.  Caches with one scale group per row only (KVQ_ERR_ARG otherwise).
+ * the window and the sinks only, and of the per-token index what finds their slots (up to its end for a bit-width that
+ * does not occur there).  One launch; one that was captured into a graph is captured again after an append to the layer.
+ * Caches with one scale group per row only (KVQ_ERR_ARG otherwise).
  */
 int kvq_decode_attn_window(kvq_ctx* ctx, int layer, const void* Q, void* O, int window, int sinks, void* stream);
 
@@ -318,6 +320,7 @@ int kvq_decode_attn_window(kvq_ctx* ctx, int layer, const void* Q, void* O, int 
  *             its own (finite, not negative; the row of a node without children may hold anything); or NULL: the
  *             drafted tokens are fixed guesses
  *   tokens, parents  dev int32 [batch][n_nodes]; parents as in kvq_attend_tree.  A token outside [0, vocab) is turned down
+ *             like any other (nodes that only pad a tree are marked by their parents: a rejection changes what is drawn)
  *   u_accept  dev fp32 [batch][n_nodes], u_next dev fp32 [batch]: uniform numbers in [0, 1)
  * From the root, the children of the node reached so far are tested in index order.  Child i with token x is accepted
  * when u_accept[i] * Z * q(x) < r(x), where r = max(p - c q, 0); before a rejection c = 0 and Z = 1, a rejection sets
@@ -491,7 +494,8 @@ int kvq_set_profiling(kvq_ctx* ctx, int on);
 int kvq_profile_read(kvq_ctx* ctx, double* attn_ms_total, int* calls);
 
 /* Device flags recorded by kernels since the last call (host uint32, cleared on read). */
-#define KVQ_FLAG_BAD_BITS 1u      /* a bit-width outside {2,4,8,16} was appended (stored as fp16) */
+#define KVQ_FLAG_BAD_BITS 1u      /* a bit-width outside {2,4,8,16} was appended (stored as fp16), or given to
+                                     kvq_attend_tree for a node in use (taken as fp16) */
 #define KVQ_FLAG_ARENA_FULL 4u    /* an append ran out of arena blocks; the tokens that did not fit are lost */
 #define KVQ_FLAG_WAIT_TIMEOUT 2u  /* a bounded wait expired in a decode call (on an async copy, or in
                                      kvq_decode_step on the class that the storing CTAs publish); that

@@ -19,10 +19,12 @@
 //
 // Unpacking K costs one AND per two codes: a field cut out in place at bit k <= 8 of a 16-bit lane IS the fp16 number
 // code * 2^(k-24) (a subnormal: that encoding is linear), and the matrix instruction takes subnormals exactly.  The
-// power 2^-k is undone on the query's side.  Both factors are exact (the query is only scaled by powers of two), so a
-// logit
+// power 2^-k is undone on the query's side.  The query is scaled by powers of two only, F (one for the rows of a unit, which
+// puts their largest value below 2^15) and down to 2^-6 for k.  That is exact while the rows' largest value is below 512;
+// above, values of less than about 2^-22 of it become subnormal, and lose at most 2^-33 of it.  So a logit
 //   y = log2(e)/8 * (s_k * sum_i q_i c_i + z_k * sum_i q_i)
-// carries fp32 accumulation error only.  V codes are cut out the same way, but as prefixes of their byte (c0, c0 + 4 c1,
+// carries, as a rule, only the error of the matrix instruction's sum of 64 products, which it truncates (see below; its tests
+// allow 2^-22 per addition of the absolute sum).  V codes are cut out the same way, but as prefixes of their byte (c0, c0 + 4 c1,
 // ...), which the accumulators undo when the pool is left.  The weight w = p * s_v is rounded once to fp16 (by at most 2^-11
 // of its value: the rounding that the fp16 operand forces).  What that does is made to act on centred codes:
 //   sum p (s c + z) = sum w (c - mid) + sum p (z + mid s),   mid = -z / s, inside [0, 2^bits - 1], per token
@@ -55,8 +57,11 @@
 //
 // Window.  Slots of a pool are handed out in position order, so a window is a suffix and the sinks a prefix of every
 // pool.  Where they start follows from the per-token index: the first token of class c at or after position p names
-// the slot.  One warp per class looks for it (a step reads 128 index words).  Rows of different depth have different
-// window starts; they are told apart only inside the tiles at the edge.
+// the slot.  One warp per class looks for it, 128 index words per step and round trip, in one or two steps where the
+// widths are mixed.  A class that does not occur from p on is looked for up to the end of the sequence: with 16 bits for
+// four sinks and 2 to 8 bits behind them a window of 256 takes 9.9 us of 2048 tokens and 68 us of 32768 (6.6 us with
+// mixed widths), one of 8192 on 16 sequences x 32 heads 214 us (86 us).  Rows of different depth have different window
+// starts; they are told apart only inside the tiles at the edge.
 //
 // Drafted rows (the tree) are quantized at their bit-width and put back together, rounded to fp16, by the CTA of the
 // last piece, as fp16 tiles in shared memory that the fp16 consumer reads under a mask of ancestors.
@@ -593,10 +598,11 @@ __device__ __forceinline__ uint32_t rows_record(const RowsParams& P, uint32_t j,
     return 2u * j + (j * P.span >= unit * P.ticks ? 0u : 1u);      // (it starts inside the unit, or in front of it)
 }
 
-// What bounds it.  Long caches: the issue of its instructions, about 240 per tile with 16 rows, in dependent chains that four
-// warps per scheduler do not hide (8192 tokens, 16 rows: a scheduler issues in 53 % of its active cycles, ALU 36 %, matrix pipe
-// 28 %, exponentials 23 %).  16 sequences x 32 heads x 32768 tokens, 1.26 GB of packed rows: 16 rows 399 us (3.2 TB/s of them,
-// 0.48 of the copy bandwidth), one row over a window of 8192 86 us (3.7 TB/s); 32 rows over 8192 tokens, 0.42 GB, 232 us, 148
+// What bounds it.  Long caches: latency.  A tile is one dependent chain of products, softmax, vote, transposition and
+// products, about 240 instructions with 16 rows, which four warps per scheduler (two with 32 rows) do not hide (8192 tokens,
+// 16 rows: a scheduler issues in 53 % of its active cycles, ALU 36 %, matrix pipe 28 %, exponentials 23 %).  The 16-row kernel
+// is held to 128 registers and spills around its loops (86 bytes stored and 56 loaded with a tree, 60 and 24 without).  16 sequences x 32 heads x 32768 tokens, 1.26 GB of packed rows: 16 rows 401 us (3.1 TB/s of them,
+// 0.48 of the copy bandwidth), one row over a window of 8192 87 us (3.6 TB/s); 32 rows over 8192 tokens, 0.42 GB, 235 us, 146
 // Tflop/s.  Pools of 16 bits alone are bound by memory.  Short caches: the chain of round trips (fills, index, block table,
 // rows, merge) and instructions that are not in the caches yet, 6 to 10 us.  Two tiles at a time, for more independent
 // instructions, outgrew the innermost instruction cache (20 % slower on mixed pools).

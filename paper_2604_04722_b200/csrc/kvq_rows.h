@@ -52,7 +52,7 @@ constexpr uint32_t kRowsMaxCluster = 16;               // CTAs of a unit that me
 constexpr int kRowsMaxRows = 32;                       // rows of a unit at most
 
 // What a handle keeps for launches that cut units: rows of partial records, two records for each CTA (at most four CTAs of
-// 8 rows per SM, three of 16, two of 32), and arrival counters, for at most four times as many units as there are CTAs.
+// 8 or 16 rows per SM, two of 32), and arrival counters, for at most four times as many units as there are CTAs.
 inline size_t rows_max_record_rows(int sm_count) { return 128 * (size_t)sm_count; }
 inline size_t rows_max_units(int sm_count) { return 16 * (size_t)sm_count; }
 
