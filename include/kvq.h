@@ -338,6 +338,100 @@ int kvq_verify_tree(const float* target, const float* draft_opt, const int32_t* 
                     int32_t* path, int32_t* next_token, void* stream);
 
 /*
+ * A paged 16-bit cache: requests that come and go one by one, and that share the pages of a prompt.  (The paper's FP16
+ * baseline in the form in which a server holds it, beside the mixed-precision cache above, whose rows live until kvq_reset.)
+ * The caller owns all memory; none of these calls needs a handle, and the buffers belong to the current device.
+ *
+ * Keys and values of one layer lie in n_pages pages of page_size slots; element (page, slot, head, channel) is at
+ * K + page * page_stride + slot * slot_stride + head * head_stride + channel (in elements; V the same), so that pages may be kept slot by slot or
+ * head by head, and keys and values in one tensor.  K and V dev, 16-byte aligned; strides multiples of 8, not negative.
+ * head_dim a multiple of 8 (kvq_page_attn: 64 or 128); dtype KVQ_FP16 or KVQ_BF16; n_pages <= KVQ_MAX_PAGES.  A request's
+ * row of a block table (int32) lists its pages in order; its token at position t is in slot t % page_size of entry t / page_size.  A page
+ * that is not full is listed by one row only; full ones may be shared.
+ */
+#define KVQ_FP16 0
+#define KVQ_BF16 1
+#define KVQ_FP32 2
+#define KVQ_MAX_PAGE_ROWS 4096                /* requests (beams) of a batch */
+#define KVQ_MAX_PAGES 1048576                 /* pages of a cache */
+typedef struct kvq_page_cache {
+    void* K;
+    void* V;
+    int64_t page_stride, slot_stride, head_stride;
+    int32_t n_pages, page_size, kv_heads, head_dim, dtype;
+} kvq_page_cache;
+
+/*
+ * One step of the block tables: rows take over the pages of their parents, pages are taken for the step's new tokens, and every
+ * new token gets its slot.  The pages in use are those that the rows list, so nothing has to be given back and no count can be wrong.
+ *   tables_in, tables_out   dev int32 [batch][table_width]; lens_in, lens_out dev int32 [batch]: tokens held
+ *   parents_opt   dev int32 [batch] or NULL.  Row b takes over the pages and tokens of row parents[b] of tables_in (beam search:
+ *                 kvq_beam_select's parents), or starts empty where that is -1 (a request leaves, another may come).  A page that is not
+ *                 full stays with the first child; every other child gets a page of its own for it and an entry in `copies`.
+ *                 NULL: every row goes on, and tables_out may be tables_in (it may not overlap it otherwise).  lens_out
+ *                 may be lens_in in any case.
+ *   new_lens      dev int32 [batch]: tokens that the step adds (0 and more)
+ *   held_opt      dev uint8 [n_pages] or NULL: pages that are not to be taken although no row lists them (not zero: held)
+ *   cu_new        dev int32 [batch + 1]: new tokens of the rows before, the total at the end
+ *   slots         dev int64 [max_new]: page * page_size + slot of the new tokens, one row after the other; -1 behind the last
+ *   positions_opt dev int32 [max_new] or NULL: their positions in their requests, -1 behind the last
+ *   copies_opt    dev int32 [batch][3] (NULL only without parents): {page, new page, slots to copy} or {-1, -1, 0}
+ *   status        dev uint32 [1]: 0, or KVQ_PAGE_* bits, and then the step did not take place: tables_out and lens_out hold
+ *                 what tables_in and lens_in hold, cu_new zeros, slots, positions and copies -1
+ * New pages are the free ones in ascending order, taken in row order.  Entries of tables_out behind a row's pages are left as
+ * they were.  table_width >= 1, 0 <= batch <= KVQ_MAX_PAGE_ROWS.  One launch.
+ */
+#define KVQ_PAGE_FULL 1u                      /* not enough free pages */
+#define KVQ_PAGE_LONG 2u                      /* a row would not fit table_width pages */
+#define KVQ_PAGE_SLOTS 4u                     /* more than max_new new tokens */
+#define KVQ_PAGE_BAD 8u                       /* a parent, length or page out of range */
+int kvq_page_step(const int32_t* tables_in, int32_t* tables_out, int table_width, const int32_t* lens_in, int32_t* lens_out,
+                  const int32_t* parents_opt, const int32_t* new_lens, int batch, const uint8_t* held_opt, int n_pages,
+                  int page_size, int max_new, int32_t* cu_new, int64_t* slots, int32_t* positions_opt, int32_t* copies_opt,
+                  uint32_t* status, void* stream);
+
+/*
+ * Stores n_new tokens of one layer: K, V dev 16-bit [n_new][kv_heads][head_dim], 16-byte aligned, to slots (dev int64 [n_new]; one
+ * outside the cache, such as -1, is passed over).  copies_opt (dev int32 [batch][3] or NULL): what kvq_page_step listed; the
+ * first slots of a page are copied to another page in the same launch.  A slot may be given once.
+ */
+int kvq_page_append(const kvq_page_cache* cache, const void* K, const void* V, const int64_t* slots, int n_new,
+                    const int32_t* copies_opt, int batch, void* stream);
+
+/*
+ * Attention of one new token per request over its pages: O = Softmax(scale * q K^T) V over the first lens[b] tokens, query head h
+ * reading KV head h / (q_heads / kv_heads).  Q, O: dev [batch][q_heads][head_dim] of the cache's type, 16-byte aligned; lse_opt
+ * dev fp32 [batch][q_heads] or NULL: the logarithm of the sum of exponentials.  A row of length 0 (or less) gets zeros and -inf; lengths beyond
+ * the table count as its width.  Slots behind a row's length may hold anything, and tokens on pages outside the cache (such as
+ * -1) do not take part.  Sums are fp32; the cut of the work does not depend on the order in which CTAs run, so equal calls give equal bits.
+ * workspace: dev, 16-byte aligned, at least kvq_page_attn_workspace_bytes (host uint64; KVQ_ERR_NOMEM if less), zero before its first use; every
+ * call leaves it ready for the next, of any shape.  Calls that may overlap on the device need a workspace each.  One launch.
+ */
+int kvq_page_attn_workspace_bytes(int batch, int q_heads, int kv_heads, int head_dim, uint64_t* bytes_out);
+int kvq_page_attn(const kvq_page_cache* cache, const void* Q, void* O, float* lse_opt, const int32_t* tables, int table_width,
+                  const int32_t* lens, int batch, int q_heads, float scale, void* workspace, uint64_t workspace_bytes,
+                  void* stream);
+
+/*
+ * Beam search: the n_out best continuations of every request.  Candidate (beam w, token v) has the score
+ * scores[w] + logits[w][v] - log sum_u exp(logits[w][u]); ties go to the lowest beam, then the lowest token.
+ *   logits        dev [batch][beams][vocab] of dtype KVQ_FP16, KVQ_BF16 or KVQ_FP32
+ *   scores        dev fp32 [batch][beams]: sums of log-probabilities so far
+ *   finished_opt  dev uint8 [batch][beams] or NULL: a beam that has ended (not zero) has one candidate, end_token at its score as it is;
+ *                 its logits are not read
+ *   end_token     0 <= end_token < vocab, or -1 (none; finished_opt is then NULL)
+ *   parents, tokens, scores_out  dev int32, int32, fp32 [batch][n_out], best first: the row b * beams + w (kvq_page_step's parents where
+ *                 n_out == beams), the token and the score; -1, -1 and -inf where candidates run out
+ *   finished_out_opt  dev uint8 [batch][n_out] or NULL: 1 for a beam that had ended, takes end_token or is missing
+ * Candidates whose score is not finite do not count (masked tokens, beams of score -inf; a row with a NaN or +inf has
+ * none).  1 <= beams, n_out <= KVQ_MAX_BEAMS; 1 <= vocab <= 2^30.  batch == 0 is a no-op.  One launch.
+ */
+#define KVQ_MAX_BEAMS 32
+int kvq_beam_select(const void* logits, int dtype, const float* scores, const uint8_t* finished_opt, int batch, int beams,
+                    int vocab, int n_out, int end_token, int32_t* parents, int32_t* tokens, float* scores_out,
+                    uint8_t* finished_out_opt, void* stream);
+
+/*
  * kvq_decode_attn without any buffer that had to be allocated for it.  (No counterpart in
  * the paper: this is a packaging variant of the call above, same arithmetic, same result.)
  *

@@ -27,6 +27,11 @@ KVQ_ERR_TOO_LARGE = -8
 KVQ_STATIC_MAX_PARTIALS = 8192
 KVQ_EXPORT_ROW_BYTES = 128
 KVQ_MAX_TREE_NODES = 64
+KVQ_FP16, KVQ_BF16, KVQ_FP32 = 0, 1, 2
+KVQ_MAX_PAGE_ROWS = 4096
+KVQ_MAX_PAGES = 1048576
+KVQ_MAX_BEAMS = 32
+KVQ_PAGE_FULL, KVQ_PAGE_LONG, KVQ_PAGE_SLOTS, KVQ_PAGE_BAD = 1, 2, 4, 8
 
 _vp, _i, _u64p = C.c_void_p, C.c_int, C.POINTER(C.c_uint64)
 
@@ -54,6 +59,11 @@ SIGNATURES = {
     "kvq_attend_tree": (_i, [_vp, _i, _vp, _vp, _vp, _vp, _vp, _i, _vp, _i, _i, _vp]),
     "kvq_decode_attn_window": (_i, [_vp, _i, _vp, _vp, _i, _i, _vp]),
     "kvq_verify_tree": (_i, [_vp, _vp, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "kvq_page_step": (_i, [_vp, _vp, _i, _vp, _vp, _vp, _vp, _i, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "kvq_page_append": (_i, [_vp, _vp, _vp, _vp, _i, _vp, _i, _vp]),
+    "kvq_page_attn_workspace_bytes": (_i, [_i, _i, _i, _i, _u64p]),
+    "kvq_page_attn": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _vp, _i, _i, C.c_float, _vp, C.c_uint64, _vp]),
+    "kvq_beam_select": (_i, [_vp, _i, _vp, _vp, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp]),
     "kvq_decode_attn_static": (_i, [_vp, _i, _vp, _vp, _vp]),
     "kvq_decode_step": (_i, [_vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "kvq_decode_step_host": (_i, [_vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
@@ -266,6 +276,102 @@ def kvq_verify_tree(target, draft, tokens, parents, batch: int, n_nodes: int, vo
     check(lib().kvq_verify_tree(_ptr(target), _ptr(draft), _ptr(tokens), _ptr(parents), batch, n_nodes, vocab,
                                 _ptr(u_accept), _ptr(u_next), _ptr(n_accepted), _ptr(path), _ptr(next_token),
                                 _stream(stream)), "kvq_verify_tree")
+
+
+class PageCache(C.Structure):
+    """``kvq_page_cache`` of the header; keeps the tensors alive."""
+    _fields_ = [("K", _vp), ("V", _vp), ("page_stride", C.c_int64), ("slot_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+def kvq_page_cache(K, V) -> PageCache:
+    """The paged cache in two CUDA tensors [pages][slots][kv_heads][head_dim] with equal strides, fp16 or bf16; views (pages kept
+    head by head, keys and values in one tensor) are fine as long as the channels are contiguous."""
+    import torch
+    if K.dtype not in (torch.float16, torch.bfloat16) or V.dtype != K.dtype or K.dim() != 4 or V.shape != K.shape:
+        raise ValueError("kvq_page_cache: two 4-dimensional fp16 or bf16 tensors of one shape")
+    if K.get_device() < 0 or V.get_device() != K.get_device():
+        raise ValueError("kvq_page_cache: both tensors on one CUDA device")
+    strides = [K.stride(i) if K.shape[i] > 1 else 0 for i in range(4)]
+    if strides != [V.stride(i) if V.shape[i] > 1 else 0 for i in range(4)] or strides[3] != 1:
+        raise ValueError("kvq_page_cache: equal strides, contiguous channels")
+    cache = PageCache(K.data_ptr(), V.data_ptr(), *strides[:3], *K.shape, KVQ_FP16 if K.dtype == torch.float16 else KVQ_BF16)
+    cache.tensors, cache.device, cache.torch_dtype, cache.ref = (K, V), K.get_device(), K.dtype, C.addressof(cache)
+    return cache
+
+
+def _dev(t, dtype, count: int, device: int, what: str) -> Optional[int]:
+    """Address of a contiguous CUDA tensor of the given type with at least ``count`` elements on ``device``, or None."""
+    if t is None:
+        return None
+    if t.get_device() != device or t.dtype != dtype or t.numel() < count or not t.is_contiguous():
+        raise ValueError("%s: a contiguous %s tensor of %d elements or more on the current device (cuda:%d)" % (what, dtype, count, device))
+    return t.data_ptr()
+
+
+def kvq_page_step(tables_in, tables_out, table_width: int, lens_in, lens_out, parents, new_lens, batch: int, held, n_pages: int,
+                  page_size: int, max_new: int, cu_new, slots, positions, copies, status, stream=None) -> None:
+    """One step of the block tables: rows take over their parents' pages, new tokens get pages and slots."""
+    import torch
+    d, i32, where = torch.cuda.current_device(), torch.int32, "kvq_page_step"
+    n = batch * table_width
+    check(lib().kvq_page_step(
+        _dev(tables_in, i32, n, d, where), _dev(tables_out, i32, n, d, where), table_width, _dev(lens_in, i32, batch, d, where),
+        _dev(lens_out, i32, batch, d, where), _dev(parents, i32, batch, d, where), _dev(new_lens, i32, batch, d, where), batch,
+        _dev(held, torch.uint8, n_pages, d, where), n_pages, page_size, max_new, _dev(cu_new, i32, batch + 1, d, where),
+        _dev(slots, torch.int64, max_new, d, where), _dev(positions, i32, max_new, d, where), _dev(copies, i32, 3 * batch, d, where),
+        _dev(status, i32, 1, d, where), _stream(stream)), where)
+
+
+def _cache(cache: PageCache, device: int, where: str) -> int:
+    if cache.device != device:
+        raise ValueError("%s: the cache is on cuda:%d, the current device is cuda:%d" % (where, cache.device, device))
+    return cache.ref
+
+
+def kvq_page_append(cache: PageCache, K, V, slots, n_new: int, copies=None, batch: int = 0, stream=None) -> None:
+    """Rows of new tokens to their slots, and the pages that kvq_page_step had copied."""
+    import torch
+    d, where = torch.cuda.current_device(), "kvq_page_append"
+    n = n_new * cache.kv_heads * cache.head_dim
+    check(lib().kvq_page_append(_cache(cache, d, where), _dev(K, cache.torch_dtype, n, d, where), _dev(V, cache.torch_dtype, n, d, where),
+                                _dev(slots, torch.int64, n_new, d, where), n_new, _dev(copies, torch.int32, 3 * batch, d, where), batch,
+                                _stream(stream)), where)
+
+
+def kvq_page_attn_workspace_bytes(batch: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
+    n = C.c_uint64()
+    check(lib().kvq_page_attn_workspace_bytes(batch, q_heads, kv_heads, head_dim, C.byref(n)), "kvq_page_attn_workspace_bytes")
+    return n.value
+
+
+def kvq_page_attn(cache: PageCache, Q, O, lse, tables, table_width: int, lens, batch: int, q_heads: int, scale: float, workspace,
+                  workspace_bytes: int, stream=None) -> None:
+    """Attention of one new token per request over its pages; the workspace (uint8) is zero before its first use."""
+    import torch
+    d, where = torch.cuda.current_device(), "kvq_page_attn"
+    n = batch * q_heads
+    check(lib().kvq_page_attn(_cache(cache, d, where), _dev(Q, cache.torch_dtype, n * cache.head_dim, d, where),
+                              _dev(O, cache.torch_dtype, n * cache.head_dim, d, where), _dev(lse, torch.float32, n, d, where),
+                              _dev(tables, torch.int32, batch * table_width, d, where), table_width, _dev(lens, torch.int32, batch, d, where),
+                              batch, q_heads, scale, _dev(workspace, torch.uint8, workspace_bytes, d, where), workspace_bytes,
+                              _stream(stream)), where)
+
+
+def kvq_beam_select(logits, dtype: int, scores, finished, batch: int, beams: int, vocab: int, n_out: int, end_token: int, parents,
+                    tokens, scores_out, finished_out=None, stream=None) -> None:
+    """The n_out best continuations of every request's beams."""
+    import torch
+    d, where = torch.cuda.current_device(), "kvq_beam_select"
+    kinds = {KVQ_FP16: torch.float16, KVQ_BF16: torch.bfloat16, KVQ_FP32: torch.float32}
+    if dtype not in kinds:
+        raise KvqError(KVQ_ERR_ARG, where)
+    n, m = batch * beams, batch * n_out
+    check(lib().kvq_beam_select(_dev(logits, kinds[dtype], n * vocab, d, where), dtype, _dev(scores, torch.float32, n, d, where),
+                                _dev(finished, torch.uint8, n, d, where), batch, beams, vocab, n_out, end_token,
+                                _dev(parents, torch.int32, m, d, where), _dev(tokens, torch.int32, m, d, where),
+                                _dev(scores_out, torch.float32, m, d, where), _dev(finished_out, torch.uint8, m, d, where),
+                                _stream(stream)), where)
 
 
 def kvq_decode_attn_static(ctx: int, layer: int, Q, O, stream=None) -> None:

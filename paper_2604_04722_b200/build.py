@@ -8,7 +8,7 @@ import sys
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libkvq.so")
-SOURCES = [os.path.join(CSRC, "kvq.cu"), os.path.join(CSRC, "kvq_rows.cu")]
+SOURCES = [os.path.join(CSRC, "kvq.cu"), os.path.join(CSRC, "kvq_rows.cu"), os.path.join(CSRC, "kvq_pages.cu")]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-Xptxas", "-v",
