@@ -48,17 +48,22 @@ struct BeamEntry {
     uint32_t key, token;                               // logit (0: none)
 };
 struct BeamPick {
-    uint64_t score;                                    // score_key (0: none)
+    uint64_t score;                                    // score_key
     uint32_t row, token;
+    __device__ bool before(const BeamPick& o) const {
+        return score != o.score ? score > o.score : row != o.row ? row < o.row : token < o.token;
+    }
 };
 
-// Dynamic shared memory: the lists of a CTA's slices, then the CTAs' picks (used by the first CTA).
-inline size_t beam_smem(int n_out) {
-    return (size_t)kBeamWarps * kBeamTasks * n_out * sizeof(BeamEntry) + (size_t)kBeamMaxCluster * n_out * sizeof(BeamPick);
+// Dynamic shared memory: the buffers of a CTA's slices, and in every CTA room for the picks that are left over (those of the
+// first CTA are used): of n slices at most n + 32 each.
+__host__ __device__ constexpr int beam_max_picks(int n) { return n * (n + 32); }
+inline size_t beam_smem(int tasks, int n) {
+    return (size_t)kBeamWarps * tasks * kBeamBuffer * sizeof(BeamEntry) + (size_t)beam_max_picks(n) * sizeof(BeamPick);
 }
 
-// The n best entries of a warp's buffer, in order (value descending, token ascending), to `list`; missing ones have the key 0.
-__device__ __forceinline__ void warp_best(const BeamEntry* buffer, int count, int n, BeamEntry* list) {
+// Cuts a warp's buffer back to its n best entries, in order (value descending, token ascending); it holds n or more.
+__device__ __noinline__ void warp_best(BeamEntry* buffer, int count, int n) {
     const int lane = threadIdx.x & 31;
     BeamEntry e[kBeamBuffer / 32];
 #pragma unroll
@@ -66,7 +71,7 @@ __device__ __forceinline__ void warp_best(const BeamEntry* buffer, int count, in
         e[k].key = 0, e[k].token = 0xffffffffu;
         if (lane + 32 * k < count) e[k] = buffer[lane + 32 * k];
     }
-    __syncwarp();                                      // (the list may be the buffer itself)
+    __syncwarp();
 #pragma unroll 1
     for (int i = 0; i < n; ++i) {
         uint32_t key = 0, token = 0xffffffffu;
@@ -78,34 +83,9 @@ __device__ __forceinline__ void warp_best(const BeamEntry* buffer, int count, in
 #pragma unroll
         for (int k = 0; k < kBeamBuffer / 32; ++k)
             if (e[k].key == best && e[k].token == at) e[k].key = 0, e[k].token = 0xffffffffu;
-        if (lane == 0) list[i].key = best, list[i].token = at;
+        if (lane == 0) buffer[i].key = best, buffer[i].token = at;
     }
     __syncwarp();
-}
-
-// Merges up to 32 sorted lists, one per lane: head(i) gives a lane's i-th pick (score 0 behind its last).  take(i, pick) is
-// called by all lanes with the picks in order.
-template <class Head, class Take>
-__device__ __forceinline__ void merge_lists(int n, Head head, Take take) {
-    int mine = 0;
-    BeamPick h = head(0);
-#pragma unroll 1
-    for (int i = 0; i < n; ++i) {
-        const uint32_t hi = (uint32_t)(h.score >> 32), lo = (uint32_t)h.score;
-        const uint32_t best_hi = __reduce_max_sync(0xffffffffu, hi);
-        bool in = hi == best_hi;
-        const uint32_t best_lo = __reduce_max_sync(0xffffffffu, in ? lo : 0u);
-        in = in && lo == best_lo;
-        const uint32_t row = __reduce_min_sync(0xffffffffu, in ? h.row : 0xffffffffu);
-        in = in && h.row == row;
-        const uint32_t token = __reduce_min_sync(0xffffffffu, in ? h.token : 0xffffffffu);
-        BeamPick pick;
-        pick.score = ((uint64_t)best_hi << 32) | best_lo;
-        pick.row = row;
-        pick.token = token;
-        take(i, pick);
-        if (in && h.token == token && pick.score != 0) h = head(++mine);
-    }
 }
 
 // Eight (16-bit) or four (fp32) neighbouring entries of a row as they lie in memory, from any address that is a multiple of
@@ -153,6 +133,10 @@ __device__ __forceinline__ void widen(const uint4& v, float* x) {
     }
 }
 
+__device__ __forceinline__ float widen_one(float x) { return x; }
+__device__ __forceinline__ float widen_one(__half x) { return __half2float(x); }
+__device__ __forceinline__ float widen_one(__nv_bfloat16 x) { return __bfloat162float(x); }
+
 // grid = batch clusters, block = kBeamThreads.
 template <class T>
 __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParams P) {
@@ -162,30 +146,34 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
     const int b = (int)blockIdx.x / ctas;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     constexpr int kVec = 16 / (int)sizeof(T), kLoads = 16 / kVec;          // entries of a load, loads of a lane per chunk
-    __shared__ BeamEntry s_buffer[kBeamWarps][kBeamBuffer];
     __shared__ float s_top[kBeamMaxSlices];            // of all slices of the request: largest logit ...
     __shared__ double s_sum[kBeamMaxSlices];           // ... and sum of exponentials relative to it
+    __shared__ uint64_t s_best[kBeamMaxSlices];        // by row, then slice: score of that logit, 0 for a slice without candidates
+    __shared__ uint8_t s_in[kBeamMaxSlices];           // ... and whether it is among the n best
     __shared__ float s_row_top[kMaxBeams];
     __shared__ double s_row_off[kMaxBeams];            // score - log of the sum
     __shared__ uint8_t s_alive[kMaxBeams];
+    __shared__ int s_count[kBeamWarps * kBeamTasks];
+    __shared__ uint64_t s_least;
+    __shared__ int s_picked;                           // (of the first CTA)
     extern __shared__ __align__(16) uint8_t s_dyn[];
     const int n = P.n_out;
-    BeamPick* s_picks = reinterpret_cast<BeamPick*>(s_dyn);                // [CTAs][n]
-    BeamEntry* s_lists = reinterpret_cast<BeamEntry*>(s_picks + kBeamMaxCluster * n);      // [warps * kBeamTasks][n]
+    const int tasks = P.beams * P.slices, warps = ctas * kBeamWarps, gwarp = rank * kBeamWarps + warp;
+    const int rounds = (tasks + warps - 1) / warps;    // slices of a warp, at most kBeamTasks
+    BeamPick* s_picks = reinterpret_cast<BeamPick*>(s_dyn);
+    BeamEntry* s_buffers = reinterpret_cast<BeamEntry*>(s_picks + beam_max_picks(n));      // [warps * rounds][kBeamBuffer]
+    if (tid == 0) s_picked = 0, s_least = 0;
 
     cluster.barrier_arrive();                          // (before another CTA's memory is written, all of them have to be there)
     pdl_launch_dependents();
     pdl_wait();
 
-    const int tasks = P.beams * P.slices, warps = ctas * kBeamWarps, gwarp = rank * kBeamWarps + warp;
-    constexpr float kLog2eF = 1.4426950408889634f;
 #pragma unroll 1
-    for (int j = 0, task = gwarp; j < kBeamTasks; ++j, task += warps) {
-        BeamEntry* list = s_lists + (warp * kBeamTasks + j) * n;
+    for (int j = 0, task = gwarp; j < rounds; ++j, task += warps) {
         float top = kBeamLowest;
         double sum = 0.0;
         int count = 0;
-        BeamEntry* buffer = s_buffer[warp];
+        BeamEntry* buffer = s_buffers + (warp * rounds + j) * kBeamBuffer;
         if (task < tasks) {
             const int row = task % P.beams, slice = task / P.beams;
             const size_t r = (size_t)b * P.beams + row;
@@ -202,7 +190,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
                 const T* z = static_cast<const T*>(P.logits) + r * (size_t)P.vocab;
                 // threshold: an entry stays in the running if it is larger, or as large and its token is below `above`
                 float least = -INFINITY;
-                uint32_t above = 0;
+                uint32_t above = 0, chunk = 0;
                 uint4 raw[kLoads];
                 auto load = [&](int c0) {
 #pragma unroll
@@ -227,15 +215,16 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
 #pragma unroll
                     for (int k = 1; k < 16; ++k) most = fmaxf(most, x[k]);
                     if (most > top) {
-                        sum *= (double)fast_exp2((top - most) * kLog2eF);
+                        sum *= (double)fast_exp2((top - most) * kLog2e);
                         top = most;
                     }
                     float part = 0.f;
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) part += fast_exp2((x[k] - top) * kLog2eF);
+                    for (int k = 0; k < 16; ++k) part += fast_exp2((x[k] - top) * kLog2e);
                     sum += (double)part;
-                    if (c0 == lo) {                    // the n-th largest of the lanes' maxima: a bitonic sort, descending
-                        float v = most;
+                    ++chunk;
+                    if ((chunk & (chunk - 1)) == 0) {  // the n-th largest of the lanes' maxima so far: a bitonic sort, descending
+                        float v = top;
 #pragma unroll
                         for (int size = 2; size <= 32; size <<= 1)
 #pragma unroll
@@ -244,29 +233,37 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
                                 const bool keep_max = ((lane & d) == 0) == ((lane & size) == 0);
                                 v = keep_max ? fmaxf(v, o) : fminf(v, o);
                             }
-                        least = __shfl_sync(0xffffffffu, v, n - 1);
-                        above = least > -INFINITY ? 0xffffffffu : 0u;      // (masked entries are no candidates)
+                        v = __shfl_sync(0xffffffffu, v, n - 1);
+                        if (v > least) least = v, above = 0xffffffffu;
                     }
                     if (!__any_sync(0xffffffffu, most >= least)) continue;
+                    uint32_t hits = 0;                 // entries of this lane that may stay
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        const uint32_t v = (uint32_t)(c0 + ((k / kVec) * 32 + lane) * kVec + k % kVec);
-                        uint32_t in = __ballot_sync(0xffffffffu, x[k] > least || (x[k] == least && v < above));
-                        if (in == 0) continue;
+                    for (int k = 0; k < 16; ++k)
+                        if (x[k] >= least) hits |= 1u << k;
+                    for (;;) {                         // one of every lane at a time, read again
+                        const int k = __ffs((int)hits) - 1;
+                        const uint32_t v = (uint32_t)(c0 + (k / kVec * 32 + lane) * kVec + k % kVec);
+                        const float z_v = k >= 0 ? widen_one(z[v]) : 0.f;
+                        bool mine = k >= 0 && (z_v > least || (z_v == least && v < above));
+                        uint32_t in = __ballot_sync(0xffffffffu, mine);
                         if (count + __popc(in) > kBeamBuffer) {
                             __syncwarp();
-                            warp_best(buffer, count, n, buffer);
+                            warp_best(buffer, count, n);
                             count = n;                 // (at least n + 1 were in it)
                             least = key_logit(buffer[n - 1].key);
                             above = buffer[n - 1].token;
-                            in = __ballot_sync(0xffffffffu, x[k] > least || (x[k] == least && v < above));
+                            mine = mine && (z_v > least || (z_v == least && v < above));
+                            in = __ballot_sync(0xffffffffu, mine);
                         }
-                        if ((in >> lane) & 1u) {
+                        if (mine) {
                             BeamEntry& e = buffer[count + __popc(in & ((1u << lane) - 1))];
-                            e.key = logit_key(x[k]);
+                            e.key = logit_key(z_v);
                             e.token = v;
                         }
                         count += __popc(in);
+                        hits &= hits - 1;
+                        if (!__any_sync(0xffffffffu, hits != 0)) break;
                     }
                 }
                 // the lanes' sums relative to the slice's largest
@@ -278,7 +275,11 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
             }
             __syncwarp();
         }
-        warp_best(buffer, count, n, list);
+        if (count > n + 32) {
+            warp_best(buffer, count, n);
+            count = n;
+        }
+        if (lane == 0) s_count[warp * rounds + j] = count;
         if (j == 0) cluster.barrier_wait();
         if (task < tasks && lane < ctas) {
             cluster.map_shared_rank(s_top, lane)[task] = top;
@@ -304,47 +305,60 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
         }
     }
     __syncthreads();
-    // ---- the CTA's lists, then the CTAs' picks
-    if (warp == 0) {
-        const int task = rank * kBeamWarps + lane % kBeamWarps + (lane / kBeamWarps) * warps, row = task % P.beams;
-        const bool live = lane < kBeamWarps * kBeamTasks && task < tasks && s_alive[row];
-        const BeamEntry* list = s_lists + ((lane % kBeamWarps) * kBeamTasks + lane / kBeamWarps) * n;
-        BeamPick* to = cluster.map_shared_rank(s_picks, 0) + rank * n;
-        merge_lists(
-            n,
-            [&](int i) {
-                BeamPick p = {0, 0xffffffffu, 0xffffffffu};
-                if (live && i < n && list[i].key != 0) {
-                    p.score = score_key(s_row_off[row] + ((double)key_logit(list[i].key) - (double)s_row_top[row]));
-                    p.row = (uint32_t)row;
-                    p.token = list[i].token;
-                }
-                return p;
-            },
-            [&](int i, const BeamPick& p) {
-                if (lane == 0) to[i] = p;
-            });
+    // ---- a bound: the n-th best of the slices' largest entries (every CTA for itself; ties by row and slice, which is their
+    // candidates' order).  n candidates are at least as good, so neither what is worse nor any other slice holds one of the n best.
+    for (int t = tid; t < tasks; t += kBeamThreads) {
+        const int row = t % P.beams;
+        const bool some = s_alive[row] && s_sum[t] > 0.0;
+        s_best[row * P.slices + t / P.beams] = some ? score_key(s_row_off[row] + ((double)s_top[t] - (double)s_row_top[row])) : 0ull;
+    }
+    __syncthreads();
+    for (int t = tid; t < tasks; t += kBeamThreads) {
+        const uint64_t mine = s_best[t];
+        int better = 0;
+        for (int o = 0; o < tasks; ++o) better += s_best[o] > mine || (s_best[o] == mine && o < t);
+        s_in[t] = better < n;
+        if (better == n - 1) s_least = mine;
+    }
+    __syncthreads();
+    // ---- the candidates that reach it go to the first CTA ...
+    {
+        const uint64_t least = s_least;
+        BeamPick* to = cluster.map_shared_rank(s_picks, 0);
+        int* picked = cluster.map_shared_rank(&s_picked, 0);
+        for (int j = 0, task = gwarp; j < rounds && task < tasks; ++j, task += warps) {
+            const int row = task % P.beams, count = s_count[warp * rounds + j];
+            if (!s_alive[row] || !s_in[row * P.slices + task / P.beams]) continue;
+            for (int i = lane; i < count; i += 32) {
+                const BeamEntry e = s_buffers[(warp * rounds + j) * kBeamBuffer + i];
+                BeamPick p;
+                p.score = score_key(s_row_off[row] + ((double)key_logit(e.key) - (double)s_row_top[row]));
+                p.row = (uint32_t)row;
+                p.token = e.token;
+                if (p.score < least) continue;
+                const int at = atomicAdd(picked, 1);
+                if (at < beam_max_picks(n)) to[at] = p;
+            }
+        }
     }
     cluster.sync();
-    if (rank == 0 && warp == 0) {
-        merge_lists(
-            n,
-            [&](int i) {
-                BeamPick p = {0, 0xffffffffu, 0xffffffffu};
-                if (lane < ctas && i < n) p = s_picks[lane * n + i];
-                return p;
-            },
-            [&](int i, const BeamPick& p) {
-                if (lane != 0) return;
-                const size_t at = (size_t)b * n + i;
-                const bool there = p.score != 0;
-                const size_t from = (size_t)b * P.beams + p.row;
-                P.parents[at] = there ? (int32_t)from : -1;
-                P.tokens[at] = there ? (int32_t)p.token : -1;
-                P.scores_out[at] = there ? (float)key_score(p.score) : -INFINITY;
-                if (P.finished_out) P.finished_out[at] = !there || (int32_t)p.token == P.end_token || (P.finished && P.finished[from] != 0);
-            });
+    if (rank != 0) return;
+    // ---- ... which ranks them: the order in which they came does not matter
+    const int picked = min(s_picked, beam_max_picks(n));
+    auto put = [&](int i, bool there, const BeamPick& p) {
+        const size_t at = (size_t)b * n + i, from = (size_t)b * P.beams + p.row;
+        P.parents[at] = there ? (int32_t)from : -1;
+        P.tokens[at] = there ? (int32_t)p.token : -1;
+        P.scores_out[at] = there ? (float)key_score(p.score) : -INFINITY;
+        if (P.finished_out) P.finished_out[at] = !there || (int32_t)p.token == P.end_token || (P.finished && P.finished[from] != 0);
+    };
+    for (int i = tid; i < picked; i += kBeamThreads) {
+        const BeamPick p = s_picks[i];
+        int better = 0;
+        for (int o = 0; o < picked && better < n; ++o) better += s_picks[o].before(p);
+        if (better < n) put(better, true, p);
     }
+    for (int i = picked + tid; i < n; i += kBeamThreads) put(i, false, BeamPick{0, 0, 0});
 }
 
 }  // namespace kvq

@@ -18,6 +18,7 @@
 // over at the borders of a CTA's stretch meets in records of the workspace: the CTA that delivers a unit's last record joins them,
 // in the order of the axis whoever comes last.  Bound: the rows' bytes, 4 D per token and KV head.
 #pragma once
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include "kvq_common.cuh"
 #include "kvq_pages.h"
@@ -26,25 +27,40 @@
 namespace kvq {
 
 constexpr int kAttnTile = 16;                          // tokens
-constexpr int kAttnWarps = 8, kAttnThreads = 32 * kAttnWarps;
 constexpr int kAttnMaxCtas = 1024;                     // arrival counters of a workspace
-constexpr int kAttnMinTiles = 1;                       // of a warp, where the work does not fill the launch
+#ifndef SNAP
+#define SNAP 16
+#endif
+#ifndef UT
+#define UT 20
+#endif
+constexpr int kAttnUnitTiles = UT;
+constexpr int kAttnMaxCluster = 16;
+#ifndef MINT
+#define MINT 1
+#endif
+constexpr int kAttnMinTilesLog2 = MINT;
+constexpr int kAttnSnap = SNAP;                           // see `border`
+constexpr int kAttnMinTiles = 1 << kAttnMinTilesLog2;                       // of a warp, where the work does not fill the launch
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLn2 = 0.69314718055994531f;
 
 template <int D>
 struct AttnGeom {
+    static constexpr int kWarps = D == 64 ? 16 : 8, kThreads = 32 * kWarps;
     static constexpr int kStages = 3;
     static constexpr int kRowBytes = 2 * D, kTensorBytes = kAttnTile * kRowBytes, kStageBytes = 2 * kTensorBytes;
     static constexpr int kRingBytes = kStages * kStageBytes;               // of a warp
 };
+constexpr int kJoinAt = (16 * (kAttnMaxCtas + 2) * (int)sizeof(float) + 127) / 128 * 128;      // behind the factors of a join
+static_assert(kJoinAt + AttnGeom<64>::kThreads * 16 <= AttnGeom<64>::kWarps * AttnGeom<64>::kRingBytes, "a join works in the rings");
 template <int D, int NT>
 __host__ __device__ constexpr int attn_record_floats() { return 8 * NT * (D + 2); }            // o [D][8 NT], m [8 NT], l [8 NT]
 
 // Shared memory: the rings, and the rows' place on the axis.
 template <int D>
 inline size_t attn_smem(int batch) {
-    return (size_t)kAttnWarps * AttnGeom<D>::kRingBytes + sizeof(int64_t) * ((size_t)batch + 1);
+    return (size_t)AttnGeom<D>::kWarps * AttnGeom<D>::kRingBytes + sizeof(int64_t) * ((size_t)batch + 1);
 }
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
@@ -98,11 +114,19 @@ struct AttnCursor {
     int b, u, t, tiles, len;
 };
 
+// A unit that a warp has part of: its number (-1: none) and its stretch of the axis.
+struct AttnPiece {
+    int unit;
+    int64_t begin, end;
+};
+
 // grid: at most kAttnMaxCtas resident CTAs; those that the lengths leave without work return.
 template <bool BF, int D, int NT>
-__global__ void __launch_bounds__(kAttnThreads, D == 64 ? 2 : 1) k_page_attn(const PageAttnParams P) {
+__global__ void __launch_bounds__(AttnGeom<D>::kThreads, 1) k_page_attn(const PageAttnParams P) {
     using G = AttnGeom<D>;
-    constexpr int kMt = D / 16, kR = 8 * NT, kStages = G::kStages;
+    constexpr int kMt = D / 16, kR = 8 * NT, kStages = G::kStages, kAttnWarps = G::kWarps, kAttnThreads = G::kThreads;
+    namespace cg = cooperative_groups;
+    const int C = P.cluster, rank = C > 1 ? (int)cg::this_cluster().block_rank() : 0, group = (int)blockIdx.x / C, groups = (int)gridDim.x / C;
     constexpr int kVecs = D / 8, kRowsAtOnce = 32 / kVecs, kCopies = kAttnTile / kRowsAtOnce;     // 16-byte vectors of a row
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
     extern __shared__ __align__(128) uint8_t s_ring_all[];
@@ -112,9 +136,10 @@ __global__ void __launch_bounds__(kAttnThreads, D == 64 ? 2 : 1) k_page_attn(con
     auto tiles_of = [&](int b) -> int { return (int)(tiles_before(b + 1) - tiles_before(b)); };
     auto len_of = [&](int b) -> int { return tiles_of(b) * kAttnTile - (int)(s_place[b] & 15); };
     __shared__ int64_t s_scan[kAttnWarps];
+    __shared__ int s_longest[kAttnWarps];
     __shared__ uint32_t s_there[kAttnWarps][kStages];  // tokens of a stage that exist
-    __shared__ int s_unit[2 * kAttnWarps];             // unit of a warp's first and last piece, -1: none
-    __shared__ uint32_t s_last;
+    __shared__ AttnPiece s_piece[2 * kAttnWarps];      // a warp's first and last piece
+    __shared__ uint32_t s_last[2];
 
     pdl_launch_dependents();
     pdl_wait();
@@ -127,13 +152,17 @@ __global__ void __launch_bounds__(kAttnThreads, D == 64 ? 2 : 1) k_page_attn(con
         auto read_len = [&](int b) { return (int)min((long long)max(P.lens[b], 0), room); };
         auto tiles = [&](int n) { return (n + (long long)kAttnTile - 1) / kAttnTile; };
         int64_t sum = 0;
+        int most = 0;
         for (int k = 0; k < per; ++k) {
             const int b = tid * per + k;
             if (b >= P.batch) break;
             const int n = read_len(b);
             s_place[b] = n;                            // for now
             sum += tiles(n);
+            most = max(most, (int)tiles(n));
         }
+        most = __reduce_max_sync(0xffffffffu, most);
+        if (lane == 0) s_longest[warp] = most;
         int64_t upto = sum;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -141,7 +170,7 @@ __global__ void __launch_bounds__(kAttnThreads, D == 64 ? 2 : 1) k_page_attn(con
             if (lane >= d) upto += o;
         }
         if (lane == 31) s_scan[warp] = upto;
-        if (tid < 2 * kAttnWarps) s_unit[tid] = -1;
+        if (tid < 2 * kAttnWarps) s_piece[tid].unit = -1;
         __syncthreads();
         int64_t at = upto - sum;
         for (int w = 0; w < warp; ++w) at += s_scan[w];
@@ -164,12 +193,16 @@ __global__ void __launch_bounds__(kAttnThreads, D == 64 ? 2 : 1) k_page_attn(con
             for (int h = tid; h < P.q_heads; h += kAttnThreads) P.lse[(size_t)b * P.q_heads + h] = -INFINITY;
     }
     const int64_t total = tiles_before(P.batch) * units_per_row;
-    const int ctas = (int)min((int64_t)gridDim.x, (total + kAttnWarps * kAttnMinTiles - 1) / (kAttnWarps * kAttnMinTiles));
-    if ((int)blockIdx.x >= ctas) return;
-    auto cta_begin = [&](int c) -> int64_t { return total * c / ctas; };
-    const int64_t lo = cta_begin(blockIdx.x), hi = cta_begin(blockIdx.x + 1);
-    const int64_t wlo = lo + (hi - lo) * warp / kAttnWarps, whi = lo + (hi - lo) * (warp + 1) / kAttnWarps;
-
+    if (total == 0) return;
+    // A cluster of CTAs (or one CTA) works on a stretch of the axis: a unit each, where there are no more units than clusters and
+    // none is long; otherwise equal shares.
+    int longest = 0;
+#pragma unroll
+    for (int w = 0; w < kAttnWarps; ++w) longest = max(longest, s_longest[w]);
+    const int units = P.batch * units_per_row, warps = C * kAttnWarps, warps_log2 = __ffs(warps) - 1;      // (a power of two)
+    const bool unit_each = units <= groups && longest <= kAttnUnitTiles * warps;
+    const int stretches = unit_each ? units : (int)min((int64_t)groups, ((total + warps * kAttnMinTiles - 1) >> (warps_log2 + kAttnMinTilesLog2)));
+    if (group >= stretches) return;
     auto locate = [&](int64_t at) -> AttnCursor {
         int b0 = 0, b1 = P.batch;
         while (b1 - b0 > 1) {
@@ -182,10 +215,31 @@ __global__ void __launch_bounds__(kAttnThreads, D == 64 ? 2 : 1) k_page_attn(con
         c.tiles = tiles_of(b0);
         c.len = len_of(b0);
         const int64_t rest = at - tiles_before(b0) * units_per_row;
-        c.u = (int)(rest / c.tiles);
+        c.u = (rest >> 32) == 0 ? (int)((uint32_t)rest / (uint32_t)c.tiles) : (int)(rest / c.tiles);
         c.t = (int)(rest - (int64_t)c.u * c.tiles);
         return c;
     };
+    // The borders between equal shares move to the border of a unit that is no more than kAttnSnap tiles away.
+    const int64_t share_size = unit_each ? 0 : (total >> 32) == 0 ? (int64_t)((uint32_t)total / (uint32_t)stretches) : total / stretches, share_more = total - share_size * stretches;     // (the first share_more have one tile more)
+    auto share = [&](int c) -> int64_t { return share_size * c + min((int64_t)c, share_more); };
+    auto border = [&](int c) -> int64_t {
+        if (c == stretches) return total;
+        if (unit_each) {
+            const int b = c / units_per_row;
+            return tiles_before(b) * units_per_row + (int64_t)(c - b * units_per_row) * tiles_of(b);
+        }
+        const int64_t at = share(c);
+        const AttnCursor x = locate(at);
+        const int back = x.t, ahead = x.tiles - x.t;
+        return min(back, ahead) > kAttnSnap ? at : back <= ahead ? at - back : at + ahead;
+    };
+    const int64_t lo = border(group), hi = border(group + 1);
+    if (lo == hi) return;                              // (the same for the whole cluster)
+    auto warp_border = [&](int w) -> int64_t { return lo + (((hi - lo) * w) >> warps_log2); };     // of the cluster's warps
+    auto cta_border = [&](int r) { return warp_border(r * kAttnWarps); };
+    const int64_t wlo = warp_border(rank * kAttnWarps + warp), whi = warp_border(rank * kAttnWarps + warp + 1);
+    const int64_t cta_lo = cta_border(rank), cta_hi = cta_border(rank + 1);
+
     auto next_unit = [&](AttnCursor& c) {
         c.t = 0;
         if (++c.u < units_per_row) return;
@@ -195,15 +249,13 @@ __global__ void __launch_bounds__(kAttnThreads, D == 64 ? 2 : 1) k_page_attn(con
         c.tiles = tiles_of(c.b);
         c.len = len_of(c.b);
     };
-    auto unit_id = [&](const AttnCursor& c) { return c.b * units_per_row + c.u; };
-    auto unit_begin = [&](int unit) -> int64_t {       // first tile of a unit
-        const int b = unit / units_per_row;
-        return tiles_before(b) * units_per_row + (int64_t)(unit - b * units_per_row) * tiles_of(b);
+    auto piece_at = [&](const AttnCursor& c, int64_t last) {       // behind its tile `last` of the axis
+        AttnPiece p;
+        p.unit = c.b * units_per_row + c.u;
+        p.begin = last + 1 - c.t;
+        p.end = p.begin + c.tiles;
+        return p;
     };
-    auto unit_end = [&](int unit) -> int64_t {
-        return unit_begin(unit) + tiles_of(unit / units_per_row);
-    };
-
     uint8_t* const ring = s_ring_all + (size_t)warp * G::kRingBytes;
     const uint32_t ring_addr = smem_addr(ring);
     const int count = (int)(whi - wlo);
@@ -406,12 +458,12 @@ __global__ void __launch_bounds__(kAttnThreads, D == 64 ? 2 : 1) k_page_attn(con
                     write_unit();
                 } else if (i + 1 < count) {            // the rest of a unit that an earlier warp began
                     deliver_piece(P.warp_rec + ((size_t)blockIdx.x * kAttnWarps + warp) * attn_record_floats<D, NT>());
-                    if (lane == 0) s_unit[2 * warp] = unit_id(at);
+                    if (lane == 0) s_piece[2 * warp] = piece_at(at, wlo + i);
                 } else {
                     cp_async_wait<0>();
                     __syncwarp();
                     deliver_piece(reinterpret_cast<float*>(ring));
-                    if (lane == 0) s_unit[2 * warp + 1] = unit_id(at);
+                    if (lane == 0) s_piece[2 * warp + 1] = piece_at(at, wlo + i);
                 }
                 if (i + 1 < count) {
                     next_unit(at);
@@ -423,90 +475,312 @@ __global__ void __launch_bounds__(kAttnThreads, D == 64 ? 2 : 1) k_page_attn(con
     }
     __syncthreads();
 
-    // ---- pieces of the CTA's units meet
-    constexpr int kRec = attn_record_floats<D, NT>();
-    auto piece = [&](int i) -> const float* {
-        return i & 1 ? reinterpret_cast<const float*>(s_ring_all + (size_t)(i >> 1) * G::kRingBytes)
-                     : P.warp_rec + ((size_t)blockIdx.x * kAttnWarps + (i >> 1)) * kRec;
+    // ---- pieces of the CTA's units meet.  First every piece's factors 2^(m_k - m) and its unit's sum of weights, a lane per
+    // piece; then the outputs, four heads of a channel per thread.
+    constexpr int kRec = attn_record_floats<D, NT>(), kPieces = 2 * kAttnWarps, kAtOnce = 32 / kPieces;
+    static_assert(kPieces == 16 || kPieces == 32, "a warp holds the pieces");
+    // (behind the first warp's piece in its ring)
+    struct Factors {
+        // factors of the pieces; at a unit's first piece its m, and its sum of weights or, where it is complete, the inverse
+        float factor[kPieces][kR], m[kPieces][kR], l[kPieces][kR];
     };
-    auto put = [&](int unit, int r, int d, float m, float l, float o) {        // of head r of the block, channel d
-        const int b = unit / units_per_row, u = unit - b * units_per_row, h0 = u / P.head_blocks;
-        const int hr = (u - h0 * P.head_blocks) * kR + r;
-        if (hr >= P.group) return;
-        const size_t row = (size_t)b * P.q_heads + h0 * P.group + hr;
-        O[row * D + d] = round16<BF>(l > 0.f || l != l ? o / l : 0.f);
-        if (d == 0 && P.lse) P.lse[row] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
+    static_assert(kRec * sizeof(float) + sizeof(Factors) <= G::kRingBytes && (G::kRingBytes - sizeof(Factors)) % 16 == 0, "a ring holds a piece and the factors");
+    Factors& s_f = *reinterpret_cast<Factors*>(s_ring_all + G::kRingBytes - sizeof(Factors));
+    auto last_piece = [&](int w) { return reinterpret_cast<const float*>(s_ring_all + (size_t)w * G::kRingBytes); };
+    auto first_piece = [&](int w) -> const float* { return P.warp_rec + ((size_t)blockIdx.x * kAttnWarps + w) * kRec; };
+    auto inverse = [](float l) { return l > 0.f || l != l ? 1.f / l : 0.f; };
+    struct Place {
+        size_t row;                                    // of the block's first head
+        int heads;
     };
-    int open[2] = {-1, -1};                            // units that go on in other CTAs: one from before, one beyond
-    for (int i = 0; i < 2 * kAttnWarps;) {
-        const int unit = s_unit[i];
-        if (unit < 0) {
-            ++i;
-            continue;
+    auto place_of = [&](int unit) {
+        const int b = unit / units_per_row, u = unit - b * units_per_row, h0 = P.head_blocks == 1 ? u : u / P.head_blocks, hb = u - h0 * P.head_blocks;
+        return Place{(size_t)b * P.q_heads + h0 * P.group + hb * kR, min(kR, P.group - hb * kR)};
+    };
+    auto put_lse = [&](const Place& at, int r, float m, float l) {
+        if (P.lse && r < at.heads) P.lse[at.row + r] = l == 0.f ? -INFINITY : m * kLn2 + logf(l);
+    };
+    auto put = [&](const Place& at, int r, int d, const float4& o, const float* inv) {
+        const float x[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (r + c < at.heads) O[(at.row + r + c) * D + d] = round16<BF>(x[c] * inv[c]);
+    };
+    const int j = lane % kPieces;
+    const AttnPiece mine = s_piece[j];
+    constexpr uint32_t kAll = kPieces == 32 ? 0xffffffffu : 0xffffu;
+    const bool is = mine.unit >= 0;
+    const uint32_t live = __ballot_sync(0xffffffffu, is) & kAll, below = live & ((1u << j) - 1);
+    const int unit_before = __shfl_sync(0xffffffffu, mine.unit, below ? 31 - __clz((int)below) : j, kPieces);
+    const uint32_t leads = __ballot_sync(0xffffffffu, is && (below == 0 || unit_before != mine.unit)) & kAll;     // the units' first pieces
+    {
+        // the lanes of a unit follow one another: a scan over them, and the unit's last lane has the result
+        const uint32_t later = leads & ~((2u << j) - 1), run = live & (later ? (1u << (__ffs((int)later) - 1)) - 1 : kAll);
+        const int begin = 31 - __clz((int)(leads & ((2u << j) - 1))), end = run ? 31 - __clz((int)run) : 0;
+        const int r = kAtOnce * warp + lane / kPieces; // (a head per warp, or two)
+        static_assert(kAtOnce * kAttnWarps >= kR, "every head has its lanes");
+        if (kAtOnce * warp < kR) {
+            float m = kLowest, l = 0.f;
+            if (is) {
+                const float* p = (j & 1 ? last_piece(j >> 1) : first_piece(j >> 1)) + D * kR + r;
+                m = p[0];
+                l = p[kR];
+            }
+            float top = m;
+#pragma unroll
+            for (int d = 1; d < kPieces; d <<= 1) {
+                const float o = __shfl_up_sync(0xffffffffu, top, d, kPieces);
+                if (j - d >= begin) top = fmaxf(top, o);
+            }
+            top = __shfl_sync(0xffffffffu, top, end, kPieces);
+            const float f = fast_exp2(m - top);
+            float sum = f * l;
+#pragma unroll
+            for (int d = 1; d < kPieces; d <<= 1) {
+                const float o = __shfl_up_sync(0xffffffffu, sum, d, kPieces);
+                if (j - d >= begin) sum += o;
+            }
+            sum = __shfl_sync(0xffffffffu, sum, end, kPieces);
+            s_f.factor[j][r] = f;
+            if ((leads >> j) & 1u) {
+                const bool closed = mine.begin >= cta_lo && mine.end <= cta_hi;
+                s_f.m[j][r] = top;
+                s_f.l[j][r] = closed ? inverse(sum) : sum;
+                if (closed) put_lse(place_of(mine.unit), r, top, sum);
+            }
         }
-        int end = i + 1;
-        while (end < 2 * kAttnWarps && (s_unit[end] == unit || s_unit[end] < 0)) ++end;
-        const int64_t u0 = unit_begin(unit), u1 = unit_end(unit);
-        const bool closed = u0 >= lo && u1 <= hi;
-        const int which = u0 < lo ? 0 : 1;
-        if (!closed) open[which] = unit;
-        float* rec = P.cta_rec + ((size_t)blockIdx.x * 2 + which) * kRec;
-        for (int e = tid; e < kR * D; e += kAttnThreads) {
-            const int r = e % kR, d = e / kR;
-            float top = kLowest;
-            for (int k = i; k < end; ++k)
-                if (s_unit[k] == unit) top = fmaxf(top, piece(k)[D * kR + r]);
-            float so = 0.f, sl = 0.f;
-            for (int k = i; k < end; ++k)
-                if (s_unit[k] == unit) {
-                    const float* p = piece(k);
-                    const float f = fast_exp2(p[D * kR + r] - top);
-                    so += f * p[d * kR + r];
-                    sl += f * p[(D + 1) * kR + r];
+    }
+    __syncthreads();
+    // what goes on in other CTAs of the cluster waits in shared memory (behind the pieces of warps 1 and 2), what goes on in other
+    // stretches in the workspace
+    auto cluster_rec = [&](int w) { return reinterpret_cast<float*>(s_ring_all + (size_t)(w + 2) * G::kRingBytes) - kRec; };
+    auto group_rec = [&](int w) { return P.cta_rec + ((size_t)group * 2 + w) * kRec; };
+    int open[2] = {-1, -1};                            // first pieces of units that go on in other CTAs: one from before, one beyond
+    if (leads) {
+        const int i0 = __ffs((int)leads) - 1, i1 = 31 - __clz((int)leads);
+        if (s_piece[i0].begin < cta_lo) open[0] = i0;
+        if (s_piece[i1].begin >= cta_lo && s_piece[i1].end > cta_hi) open[1] = i1;
+        if (open[0] < 0 && s_piece[i0].begin >= cta_lo && s_piece[i0].end > cta_hi) open[1] = i0;
+    }
+    // threads over the units of the CTA, quads of heads, channels
+    const int quads = min(kR, P.group + 3) / 4;        // (at most what the group needs)
+    for (int e = tid; e < __popc(leads) * quads * D; e += kAttnThreads) {
+        const int d = e % D, x = e / D, nth = quads == 1 ? x : quads == 2 ? x / 2 : quads == 3 ? x / 3 : x / 4, r = 4 * (x - nth * quads);
+        uint32_t rest = leads;
+        for (int k = 0; k < nth; ++k) rest &= rest - 1;
+        const int i = __ffs((int)rest) - 1;            // the unit's first piece
+        rest &= rest - 1;
+        const uint32_t run = live & ~((1u << i) - 1) & (rest ? (1u << (__ffs((int)rest) - 1)) - 1 : kAll);
+        // warps that end within the unit, and one at most that ends it and goes on
+        const uint32_t lasts = run & 0xaaaaaaaau, firsts = run & 0x55555555u;
+        float4 so = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (firsts) {
+            const int k = __ffs((int)firsts) - 1;
+            const float4 f = *reinterpret_cast<const float4*>(&s_f.factor[k][r]), y = *reinterpret_cast<const float4*>(first_piece(k >> 1) + d * kR + r);
+            so = make_float4(f.x * y.x, f.y * y.y, f.z * y.z, f.w * y.w);
+        }
+        if (lasts) {
+            const int some = (__ffs((int)lasts) - 1) >> 1;
+#pragma unroll
+            for (int w0 = 0; w0 < kAttnWarps; w0 += 8) {
+                float4 y[8], f[8];
+#pragma unroll
+                for (int w = 0; w < 8; ++w) {          // (no branches: what is not there counts zero times)
+                    const bool in = (lasts >> (2 * (w0 + w) + 1)) & 1u;
+                    const int k = in ? w0 + w : some;
+                    y[w] = *reinterpret_cast<const float4*>(last_piece(k) + d * kR + r);
+                    f[w] = *reinterpret_cast<const float4*>(&s_f.factor[2 * k + 1][r]);
+                    if (!in) f[w] = make_float4(0.f, 0.f, 0.f, 0.f), y[w] = f[w];
                 }
-            if (closed) {
-                put(unit, r, d, top, sl, so);
-            } else {
-                rec[d * kR + r] = so;
-                if (d == 0) rec[D * kR + r] = top, rec[(D + 1) * kR + r] = sl;
+#pragma unroll
+                for (int w = 0; w < 8; ++w) so.x += f[w].x * y[w].x, so.y += f[w].y * y[w].y, so.z += f[w].z * y[w].z, so.w += f[w].w * y[w].w;
             }
         }
-        i = end;
+        const int which = i == open[0] ? 0 : i == open[1] ? 1 : -1;
+        if (which < 0) {
+            put(place_of(s_piece[i].unit), r, d, so, &s_f.l[i][r]);
+        } else {
+            float* rec = C > 1 ? cluster_rec(which) : group_rec(which);
+            *reinterpret_cast<float4*>(rec + d * kR + r) = so;
+            if (d < 2) *reinterpret_cast<float4*>(rec + (D + d) * kR + r) = *reinterpret_cast<const float4*>(d == 0 ? &s_f.m[i][r] : &s_f.l[i][r]);
+        }
     }
-    // ---- units that several CTAs share: the CTA with the last record joins them
+    // ---- units that several stretches share: the CTA with the last record joins them.  A border inside a unit is more than
+    // kAttnSnap tiles away from both its ends, so the stretches that share it follow from the equal shares alone.
+    auto join_stretches = [&]() {
+        const double shares_per_tile = (double)stretches / (double)total;
+        int first_group[2] = {0, 0}, parts[2] = {0, 0};
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            if (open[w] < 0) continue;
+            auto cta_of = [&](int64_t t) {                 // the last CTA whose share begins at or before tile t
+                int c = min(stretches - 1, (int)((double)t * shares_per_tile));
+                while (c + 1 < stretches && share(c + 1) <= t) ++c;
+                while (share(c) > t) --c;
+                return c;
+            };
+            first_group[w] = cta_of(s_piece[open[w]].begin + kAttnSnap);
+            parts[w] = cta_of(s_piece[open[w]].end - kAttnSnap - 1) - first_group[w] + 1;
+        }
+        __syncthreads();
+        if (tid < 2 && open[tid] >= 0) {
+            __threadfence();                               // (the whole CTA's records, which the barrier has ordered before)
+            const uint32_t most = (uint32_t)(tid == 0 ? parts[0] : parts[1]) - 1u;
+            s_last[tid] = atomicInc(&P.arrivals[tid == 0 ? first_group[0] : first_group[1]], most) == most;
+            __threadfence();
+        }
+        __syncthreads();
+        // Factors 2^(m_c - m) of the records and the sum of weights, a warp per head; the outputs, four heads of a channel per thread and as
+        // many records at once as there are threads for (the rings are free by now).
+        float* const s_m = reinterpret_cast<float*>(s_ring_all);               // [kR][stretches], then the factors
+        float* const s_sum = s_m + kR * stretches;                                  // [kR] inverse sums of weights
+        float4* const s_part = reinterpret_cast<float4*>(s_ring_all + kJoinAt);        // [kAttnThreads]
 #pragma unroll 1
-    for (int which = 0; which < 2; ++which) {
-        const int unit = open[which];
-        if (unit < 0) continue;                        // (the same for all threads)
-        const int64_t u0 = unit_begin(unit), u1 = unit_end(unit);
-        auto cta_of = [&](int64_t t) {                 // the CTA whose stretch holds tile t
-            int c = (int)(t * ctas / total);
-            while (cta_begin(c + 1) <= t) ++c;
-            while (cta_begin(c) > t) --c;
-            return c;
-        };
-        const int c0 = cta_of(u0), c1 = cta_of(u1 - 1);
-        __threadfence();
-        __syncthreads();
-        if (tid == 0) s_last = atomicInc(&P.arrivals[c0], (uint32_t)(c1 - c0)) == (uint32_t)(c1 - c0);
-        __syncthreads();
-        if (!s_last) continue;
-        __threadfence();
-        auto record = [&](int c) { return P.cta_rec + ((size_t)c * 2 + (cta_begin(c) <= u0 ? 1 : 0)) * kRec; };
-        for (int e = tid; e < kR * D; e += kAttnThreads) {
-            const int r = e % kR, d = e / kR;
-            float top = kLowest, so = 0.f, sl = 0.f;
-            for (int c = c0; c <= c1; ++c) top = fmaxf(top, __ldcg(record(c) + D * kR + r));
-#pragma unroll 4
-            for (int c = c0; c <= c1; ++c) {
-                const float* p = record(c);
-                const float f = fast_exp2(__ldcg(p + D * kR + r) - top);
-                so += f * __ldcg(p + d * kR + r);
-                sl += f * __ldcg(p + (D + 1) * kR + r);
+        for (int w = 0; w < 2; ++w) {
+            if (open[w] < 0 || !s_last[w]) continue;
+            const int n = parts[w];
+            const Place at = place_of(s_piece[open[w]].unit);
+            // (only the first part begins with the unit)
+            auto record = [&](int i) -> const float* { return P.cta_rec + ((size_t)(first_group[w] + i) * 2 + (i == 0 ? 1 : 0)) * kRec; };
+            const int quads = (at.heads + 3) / 4, vecs = quads * D, at_once = max(1, kAttnThreads / vecs), stride = min(vecs, kAttnThreads);
+            const int part0 = tid / stride;
+            constexpr int kEarly = 16;                     // outputs on their way while the factors are worked out
+            float4 early[kEarly];
+            {
+                const int v = tid - part0 * stride, d = v / quads, r = (v - d * quads) * 4;
+#pragma unroll
+                for (int k = 0; k < kEarly; ++k) {
+                    const int i = part0 + k * at_once;
+                    if (part0 < at_once && i < n) early[k] = __ldcg(reinterpret_cast<const float4*>(record(i) + d * kR + r));
+                }
             }
-            put(unit, r, d, top, sl, so);
+            for (int r = warp; r < at.heads; r += kAttnWarps) {
+                float top = kLowest, sum = 0.f;
+                for (int i0 = lane; i0 < n; i0 += 128) {
+                    float m[4], l[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const bool in = i0 + 32 * k < n;
+                        m[k] = in ? __ldcg(record(i0 + 32 * k) + D * kR + r) : kLowest;
+                        l[k] = in ? __ldcg(record(i0 + 32 * k) + (D + 1) * kR + r) : 0.f;
+                    }
+                    const float now = fmaxf(top, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
+                    sum *= fast_exp2(top - now);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (i0 + 32 * k < n) s_m[r * stretches + i0 + 32 * k] = m[k];
+                        sum += l[k] * fast_exp2(m[k] - now);
+                    }
+                    top = now;
+                }
+                const float all = warp_max(top);
+                sum = warp_sum(sum * fast_exp2(top - all));
+                for (int i0 = lane; i0 < n; i0 += 32) s_m[r * stretches + i0] = fast_exp2(s_m[r * stretches + i0] - all);
+                if (lane == 0) s_sum[r] = inverse(sum), put_lse(at, r, all, sum);
+            }
+            __syncthreads();
+#pragma unroll 1
+            for (int v0 = 0; v0 < vecs; v0 += kAttnThreads) {
+                const int v = v0 + tid - part0 * stride, d = v / quads, r = (v - d * quads) * 4;
+                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+                auto add = [&](int i, const float4& x) {
+                    const float* f = s_m + r * stretches + i;
+                    sum.x += f[0] * x.x;
+                    if (r + 1 < at.heads) sum.y += f[stretches] * x.y;
+                    if (r + 2 < at.heads) sum.z += f[2 * stretches] * x.z;
+                    if (r + 3 < at.heads) sum.w += f[3 * stretches] * x.w;
+                };
+                if (part0 < at_once && v < vecs) {
+                    if (v0 == 0) {
+#pragma unroll
+                        for (int k = 0; k < kEarly; ++k)
+                            if (part0 + k * at_once < n) add(part0 + k * at_once, early[k]);
+                    }
+#pragma unroll 4
+                    for (int i = part0 + (v0 == 0 ? kEarly * at_once : 0); i < n; i += at_once)
+                        add(i, __ldcg(reinterpret_cast<const float4*>(record(i) + d * kR + r)));
+                }
+                if (at_once > 1) {
+                    s_part[tid] = sum;
+                    __syncthreads();
+                    if (part0 == 0)
+                        for (int i = 1; i < at_once; ++i) {
+                            const float4 x = s_part[i * stride + tid];
+                            sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
+                        }
+                }
+                if (part0 == 0 && v < vecs) {
+                    put(at, r, d, sum, s_sum + r);
+                }
+            }
+            __syncthreads();                               // (the factors are read; the next unit's may be written)
         }
+    };
+    if (C > 1) {
+        // ---- units that several CTAs of the cluster share: the first of them adds up, lanes and threads as above
+        cg::cluster_group cluster = cg::this_cluster();
+        cluster.sync();
+#pragma unroll 1
+        for (int w = 0; w < 2; ++w) {
+            if (open[w] < 0) continue;
+            const AttnPiece unit = s_piece[open[w]];
+            const int64_t from = max(unit.begin, lo), to = min(unit.end, hi);
+            if (from < cta_lo) {                       // another CTA's
+                open[w] = -1;
+                continue;
+            }
+            const int part = rank + (lane & 15);       // of this lane
+            const int64_t p0 = cta_border(min(part, C)), p1 = cta_border(min(part + 1, C));
+            const bool in = part < C && p0 < to && p0 < p1;
+            const uint32_t parts = __ballot_sync(0xffffffffu, in) & 0xffffu;
+            auto record = [&](int r) -> const float* { return cluster.map_shared_rank(cluster_rec(r == rank ? w : 0), r); };
+            const bool closed = unit.begin >= lo && unit.end <= hi;
+            const Place at = place_of(unit.unit);
+            for (int r = 2 * warp + (lane >> 4); r < kR; r += 2 * kAttnWarps) {
+                const float* p = record(in ? part : rank) + D * kR + r;
+                const float m = in ? p[0] : kLowest, l = in ? p[kR] : 0.f;
+                float top = m;
+#pragma unroll
+                for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                const float f = in ? fast_exp2(m - top) : 0.f;
+                float sum = f * l;
+#pragma unroll
+                for (int d = 1; d < 16; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                s_f.factor[lane & 15][r] = f;
+                if ((lane & 15) == 0) {
+                    s_f.m[0][r] = top, s_f.l[0][r] = closed ? inverse(sum) : sum;
+                    if (closed) put_lse(at, r, top, sum);
+                }
+            }
+            __syncthreads();
+            for (int e = tid; e < quads * D; e += kAttnThreads) {
+                const int d = e % D, r = 4 * (e / D);
+                float4 so = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int k0 = 0; (parts >> k0) != 0; k0 += 8) {    // eight on their way at a time
+                    float4 y[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) y[k] = *reinterpret_cast<const float4*>(record((parts >> (k0 + k)) & 1u ? rank + k0 + k : rank) + d * kR + r);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        if (!((parts >> (k0 + k)) & 1u)) continue;
+                        const float4 f = *reinterpret_cast<const float4*>(&s_f.factor[k0 + k][r]);
+                        so.x += f.x * y[k].x, so.y += f.y * y[k].y, so.z += f.z * y[k].z, so.w += f.w * y[k].w;
+                    }
+                }
+                if (closed) {
+                    put(at, r, d, so, &s_f.l[0][r]);
+                } else {
+                    float* rec = group_rec(w);
+                    *reinterpret_cast<float4*>(rec + d * kR + r) = so;
+                    if (d < 2) *reinterpret_cast<float4*>(rec + (D + d) * kR + r) = *reinterpret_cast<const float4*>(d == 0 ? &s_f.m[0][r] : &s_f.l[0][r]);
+                }
+            }
+            __syncthreads();
+            if (closed) open[w] = -1;
+        }
+        cluster.sync();                                // (nobody leaves, or uses its rings, while its records may be read)
     }
+    if (open[0] >= 0 || open[1] >= 0) join_stretches();
 }
 
 }  // namespace kvq

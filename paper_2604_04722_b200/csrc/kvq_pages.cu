@@ -26,7 +26,10 @@ bool overlap(const void* a, const void* b, size_t bytes) {
 // What a device allows, asked for once; the kernels' shared-memory limits and cluster sizes are set on the way.
 struct PagesDevice {
     int sm_count = 0;
+    int attn_clusters[4][5] = {};                      // resident clusters of 2^i CTAs, by channels (64, 128) and blocks of heads (1, 2)
 };
+int log2_of(int c) { return c <= 1 ? 0 : 1 + log2_of(c / 2); }
+
 OncePerDevice<PagesDevice> g_device;
 
 template <class Kernel>
@@ -41,6 +44,27 @@ cudaError_t allow_smem(Kernel kernel, bool cluster) {
     return e;
 }
 
+// Both types of a shape are the same to the device; the batch's share of the shared memory is small.
+template <int D, int NT>
+cudaError_t set_up_attn(int (&clusters)[5]) {
+    cudaError_t e = allow_smem(k_page_attn<true, D, NT>, true);
+    if (e == cudaSuccess) e = allow_smem(k_page_attn<false, D, NT>, true);
+    for (int i = 1; i < 5 && e == cudaSuccess; ++i) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(1u << i);
+        cfg.blockDim = dim3(AttnGeom<D>::kThreads);
+        cfg.dynamicSmemBytes = attn_smem<D>(64);
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = 1u << i;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        e = cudaOccupancyMaxActiveClusters(&clusters[i], k_page_attn<false, D, NT>, &cfg);
+    }
+    return e;
+}
+
 const PagesDevice* device_of_call() {
     int device = 0;
     if (cudaGetDevice(&device) != cudaSuccess) return nullptr;
@@ -51,14 +75,10 @@ const PagesDevice* device_of_call() {
         if (err == cudaSuccess) err = allow_smem(k_beam_select<__half>, true);
         if (err == cudaSuccess) err = allow_smem(k_beam_select<__nv_bfloat16>, true);
         if (err == cudaSuccess) err = allow_smem(k_beam_select<float>, true);
-        if (err == cudaSuccess) err = allow_smem(k_page_attn<false, 64, 1>, false);
-        if (err == cudaSuccess) err = allow_smem(k_page_attn<false, 64, 2>, false);
-        if (err == cudaSuccess) err = allow_smem(k_page_attn<false, 128, 1>, false);
-        if (err == cudaSuccess) err = allow_smem(k_page_attn<false, 128, 2>, false);
-        if (err == cudaSuccess) err = allow_smem(k_page_attn<true, 64, 1>, false);
-        if (err == cudaSuccess) err = allow_smem(k_page_attn<true, 64, 2>, false);
-        if (err == cudaSuccess) err = allow_smem(k_page_attn<true, 128, 1>, false);
-        if (err == cudaSuccess) err = allow_smem(k_page_attn<true, 128, 2>, false);
+        if (err == cudaSuccess) err = set_up_attn<64, 1>(d.attn_clusters[0]);
+        if (err == cudaSuccess) err = set_up_attn<64, 2>(d.attn_clusters[1]);
+        if (err == cudaSuccess) err = set_up_attn<128, 1>(d.attn_clusters[2]);
+        if (err == cudaSuccess) err = set_up_attn<128, 2>(d.attn_clusters[3]);
         return err;
     });
     if (e != cudaSuccess) cudaGetLastError();          // (reported by the call's return code)
@@ -97,17 +117,18 @@ bool cache_ok(const kvq_page_cache* c) {
 }
 
 // Resident CTAs of the attention, and what it keeps in the workspace: arrival counters, then two kinds of records.
+int attn_warps(int head_dim) { return head_dim == 64 ? AttnGeom<64>::kWarps : AttnGeom<128>::kWarps; }
 struct AttnSpace {
     int ctas, nt;
     size_t record, warp_at, cta_at, bytes;
 };
 AttnSpace attn_space(int sm_count, int group, int head_dim) {
     AttnSpace s;
-    s.ctas = std::min(kAttnMaxCtas, sm_count * (head_dim == 64 ? 2 : 1));
+    s.ctas = std::min(kAttnMaxCtas, sm_count);
     s.nt = group <= 8 ? 1 : 2;
     s.record = (size_t)8 * s.nt * (head_dim + 2) * sizeof(float);
     s.warp_at = (size_t)kAttnMaxCtas * sizeof(uint32_t);
-    s.cta_at = s.warp_at + (size_t)s.ctas * kAttnWarps * s.record;
+    s.cta_at = s.warp_at + (size_t)s.ctas * attn_warps(head_dim) * s.record;
     s.bytes = s.cta_at + (size_t)s.ctas * 2 * s.record;
     return s;
 }
@@ -118,7 +139,7 @@ bool attn_shape_ok(int batch, int q_heads, int kv_heads, int head_dim) {
 
 template <bool BF, int D, int NT>
 int launch_attn(const PageAttnParams& p, uint64_t ctas, void* stream) {
-    return launch(k_page_attn<BF, D, NT>, ctas, kAttnThreads, attn_smem<D>(p.batch), 0, p, stream);
+    return launch(k_page_attn<BF, D, NT>, ctas, AttnGeom<D>::kThreads, attn_smem<D>(p.batch), p.cluster > 1 ? p.cluster : 0, p, stream);
 }
 
 }  // namespace
@@ -241,9 +262,15 @@ int kvq_page_attn(const kvq_page_cache* cache, const void* Q, void* O, float* ls
     p.head_blocks = (p.group + 8 * space.nt - 1) / (8 * space.nt);
     p.scale2 = scale * kLog2e;
     p.by_page = FastDiv((uint32_t)cache->page_size);
-    // as many CTAs as the tables could give a tile to every warp of, as far as they are resident together
-    const double tiles = std::ceil((double)table_width * cache->page_size / kAttnTile) * batch * p.kv_heads * p.head_blocks;
-    const uint64_t ctas = (uint64_t)std::max(1.0, std::min((double)space.ctas, std::ceil(tiles / kAttnWarps)));
+    // Clusters as wide as leaves one for every unit, with two tiles for every warp of the longest that the table could hold;
+    // as many CTAs as the tables could give a tile to every warp of, as far as they are resident together.
+    const double units = (double)batch * p.kv_heads * p.head_blocks, longest = std::ceil((double)table_width * cache->page_size / kAttnTile);
+    const int warps = attn_warps(D), which = (D == 64 ? 0 : 2) + space.nt - 1;
+    p.cluster = 1;
+    while (p.cluster < kAttnMaxCluster && longest >= 2.0 * warps * (2 * p.cluster) && units <= d->attn_clusters[which][log2_of(2 * p.cluster)]) p.cluster *= 2;
+    const uint64_t most = p.cluster > 1 ? (uint64_t)d->attn_clusters[which][log2_of(p.cluster)] * p.cluster : (uint64_t)space.ctas;
+    const double wanted = std::max(units, std::ceil(units * longest / (warps * p.cluster))) * p.cluster;
+    const uint64_t ctas = (uint64_t)std::max((double)p.cluster, std::min((double)std::min<uint64_t>(most, space.ctas) / p.cluster * p.cluster, wanted));
     if (cache->dtype == KVQ_BF16) {
         if (D == 64) return space.nt == 1 ? launch_attn<true, 64, 1>(p, ctas, stream) : launch_attn<true, 64, 2>(p, ctas, stream);
         return space.nt == 1 ? launch_attn<true, 128, 1>(p, ctas, stream) : launch_attn<true, 128, 2>(p, ctas, stream);
@@ -285,9 +312,10 @@ int kvq_beam_select(const void* logits, int dtype, const float* scores, const ui
     p.slices = std::max(1, std::min(ctas * kBeamWarps / beams, (vocab + kBeamChunk - 1) / kBeamChunk));
     p.slice_len = (int)((((int64_t)vocab + p.slices - 1) / p.slices + 255) / 256 * 256);
     const uint64_t grid = (uint64_t)batch * ctas;
-    if (dtype == KVQ_FP32) return launch(k_beam_select<float>, grid, kBeamThreads, beam_smem(n_out), ctas, p, stream);
-    if (dtype == KVQ_BF16) return launch(k_beam_select<__nv_bfloat16>, grid, kBeamThreads, beam_smem(n_out), ctas, p, stream);
-    return launch(k_beam_select<__half>, grid, kBeamThreads, beam_smem(n_out), ctas, p, stream);
+    const size_t smem = beam_smem((beams * p.slices + ctas * kBeamWarps - 1) / (ctas * kBeamWarps), n_out);
+    if (dtype == KVQ_FP32) return launch(k_beam_select<float>, grid, kBeamThreads, smem, ctas, p, stream);
+    if (dtype == KVQ_BF16) return launch(k_beam_select<__nv_bfloat16>, grid, kBeamThreads, smem, ctas, p, stream);
+    return launch(k_beam_select<__half>, grid, kBeamThreads, smem, ctas, p, stream);
 }
 
 }  // extern "C"

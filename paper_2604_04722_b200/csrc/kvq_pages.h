@@ -63,6 +63,7 @@ struct PageAttnParams {
     float* warp_rec;               // [CTAs][warps] records of R (D + 2) floats
     float* cta_rec;                // [CTAs][2] records
     int width, batch, n_pages, page_size, q_heads, kv_heads, group, head_blocks;
+    int cluster;                   // CTAs that share a stretch of the axis and meet through shared memory (1: no clusters)
     float scale2;                  // softmax scale in log2 units
     FastDiv by_page;
 };
