@@ -1,20 +1,22 @@
 // One step of beam search: of all candidates (beam w, token v) with the score  s_w + z_wv - log sum_u exp(z_wu)  the n best,
 // ties to the lowest (w, v).
 //
-// A cluster of CTAs serves a request, and reads its logits once.  Every row is cut into slices, one warp each; the cut does not
-// depend on the row or its address, so that equal rows have equal sums and tie as they should.  A warp keeps, over its slice, the
-// largest logit and the sum of exponentials (fp32 within 16 entries of a lane, fp64 beyond: what is compared between beams
-// must not depend on their order), and the entries that can still be among the n best of the row: those above a
-// threshold, which starts as the n-th largest of the 32 lanes' maxima (n entries are at least as large, so nothing smaller can
-// be among the n best) and rises whenever the buffer is full and cut back to its n best.  After the first 512 entries hardly any logit
-// passes, so the loop is one exponential and a comparison per entry.
+// A cluster of CTAs serves a request.  Every row is cut into slices, one warp each; the cut does not depend on the row or its
+// address, so that equal rows have equal sums and tie as they should.  Reading its slice, a warp keeps nothing but the sum of
+// exponentials (fp32 within 16 entries of a lane, fp64 beyond: what is compared between beams must not depend on their order)
+// and the largest entry of every group of chunks: one exponential, a maximum and two or three more instructions per logit.
 //
-// Then the slices' sums are exchanged (one cluster barrier), every CTA merges its warps' sorted lists to its n best, a warp per CTA, by score in
-// fp64, and the first CTA merges those.  Bound: the logits' bytes for many requests; for few of them the chain of the
-// row's loads, two cluster barriers and two merges.
+// The slices' sums are exchanged (a cluster barrier).  Then the scores of the groups' largest entries are known, and the n-th
+// best of a CTA's bounds its n best candidates from below: only groups whose largest entry reaches it are read again, and of
+// those only the entries that reach it are kept, a few more than n in all.  A CTA ranks its own, sends its n best to the first
+// CTA (a second barrier), and that ranks them.  Scores are compared in fp64.
+//
+// Bound: the logits' bytes for many requests; for few of them the chain of the rows' loads, two cluster barriers, the
+// bound and a second read.
 #pragma once
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
+#include <cfloat>
 #include <type_traits>
 #include "kvq_common.cuh"
 #include "kvq_pages.h"
@@ -26,16 +28,12 @@ constexpr int kBeamThreads = 512, kBeamWarps = kBeamThreads / 32;
 constexpr int kBeamMaxCluster = 16;
 constexpr int kBeamChunk = 512;                        // entries that a warp works on at a time, 16 per lane
 constexpr int kBeamBuffer = 128;                       // entries of a warp's buffer, 4 per lane: at least n + 32
-constexpr int kBeamTasks = (kMaxBeams + kBeamWarps - 1) / kBeamWarps;      // slices of a warp at most
+constexpr int kBeamTasks = (kMaxBeams + kBeamWarps - 1) / kBeamWarps;      // slices of a warp at most: where there are more rows than warps
 constexpr int kBeamMaxSlices = kBeamMaxCluster * kBeamWarps;
-constexpr float kBeamLowest = -3.402823466e38f;
+constexpr int kBeamGroups = 16;                        // groups of chunks of a warp's slices at most
+constexpr float kBeamLowest = -FLT_MAX;
 
-// Order-preserving 32-bit keys of logits (-0 counts as 0); no logit has the key 0.
-__device__ __forceinline__ uint32_t logit_key(float x) {
-    const uint32_t b = __float_as_uint(x + 0.f);
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-__device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+// Order-preserving keys of scores (-0 counts as 0); none is 0 or the largest number.
 __device__ __forceinline__ uint64_t score_key(double x) {
     const uint64_t b = (uint64_t)__double_as_longlong(x + 0.0);
     return b >> 63 ? ~b : b | (1ull << 63);
@@ -44,71 +42,107 @@ __device__ __forceinline__ double key_score(uint64_t k) {
     return __longlong_as_double((long long)(k >> 63 ? k ^ (1ull << 63) : ~k));
 }
 
-struct BeamEntry {
-    uint32_t key, token;                               // logit (0: none)
-};
+// A candidate: its score (score_key; 0: none) and its place.
 struct BeamPick {
-    uint64_t score;                                    // score_key
+    uint64_t score;
     uint32_t row, token;
     __device__ bool before(const BeamPick& o) const {
         return score != o.score ? score > o.score : row != o.row ? row < o.row : token < o.token;
     }
 };
+__device__ __forceinline__ BeamPick no_pick() { return BeamPick{0, 0xffffffffu, 0xffffffffu}; }
 
-// Dynamic shared memory: the buffers of a CTA's slices, and in every CTA room for the picks that are left over (those of the
-// first CTA are used): of n slices at most n + 32 each.
-__host__ __device__ constexpr int beam_max_picks(int n) { return n * (n + 32); }
-inline size_t beam_smem(int tasks, int n) {
-    return (size_t)kBeamWarps * tasks * kBeamBuffer * sizeof(BeamEntry) + (size_t)beam_max_picks(n) * sizeof(BeamPick);
-}
+// Dynamic shared memory: the warps' buffers, the CTA's picks and, in the first CTA, those of all CTAs.
+inline size_t beam_smem(int n) { return ((size_t)kBeamWarps * kBeamBuffer + kBeamThreads + (size_t)kBeamMaxCluster * n) * sizeof(BeamPick); }
 
-// Cuts a warp's buffer back to its n best entries, in order (value descending, token ascending); it holds n or more.
-__device__ __noinline__ void warp_best(BeamEntry* buffer, int count, int n) {
+// Cuts a warp's buffer back to its n best entries, in order; it holds n or more.
+__device__ __noinline__ void warp_best(BeamPick* buffer, int count, int n) {
     const int lane = threadIdx.x & 31;
-    BeamEntry e[kBeamBuffer / 32];
+    BeamPick e[kBeamBuffer / 32];
 #pragma unroll
-    for (int k = 0; k < kBeamBuffer / 32; ++k) {
-        e[k].key = 0, e[k].token = 0xffffffffu;
-        if (lane + 32 * k < count) e[k] = buffer[lane + 32 * k];
-    }
+    for (int k = 0; k < kBeamBuffer / 32; ++k) e[k] = lane + 32 * k < count ? buffer[lane + 32 * k] : no_pick();
     __syncwarp();
 #pragma unroll 1
     for (int i = 0; i < n; ++i) {
-        uint32_t key = 0, token = 0xffffffffu;
+        BeamPick best = e[0];
+#pragma unroll
+        for (int k = 1; k < kBeamBuffer / 32; ++k)
+            if (e[k].before(best)) best = e[k];
+        const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(best.score >> 32));
+        bool in = (uint32_t)(best.score >> 32) == hi;
+        const uint32_t lo = __reduce_max_sync(0xffffffffu, in ? (uint32_t)best.score : 0u);
+        in = in && (uint32_t)best.score == lo;
+        const uint32_t row = __reduce_min_sync(0xffffffffu, in ? best.row : 0xffffffffu);
+        in = in && best.row == row;
+        const uint32_t token = __reduce_min_sync(0xffffffffu, in ? best.token : 0xffffffffu);
+        in = in && best.token == token;
 #pragma unroll
         for (int k = 0; k < kBeamBuffer / 32; ++k)
-            if (e[k].key > key || (e[k].key == key && e[k].token < token)) key = e[k].key, token = e[k].token;
-        const uint32_t best = __reduce_max_sync(0xffffffffu, key);
-        const uint32_t at = __reduce_min_sync(0xffffffffu, key == best ? token : 0xffffffffu);
-#pragma unroll
-        for (int k = 0; k < kBeamBuffer / 32; ++k)
-            if (e[k].key == best && e[k].token == at) e[k].key = 0, e[k].token = 0xffffffffu;
-        if (lane == 0) buffer[i].key = best, buffer[i].token = at;
+            if (in && e[k].row == row && e[k].token == token) e[k] = no_pick();
+        if (lane == 0) buffer[i] = BeamPick{((uint64_t)hi << 32) | lo, row, token};
     }
     __syncwarp();
 }
 
-// Eight (16-bit) or four (fp32) neighbouring entries of a row as they lie in memory, from any address that is a multiple of
-// their size: two aligned 16-byte loads and a shift where the row is not aligned.  Bytes outside [begin, end) are not read.
-template <class T>
-__device__ __forceinline__ uint4 load_entries(const T* src, const void* begin, const void* end) {
-    const uintptr_t a = reinterpret_cast<uintptr_t>(src);
-    const uint32_t off = (uint32_t)(a & 15u);
-    if (off == 0 && a + 16 <= reinterpret_cast<uintptr_t>(end)) return __ldg(reinterpret_cast<const uint4*>(src));
-    const uint4* p = reinterpret_cast<const uint4*>(a - off);
-    if (reinterpret_cast<uintptr_t>(p) >= reinterpret_cast<uintptr_t>(begin) && reinterpret_cast<uintptr_t>(p + 2) <= reinterpret_cast<uintptr_t>(end)) {
-        const uint4 u = __ldg(p), w = __ldg(p + 1);
-        uint32_t x0 = u.x, x1 = u.y, x2 = u.z, x3 = u.w, x4 = w.x, x5 = w.y, x6 = w.z;
-        if (off & 8u) x0 = x2, x1 = x3, x2 = x4, x3 = x5, x4 = x6, x5 = w.w;
-        if (off & 4u) x0 = x1, x1 = x2, x2 = x3, x3 = x4, x4 = x5;
-        const uint32_t bits = (off & 3u) * 8u;
-        return make_uint4(__funnelshift_r(x0, x1, bits), __funnelshift_r(x1, x2, bits), __funnelshift_r(x2, x3, bits), __funnelshift_r(x3, x4, bits));
+// A score that n of a warp's candidates (0: none, K per lane) reach, and few more: distances from the best one in steps of 2^-10,
+// the smallest number of steps that n of them keep within, one bit after the other.  0: fewer than n within 64.
+template <int K>
+__device__ __forceinline__ uint64_t warp_bound(const uint64_t (&mine)[K], int n) {
+    uint64_t top = mine[0];
+#pragma unroll
+    for (int k = 1; k < K; ++k) top = mine[k] > top ? mine[k] : top;
+    const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(top >> 32));
+    const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(top >> 32) == hi ? (uint32_t)top : 0u);
+    const double best = key_score(((uint64_t)hi << 32) | lo);
+    uint32_t left[K];                                  // 2^16 - 1 less the steps; 0: farther away, or none
+#pragma unroll
+    for (int k = 0; k < K; ++k) left[k] = mine[k] ? 65535u - (uint32_t)fmin((best - key_score(mine[k])) * 1024.0, 65535.0) : 0u;
+    uint32_t prefix = 0;
+#pragma unroll 1
+    for (int bit = 15; bit >= 0; --bit) {
+        const uint32_t next = prefix | (1u << bit);
+        int reach = 0;
+#pragma unroll
+        for (int k = 0; k < K; ++k) reach += left[k] >= next;
+        if (__reduce_add_sync(0xffffffffu, reach) >= n) prefix = next;
     }
+    return prefix == 0 ? 0ull : score_key(best - (double)(65537u - prefix) * (1.0 / 1024.0));      // (one step for the roundings)
+}
+
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 r;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 r;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+
+// Eight (16-bit) or four (fp32) neighbouring entries of a row as they lie in memory, `off` bytes (the same for a whole row)
+// behind a 16-byte border: two aligned loads and a shift where the row is not aligned.
+__device__ __forceinline__ uint4 load_shifted(const uint4* p, uint32_t off) {
+    const uint4 u = __ldg(p);
+    if (off == 0) return u;
+    const uint4 w = __ldg(p + 1);
+    uint32_t x0 = u.x, x1 = u.y, x2 = u.z, x3 = u.w, x4 = w.x, x5 = w.y, x6 = w.z;
+    if (off & 8u) x0 = x2, x1 = x3, x2 = x4, x3 = x5, x4 = x6, x5 = w.w;
+    if (off & 4u) x0 = x1, x1 = x2, x2 = x3, x3 = x4, x4 = x5;
+    const uint32_t bits = (off & 3u) * 8u;
+    return make_uint4(__funnelshift_r(x0, x1, bits), __funnelshift_r(x1, x2, bits), __funnelshift_r(x2, x3, bits), __funnelshift_r(x3, x4, bits));
+}
+// The same one by one, for the ends of the tensor: `n` entries, the rest is zero.
+template <class T>
+__device__ __noinline__ uint4 load_few(const T* src, int n) {
     constexpr int kN = 16 / sizeof(T);
     uint32_t out[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {                     // at the ends of the tensor: one by one
-        if (reinterpret_cast<uintptr_t>(src + i + 1) > reinterpret_cast<uintptr_t>(end)) break;
+    for (int i = 0; i < kN; ++i) {
+        if (i >= n) break;
         if constexpr (sizeof(T) == 2) out[i / 2] |= (uint32_t)(*reinterpret_cast<const uint16_t*>(src + i)) << (16 * (i & 1));
         else out[i] = *reinterpret_cast<const uint32_t*>(src + i);
     }
@@ -133,10 +167,6 @@ __device__ __forceinline__ void widen(const uint4& v, float* x) {
     }
 }
 
-__device__ __forceinline__ float widen_one(float x) { return x; }
-__device__ __forceinline__ float widen_one(__half x) { return __half2float(x); }
-__device__ __forceinline__ float widen_one(__nv_bfloat16 x) { return __bfloat162float(x); }
-
 // grid = batch clusters, block = kBeamThreads.
 template <class T>
 __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParams P) {
@@ -148,138 +178,124 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
     constexpr int kVec = 16 / (int)sizeof(T), kLoads = 16 / kVec;          // entries of a load, loads of a lane per chunk
     __shared__ float s_top[kBeamMaxSlices];            // of all slices of the request: largest logit ...
     __shared__ double s_sum[kBeamMaxSlices];           // ... and sum of exponentials relative to it
-    __shared__ uint64_t s_best[kBeamMaxSlices];        // by row, then slice: score of that logit, 0 for a slice without candidates
-    __shared__ uint8_t s_in[kBeamMaxSlices];           // ... and whether it is among the n best
     __shared__ float s_row_top[kMaxBeams];
     __shared__ double s_row_off[kMaxBeams];            // score - log of the sum
     __shared__ uint8_t s_alive[kMaxBeams];
-    __shared__ int s_count[kBeamWarps * kBeamTasks];
-    __shared__ uint64_t s_least;
-    __shared__ int s_picked;                           // (of the first CTA)
+    __shared__ float s_group_top[kBeamWarps * kBeamGroups];
+    __shared__ uint64_t s_group_best[kBeamWarps * kBeamGroups];            // score of that logit, 0 without candidates
+    __shared__ uint64_t s_bound;
+    __shared__ int s_picked, s_listed, s_counts[kBeamWarps];
+    __shared__ uint16_t s_list[kBeamThreads];
     extern __shared__ __align__(16) uint8_t s_dyn[];
     const int n = P.n_out;
     const int tasks = P.beams * P.slices, warps = ctas * kBeamWarps, gwarp = rank * kBeamWarps + warp;
     const int rounds = (tasks + warps - 1) / warps;    // slices of a warp, at most kBeamTasks
-    BeamPick* s_picks = reinterpret_cast<BeamPick*>(s_dyn);
-    BeamEntry* s_buffers = reinterpret_cast<BeamEntry*>(s_picks + beam_max_picks(n));      // [warps * rounds][kBeamBuffer]
-    if (tid == 0) s_picked = 0, s_least = 0;
+    const int per_slice = kBeamGroups / rounds;        // groups
+    const int group_len = ((P.slice_len + kBeamChunk * per_slice - 1) / (kBeamChunk * per_slice)) * kBeamChunk;        // entries
+    BeamPick* s_buffers = reinterpret_cast<BeamPick*>(s_dyn);              // [warps][kBeamBuffer]
+    BeamPick* s_picks = s_buffers + kBeamWarps * kBeamBuffer;              // [threads]
+    BeamPick* s_sent = s_picks + kBeamThreads;                             // [CTAs][n]
+    if (tid == 0) s_picked = s_listed = 0;
+    if (tid < kBeamWarps * kBeamGroups) s_group_top[tid] = -INFINITY;
+    static_assert(kBeamWarps * kBeamGroups <= kBeamThreads, "a thread per group");
+    __syncthreads();
 
     cluster.barrier_arrive();                          // (before another CTA's memory is written, all of them have to be there)
     pdl_launch_dependents();
     pdl_wait();
 
+    // a warp's view of a slice: whole vectors, if they lie within the tensor
+    struct Slice {
+        int lo, hi;
+        const T* z;
+        const uint4* vecs;
+        uint32_t off;
+        bool inside;
+    };
+    auto slice_of = [&](int task) {
+        Slice v;
+        const int row = task % P.beams, slice = task / P.beams;
+        v.lo = (int)min((long long)slice * P.slice_len, (long long)P.vocab);
+        v.hi = (int)min((long long)v.lo + P.slice_len, (long long)P.vocab);
+        v.z = static_cast<const T*>(P.logits) + ((size_t)b * P.beams + row) * (size_t)P.vocab;
+        const uintptr_t at = reinterpret_cast<uintptr_t>(v.z);
+        v.off = (uint32_t)(at & 15u);
+        v.vecs = reinterpret_cast<const uint4*>(at - v.off);
+        v.inside = reinterpret_cast<uintptr_t>(v.vecs + v.lo / kVec) >= reinterpret_cast<uintptr_t>(P.logits) &&
+                   reinterpret_cast<uintptr_t>(v.vecs + (v.hi + kVec - 1) / kVec + (v.off ? 1 : 0)) <= reinterpret_cast<uintptr_t>(P.logits_end);
+        return v;
+    };
+    auto load = [&](const Slice& v, int c0, uint4 (&raw)[kLoads]) {
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+            const int t = c0 + (k * 32 + lane) * kVec;
+            if (t < v.hi) raw[k] = v.inside ? load_shifted(v.vecs + t / kVec, v.off) : load_few<T>(v.z + t, P.vocab - t);
+        }
+    };
+    auto values = [&](const Slice& v, int c0, const uint4 (&raw)[kLoads], float (&x)[16]) {
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) widen<T>(raw[k], x + k * kVec);
+        if (c0 + kBeamChunk > v.hi) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                if (c0 + ((k / kVec) * 32 + lane) * kVec + k % kVec >= v.hi) x[k] = -INFINITY;
+        }
+    };
 #pragma unroll 1
     for (int j = 0, task = gwarp; j < rounds; ++j, task += warps) {
         float top = kBeamLowest;
         double sum = 0.0;
-        int count = 0;
-        BeamEntry* buffer = s_buffers + (warp * rounds + j) * kBeamBuffer;
         if (task < tasks) {
-            const int row = task % P.beams, slice = task / P.beams;
+            const int row = task % P.beams;
             const size_t r = (size_t)b * P.beams + row;
+            float* groups = s_group_top + warp * kBeamGroups + j * per_slice;
+            const Slice v = slice_of(task);
+            uint4 raw[kLoads];
+            load(v, v.lo, raw);                        // (of rows that are out no more than this is read)
             const bool over = P.finished && P.finished[r] != 0, alive = isfinite(P.scores[r]);
             if (over) {                                // one candidate: the end token at the score as it is
-                if (slice == 0) {
-                    if (lane == 0) buffer[0].key = logit_key(0.f), buffer[0].token = (uint32_t)P.end_token;
-                    count = 1;
-                    top = 0.f;
-                    sum = 1.0;
-                }
+                if (task < P.beams) top = 0.f, sum = lane == 0 ? 1.0 : 0.0, groups[0] = 0.f;
             } else if (alive) {
-                const int lo = min((long long)slice * P.slice_len, (long long)P.vocab), hi = min((long long)lo + P.slice_len, (long long)P.vocab);
-                const T* z = static_cast<const T*>(P.logits) + r * (size_t)P.vocab;
-                // threshold: an entry stays in the running if it is larger, or as large and its token is below `above`
-                float least = -INFINITY;
-                uint32_t above = 0, chunk = 0;
-                uint4 raw[kLoads];
-                auto load = [&](int c0) {
-#pragma unroll
-                    for (int k = 0; k < kLoads; ++k) {
-                        const int v = c0 + (k * 32 + lane) * kVec;
-                        if (v < hi) raw[k] = load_entries<T>(z + v, P.logits, P.logits_end);
-                    }
-                };
-                load(lo);
+                float most = -INFINITY;
+                int g = 0, next = v.lo + group_len;
 #pragma unroll 1
-                for (int c0 = lo; c0 < hi; c0 += kBeamChunk) {
+                for (int c0 = v.lo; c0 < v.hi; c0 += kBeamChunk) {
                     float x[16];
+                    values(v, c0, raw, x);
+                    load(v, c0 + kBeamChunk, raw);     // (on their way while this chunk is worked on)
+                    float here = x[0];
 #pragma unroll
-                    for (int k = 0; k < kLoads; ++k) widen<T>(raw[k], x + k * kVec);
-                    if (c0 + kBeamChunk > hi) {
-#pragma unroll
-                        for (int k = 0; k < 16; ++k)
-                            if (c0 + ((k / kVec) * 32 + lane) * kVec + k % kVec >= hi) x[k] = -INFINITY;
+                    for (int k = 1; k < 16; ++k) here = fmaxf(here, x[k]);
+                    if (here > top) {
+                        sum *= (double)fast_exp2((top - here) * kLog2e);
+                        top = here;
                     }
-                    load(c0 + kBeamChunk);             // (on their way while this chunk is worked on)
-                    float most = x[0];
+                    // (x - top) log2 e: the difference first, so that the type's lowest value next to itself is zero, and what is near
+                    // the largest loses nothing
+                    float2 part = make_float2(0.f, 0.f);
 #pragma unroll
-                    for (int k = 1; k < 16; ++k) most = fmaxf(most, x[k]);
-                    if (most > top) {
-                        sum *= (double)fast_exp2((top - most) * kLog2e);
-                        top = most;
+                    for (int k = 0; k < 16; k += 2) {
+                        const float2 t = mul2(add2(make_float2(x[k], x[k + 1]), make_float2(-top, -top)), make_float2(kLog2e, kLog2e));
+                        part = add2(part, make_float2(fast_exp2(t.x), fast_exp2(t.y)));
                     }
-                    float part = 0.f;
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) part += fast_exp2((x[k] - top) * kLog2e);
-                    sum += (double)part;
-                    ++chunk;
-                    if ((chunk & (chunk - 1)) == 0) {  // the n-th largest of the lanes' maxima so far: a bitonic sort, descending
-                        float v = top;
-#pragma unroll
-                        for (int size = 2; size <= 32; size <<= 1)
-#pragma unroll
-                            for (int d = size >> 1; d > 0; d >>= 1) {
-                                const float o = __shfl_xor_sync(0xffffffffu, v, d);
-                                const bool keep_max = ((lane & d) == 0) == ((lane & size) == 0);
-                                v = keep_max ? fmaxf(v, o) : fminf(v, o);
-                            }
-                        v = __shfl_sync(0xffffffffu, v, n - 1);
-                        if (v > least) least = v, above = 0xffffffffu;
-                    }
-                    if (!__any_sync(0xffffffffu, most >= least)) continue;
-                    uint32_t hits = 0;                 // entries of this lane that may stay
-#pragma unroll
-                    for (int k = 0; k < 16; ++k)
-                        if (x[k] >= least) hits |= 1u << k;
-                    for (;;) {                         // one of every lane at a time, read again
-                        const int k = __ffs((int)hits) - 1;
-                        const uint32_t v = (uint32_t)(c0 + (k / kVec * 32 + lane) * kVec + k % kVec);
-                        const float z_v = k >= 0 ? widen_one(z[v]) : 0.f;
-                        bool mine = k >= 0 && (z_v > least || (z_v == least && v < above));
-                        uint32_t in = __ballot_sync(0xffffffffu, mine);
-                        if (count + __popc(in) > kBeamBuffer) {
-                            __syncwarp();
-                            warp_best(buffer, count, n);
-                            count = n;                 // (at least n + 1 were in it)
-                            least = key_logit(buffer[n - 1].key);
-                            above = buffer[n - 1].token;
-                            mine = mine && (z_v > least || (z_v == least && v < above));
-                            in = __ballot_sync(0xffffffffu, mine);
-                        }
-                        if (mine) {
-                            BeamEntry& e = buffer[count + __popc(in & ((1u << lane) - 1))];
-                            e.key = logit_key(z_v);
-                            e.token = v;
-                        }
-                        count += __popc(in);
-                        hits &= hits - 1;
-                        if (!__any_sync(0xffffffffu, hits != 0)) break;
+                    sum += (double)(part.x + part.y);
+                    most = fmaxf(most, here);
+                    if (c0 + kBeamChunk >= min(next, v.hi)) {
+                        most = warp_max(most);
+                        if (lane == 0) groups[g] = most;
+                        ++g;
+                        next += group_len;
+                        most = -INFINITY;
                     }
                 }
                 // the lanes' sums relative to the slice's largest
                 const float all = warp_max(top);
-                sum *= exp((double)top - (double)all);
+                sum *= (double)fast_exp2((top - all) * kLog2e);
                 top = all;
-#pragma unroll
-                for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
             }
-            __syncwarp();
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         }
-        if (count > n + 32) {
-            warp_best(buffer, count, n);
-            count = n;
-        }
-        if (lane == 0) s_count[warp * rounds + j] = count;
         if (j == 0) cluster.barrier_wait();
         if (task < tasks && lane < ctas) {
             cluster.map_shared_rank(s_top, lane)[task] = top;
@@ -305,60 +321,155 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
         }
     }
     __syncthreads();
-    // ---- a bound: the n-th best of the slices' largest entries (every CTA for itself; ties by row and slice, which is their
-    // candidates' order).  n candidates are at least as good, so neither what is worse nor any other slice holds one of the n best.
-    for (int t = tid; t < tasks; t += kBeamThreads) {
-        const int row = t % P.beams;
-        const bool some = s_alive[row] && s_sum[t] > 0.0;
-        s_best[row * P.slices + t / P.beams] = some ? score_key(s_row_off[row] + ((double)s_top[t] - (double)s_row_top[row])) : 0ull;
+    // ---- a bound: the n-th best of the CTA's groups' largest entries, which n of its candidates reach
+    uint64_t best = 0;                                 // of this thread's group
+    if (tid < kBeamWarps * kBeamGroups) {
+        const int w = tid / kBeamGroups, j = tid % kBeamGroups / per_slice, task = rank * kBeamWarps + w + j * warps, row = task % P.beams;
+        const float top = s_group_top[tid];
+        if (j < rounds && task < tasks && s_alive[row] && top > -INFINITY) best = score_key(s_row_off[row] + ((double)top - (double)s_row_top[row]));
+        s_group_best[tid] = best;
     }
     __syncthreads();
-    for (int t = tid; t < tasks; t += kBeamThreads) {
-        const uint64_t mine = s_best[t];
-        int better = 0;
-        for (int o = 0; o < tasks; ++o) better += s_best[o] > mine || (s_best[o] == mine && o < t);
-        s_in[t] = better < n;
-        if (better == n - 1) s_least = mine;
+    if (warp == 0) {
+        uint64_t some[kBeamWarps * kBeamGroups / 32];
+#pragma unroll
+        for (int k = 0; k < kBeamWarps * kBeamGroups / 32; ++k) some[k] = s_group_best[32 * k + lane];
+        const uint64_t of_groups = warp_bound(some, n);
+        if (lane == 0) s_bound = of_groups;
     }
     __syncthreads();
-    // ---- the candidates that reach it go to the first CTA ...
+    const uint64_t bound = s_bound;
+    if (best != 0 && best >= bound) s_list[atomicAdd(&s_listed, 1)] = (uint16_t)tid;
+    __syncthreads();
+    // ---- the groups that reach it are read again, one warp each, and the entries that reach it kept; more than n of a warp never
+    // count
     {
-        const uint64_t least = s_least;
-        BeamPick* to = cluster.map_shared_rank(s_picks, 0);
-        int* picked = cluster.map_shared_rank(&s_picked, 0);
-        for (int j = 0, task = gwarp; j < rounds && task < tasks; ++j, task += warps) {
-            const int row = task % P.beams, count = s_count[warp * rounds + j];
-            if (!s_alive[row] || !s_in[row * P.slices + task / P.beams]) continue;
-            for (int i = lane; i < count; i += 32) {
-                const BeamEntry e = s_buffers[(warp * rounds + j) * kBeamBuffer + i];
-                BeamPick p;
-                p.score = score_key(s_row_off[row] + ((double)key_logit(e.key) - (double)s_row_top[row]));
-                p.row = (uint32_t)row;
-                p.token = e.token;
-                if (p.score < least) continue;
-                const int at = atomicAdd(picked, 1);
-                if (at < beam_max_picks(n)) to[at] = p;
+        BeamPick* buffer = s_buffers + warp * kBeamBuffer;
+        BeamPick worst = no_pick();                    // once the buffer was full: what has to be beaten
+        int count = 0;
+        {
+            const int listed = s_listed;
+#pragma unroll 1
+            for (int i = warp; i < listed; i += kBeamWarps) {
+                const int group = s_list[i], j = group % kBeamGroups / per_slice;
+                const int task = rank * kBeamWarps + group / kBeamGroups + j * warps, row = task % P.beams;
+                const double off = s_row_off[row];
+                const float row_top = s_row_top[row];
+                auto score_of = [&](float x) { return score_key(off + ((double)x - (double)row_top)); };
+                auto keep = [&](bool mine_in, BeamPick p) {
+                    uint32_t in = __ballot_sync(0xffffffffu, mine_in);
+                    if (count + __popc(in) > kBeamBuffer) {
+                        __syncwarp();
+                        warp_best(buffer, count, n);
+                        count = n;                     // (at least n + 1 were in it)
+                        worst = buffer[n - 1];
+                        mine_in = mine_in && p.before(worst);
+                        in = __ballot_sync(0xffffffffu, mine_in);
+                    }
+                    if (mine_in) buffer[count + __popc(in & ((1u << lane) - 1))] = p;
+                    count += __popc(in);
+                };
+                if (P.finished && P.finished[(size_t)b * P.beams + row] != 0) {
+                    keep(lane == 0, BeamPick{score_of(0.f), (uint32_t)row, (uint32_t)P.end_token});
+                    continue;
+                }
+                // logits below this do not reach the bound (or what has to be beaten; exactly: below)
+                const uint64_t at_least = worst.score > bound ? worst.score : bound;
+                float least = -FLT_MAX;
+                if (at_least != 0) least = fmaxf(least, nextafterf(__double2float_rd((key_score(at_least) - off) + (double)row_top), -INFINITY));
+                const Slice v = slice_of(task);
+                const int begin = v.lo + (group % kBeamGroups - j * per_slice) * group_len;
+#pragma unroll 1
+                for (int c0 = begin; c0 < min(v.hi, begin + group_len); c0 += kBeamChunk) {
+                    uint4 raw[kLoads];
+                    float x[16];
+                    load(v, c0, raw);
+                    values(v, c0, raw, x);
+                    uint32_t hits = 0;                 // entries of this lane that may count
+#pragma unroll
+                    for (int k = 0; k < 16; ++k)
+                        if (x[k] >= least) hits |= 1u << k;
+                    while (__any_sync(0xffffffffu, hits != 0)) {           // one of every lane at a time
+                        const int k = __ffs((int)hits) - 1;
+                        float z = x[0];
+#pragma unroll
+                        for (int c = 1; c < 16; ++c) z = k == c ? x[c] : z;
+                        BeamPick p;
+                        p.score = score_of(z);
+                        p.row = (uint32_t)row;
+                        p.token = (uint32_t)(c0 + (k / kVec * 32 + lane) * kVec + k % kVec);
+                        keep(k >= 0 && p.score >= bound && (worst.score == 0 || p.before(worst)), p);
+                        hits &= hits - 1;
+                    }
+                }
             }
         }
+        // (all that was kept, if there is room for it; otherwise the n best of every warp)
+        if (lane == 0) s_counts[warp] = count;
+        __syncthreads();
+        int kept = 0;
+#pragma unroll
+        for (int w = 0; w < kBeamWarps; ++w) kept += s_counts[w];
+        if (kept > kBeamThreads && count > n) {
+            warp_best(buffer, count, n);
+            count = n;
+        }
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&s_picked, count);
+        at = __shfl_sync(0xffffffffu, at, 0);
+        for (int i = lane; i < count; i += 32) s_picks[at + i] = buffer[i];
+    }
+    __syncthreads();
+    // Ranks `count` candidates, one per thread at most, and calls put(rank, candidate) in one lane for each of the n best: those
+    // that reach the bound are listed, then a warp per candidate counts the better ones.  (The order in which they lie does not matter.)
+    auto rank_all = [&](const BeamPick* list, int count, auto put) {
+        const uint64_t mine = tid < count ? list[tid].score : 0ull;
+        if (warp == 0) {
+            uint64_t least = 0;
+            if (count > 2 * n) {
+                uint64_t some[kBeamThreads / 32];
+#pragma unroll
+                for (int k = 0; k < kBeamThreads / 32; ++k) some[k] = 32 * k + lane < count ? list[32 * k + lane].score : 0ull;
+                least = warp_bound(some, n);
+            }
+            if (lane == 0) s_bound = least, s_listed = 0;
+        }
+        __syncthreads();
+        const uint64_t least = s_bound;
+        if (mine != 0 && mine >= least) s_list[atomicAdd(&s_listed, 1)] = (uint16_t)tid;
+        __syncthreads();
+        const int listed = s_listed;
+        for (int i = warp; i < listed; i += kBeamWarps) {
+            const BeamPick p = list[s_list[i]];
+            int better = 0;
+            for (int o = lane; o < listed; o += 32) better += list[s_list[o]].before(p);
+            better = __reduce_add_sync(0xffffffffu, better);
+            if (better < n && lane == 0) put(better, p);
+        }
+        return listed;
+    };
+    static_assert(kBeamWarps * kMaxBeams <= kBeamThreads && kBeamMaxCluster * kMaxBeams <= kBeamThreads, "a thread per candidate");
+    // ---- the CTA's n best go to the first CTA, which joins those of all
+    {
+        BeamPick* to = cluster.map_shared_rank(s_sent, 0) + rank * n;
+        const int listed = rank_all(s_picks, s_picked, [&](int i, const BeamPick& p) { to[i] = p; });
+        for (int i = listed + tid; i < n; i += kBeamThreads) to[i] = no_pick();
     }
     cluster.sync();
     if (rank != 0) return;
-    // ---- ... which ranks them: the order in which they came does not matter
-    const int picked = min(s_picked, beam_max_picks(n));
-    auto put = [&](int i, bool there, const BeamPick& p) {
+    const int found = rank_all(s_sent, ctas * n, [&](int i, const BeamPick& p) {
         const size_t at = (size_t)b * n + i, from = (size_t)b * P.beams + p.row;
-        P.parents[at] = there ? (int32_t)from : -1;
-        P.tokens[at] = there ? (int32_t)p.token : -1;
-        P.scores_out[at] = there ? (float)key_score(p.score) : -INFINITY;
-        if (P.finished_out) P.finished_out[at] = !there || (int32_t)p.token == P.end_token || (P.finished && P.finished[from] != 0);
-    };
-    for (int i = tid; i < picked; i += kBeamThreads) {
-        const BeamPick p = s_picks[i];
-        int better = 0;
-        for (int o = 0; o < picked && better < n; ++o) better += s_picks[o].before(p);
-        if (better < n) put(better, true, p);
+        P.parents[at] = (int32_t)from;
+        P.tokens[at] = (int32_t)p.token;
+        P.scores_out[at] = (float)key_score(p.score);
+        if (P.finished_out) P.finished_out[at] = (int32_t)p.token == P.end_token || (P.finished && P.finished[from] != 0);
+    });
+    for (int i = found + tid; i < n; i += kBeamThreads) {
+        const size_t at = (size_t)b * n + i;
+        P.parents[at] = P.tokens[at] = -1;
+        P.scores_out[at] = -INFINITY;
+        if (P.finished_out) P.finished_out[at] = 1;
     }
-    for (int i = picked + tid; i < n; i += kBeamThreads) put(i, false, BeamPick{0, 0, 0});
 }
 
 }  // namespace kvq

@@ -26,7 +26,8 @@ bool overlap(const void* a, const void* b, size_t bytes) {
 // What a device allows, asked for once; the kernels' shared-memory limits and cluster sizes are set on the way.
 struct PagesDevice {
     int sm_count = 0;
-    int attn_clusters[4][5] = {};                      // resident clusters of 2^i CTAs, by channels (64, 128) and blocks of heads (1, 2)
+    int beam_clusters[5] = {};                         // resident clusters of 2^i CTAs of the selection ...
+    int attn_clusters[4][5] = {};                      // ... and of the attention, by channels (64, 128) and blocks of heads (1, 2)
 };
 int log2_of(int c) { return c <= 1 ? 0 : 1 + log2_of(c / 2); }
 
@@ -44,25 +45,31 @@ cudaError_t allow_smem(Kernel kernel, bool cluster) {
     return e;
 }
 
-// Both types of a shape are the same to the device; the batch's share of the shared memory is small.
-template <int D, int NT>
-cudaError_t set_up_attn(int (&clusters)[5]) {
-    cudaError_t e = allow_smem(k_page_attn<true, D, NT>, true);
-    if (e == cudaSuccess) e = allow_smem(k_page_attn<false, D, NT>, true);
+template <class Kernel>
+cudaError_t ask_clusters(Kernel kernel, int threads, size_t smem, int (&clusters)[5]) {
+    cudaError_t e = cudaSuccess;
     for (int i = 1; i < 5 && e == cudaSuccess; ++i) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(1u << i);
-        cfg.blockDim = dim3(AttnGeom<D>::kThreads);
-        cfg.dynamicSmemBytes = attn_smem<D>(64);
+        cfg.blockDim = dim3((unsigned)threads);
+        cfg.dynamicSmemBytes = smem;
         cudaLaunchAttribute attr;
         attr.id = cudaLaunchAttributeClusterDimension;
         attr.val.clusterDim.x = 1u << i;
         attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
-        e = cudaOccupancyMaxActiveClusters(&clusters[i], k_page_attn<false, D, NT>, &cfg);
+        e = cudaOccupancyMaxActiveClusters(&clusters[i], kernel, &cfg);
     }
     return e;
+}
+
+// Both types of a shape are the same to the device; the batch's share of the shared memory is small.
+template <int D, int NT>
+cudaError_t set_up_attn(int (&clusters)[5]) {
+    cudaError_t e = allow_smem(k_page_attn<true, D, NT>, true);
+    if (e == cudaSuccess) e = allow_smem(k_page_attn<false, D, NT>, true);
+    return e == cudaSuccess ? ask_clusters(k_page_attn<false, D, NT>, AttnGeom<D>::kThreads, attn_smem<D>(64), clusters) : e;
 }
 
 const PagesDevice* device_of_call() {
@@ -75,6 +82,7 @@ const PagesDevice* device_of_call() {
         if (err == cudaSuccess) err = allow_smem(k_beam_select<__half>, true);
         if (err == cudaSuccess) err = allow_smem(k_beam_select<__nv_bfloat16>, true);
         if (err == cudaSuccess) err = allow_smem(k_beam_select<float>, true);
+        if (err == cudaSuccess) err = ask_clusters(k_beam_select<float>, kBeamThreads, beam_smem(kMaxBeams), d.beam_clusters);
         if (err == cudaSuccess) err = set_up_attn<64, 1>(d.attn_clusters[0]);
         if (err == cudaSuccess) err = set_up_attn<64, 2>(d.attn_clusters[1]);
         if (err == cudaSuccess) err = set_up_attn<128, 1>(d.attn_clusters[2]);
@@ -291,9 +299,9 @@ int kvq_beam_select(const void* logits, int dtype, const float* scores, const ui
     if (!aligned(logits, size) || !aligned(scores, 4) || !aligned(parents, 4) || !aligned(tokens, 4) || !aligned(scores_out, 4)) return KVQ_ERR_ARG;
     const PagesDevice* d = device_of_call();
     if (!d) return KVQ_ERR_CUDA;
-    // a cluster per request, as wide as keeps the launch within two CTAs per SM
+    // a cluster per request, as wide as leaves all of them resident together
     int ctas = kBeamMaxCluster;
-    while (ctas > 1 && (uint64_t)batch * ctas > 2ull * (unsigned)d->sm_count) ctas /= 2;
+    while (ctas > 1 && batch > d->beam_clusters[log2_of(ctas)]) ctas /= 2;
     BeamParams p{};
     p.logits = logits;
     p.logits_end = static_cast<const uint8_t*>(logits) + size * (size_t)batch * beams * vocab;
@@ -312,7 +320,7 @@ int kvq_beam_select(const void* logits, int dtype, const float* scores, const ui
     p.slices = std::max(1, std::min(ctas * kBeamWarps / beams, (vocab + kBeamChunk - 1) / kBeamChunk));
     p.slice_len = (int)((((int64_t)vocab + p.slices - 1) / p.slices + 255) / 256 * 256);
     const uint64_t grid = (uint64_t)batch * ctas;
-    const size_t smem = beam_smem((beams * p.slices + ctas * kBeamWarps - 1) / (ctas * kBeamWarps), n_out);
+    const size_t smem = beam_smem(n_out);
     if (dtype == KVQ_FP32) return launch(k_beam_select<float>, grid, kBeamThreads, smem, ctas, p, stream);
     if (dtype == KVQ_BF16) return launch(k_beam_select<__nv_bfloat16>, grid, kBeamThreads, smem, ctas, p, stream);
     return launch(k_beam_select<__half>, grid, kBeamThreads, smem, ctas, p, stream);
