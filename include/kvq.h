@@ -379,7 +379,7 @@ typedef struct kvq_page_cache {
  *   status        dev uint32 [1]: 0, or KVQ_PAGE_* bits, and then the step did not take place: tables_out and lens_out hold
  *                 what tables_in and lens_in hold, cu_new zeros, slots, positions and copies -1
  * New pages are the free ones in ascending order, taken in row order.  Entries of tables_out behind a row's pages are left as
- * they were.  table_width >= 1, 0 <= batch <= KVQ_MAX_PAGE_ROWS.  One launch.
+ * they were (unspecified after a step that did not take place, unless tables_out is tables_in).  table_width >= 1, 0 <= batch <= KVQ_MAX_PAGE_ROWS.  One launch.
  */
 #define KVQ_PAGE_FULL 1u                      /* not enough free pages */
 #define KVQ_PAGE_LONG 2u                      /* a row would not fit table_width pages */

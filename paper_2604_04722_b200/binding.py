@@ -300,6 +300,14 @@ def kvq_page_cache(K, V) -> PageCache:
     return cache
 
 
+def _here(stream=None):
+    """The current device and the given or current stream of it (``torch.cuda.current_stream`` builds an object for it,
+    which takes 3 us)."""
+    import torch
+    device = torch.cuda.current_device()
+    return device, int(stream) if stream is not None else torch._C._cuda_getCurrentRawStream(device)
+
+
 def _dev(t, dtype, count: int, device: int, what: str) -> Optional[int]:
     """Address of a contiguous CUDA tensor of the given type with at least ``count`` elements on ``device``, or None."""
     if t is None:
@@ -313,14 +321,14 @@ def kvq_page_step(tables_in, tables_out, table_width: int, lens_in, lens_out, pa
                   page_size: int, max_new: int, cu_new, slots, positions, copies, status, stream=None) -> None:
     """One step of the block tables: rows take over their parents' pages, new tokens get pages and slots."""
     import torch
-    d, i32, where = torch.cuda.current_device(), torch.int32, "kvq_page_step"
+    (d, st), i32, where = _here(stream), torch.int32, "kvq_page_step"
     n = batch * table_width
     check(lib().kvq_page_step(
         _dev(tables_in, i32, n, d, where), _dev(tables_out, i32, n, d, where), table_width, _dev(lens_in, i32, batch, d, where),
         _dev(lens_out, i32, batch, d, where), _dev(parents, i32, batch, d, where), _dev(new_lens, i32, batch, d, where), batch,
         _dev(held, torch.uint8, n_pages, d, where), n_pages, page_size, max_new, _dev(cu_new, i32, batch + 1, d, where),
         _dev(slots, torch.int64, max_new, d, where), _dev(positions, i32, max_new, d, where), _dev(copies, i32, 3 * batch, d, where),
-        _dev(status, i32, 1, d, where), _stream(stream)), where)
+        _dev(status, i32, 1, d, where), st), where)
 
 
 def _cache(cache: PageCache, device: int, where: str) -> int:
@@ -332,11 +340,11 @@ def _cache(cache: PageCache, device: int, where: str) -> int:
 def kvq_page_append(cache: PageCache, K, V, slots, n_new: int, copies=None, batch: int = 0, stream=None) -> None:
     """Rows of new tokens to their slots, and the pages that kvq_page_step had copied."""
     import torch
-    d, where = torch.cuda.current_device(), "kvq_page_append"
+    (d, st), where = _here(stream), "kvq_page_append"
     n = n_new * cache.kv_heads * cache.head_dim
     check(lib().kvq_page_append(_cache(cache, d, where), _dev(K, cache.torch_dtype, n, d, where), _dev(V, cache.torch_dtype, n, d, where),
                                 _dev(slots, torch.int64, n_new, d, where), n_new, _dev(copies, torch.int32, 3 * batch, d, where), batch,
-                                _stream(stream)), where)
+                                st), where)
 
 
 def kvq_page_attn_workspace_bytes(batch: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
@@ -349,20 +357,20 @@ def kvq_page_attn(cache: PageCache, Q, O, lse, tables, table_width: int, lens, b
                   workspace_bytes: int, stream=None) -> None:
     """Attention of one new token per request over its pages; the workspace (uint8) is zero before its first use."""
     import torch
-    d, where = torch.cuda.current_device(), "kvq_page_attn"
+    (d, st), where = _here(stream), "kvq_page_attn"
     n = batch * q_heads
     check(lib().kvq_page_attn(_cache(cache, d, where), _dev(Q, cache.torch_dtype, n * cache.head_dim, d, where),
                               _dev(O, cache.torch_dtype, n * cache.head_dim, d, where), _dev(lse, torch.float32, n, d, where),
                               _dev(tables, torch.int32, batch * table_width, d, where), table_width, _dev(lens, torch.int32, batch, d, where),
                               batch, q_heads, scale, _dev(workspace, torch.uint8, workspace_bytes, d, where), workspace_bytes,
-                              _stream(stream)), where)
+                              st), where)
 
 
 def kvq_beam_select(logits, dtype: int, scores, finished, batch: int, beams: int, vocab: int, n_out: int, end_token: int, parents,
                     tokens, scores_out, finished_out=None, stream=None) -> None:
     """The n_out best continuations of every request's beams."""
     import torch
-    d, where = torch.cuda.current_device(), "kvq_beam_select"
+    (d, st), where = _here(stream), "kvq_beam_select"
     kinds = {KVQ_FP16: torch.float16, KVQ_BF16: torch.bfloat16, KVQ_FP32: torch.float32}
     if dtype not in kinds:
         raise KvqError(KVQ_ERR_ARG, where)
@@ -371,7 +379,7 @@ def kvq_beam_select(logits, dtype: int, scores, finished, batch: int, beams: int
                                 _dev(finished, torch.uint8, n, d, where), batch, beams, vocab, n_out, end_token,
                                 _dev(parents, torch.int32, m, d, where), _dev(tokens, torch.int32, m, d, where),
                                 _dev(scores_out, torch.float32, m, d, where), _dev(finished_out, torch.uint8, m, d, where),
-                                _stream(stream)), where)
+                                st), where)
 
 
 def kvq_decode_attn_static(ctx: int, layer: int, Q, O, stream=None) -> None:

@@ -19,48 +19,20 @@
 
 namespace kvq {
 
-constexpr int kPageStepThreads = 1024, kPageStepWarps = kPageStepThreads / 32;
+constexpr int kPageStepThreads = 512, kPageStepWarps = kPageStepThreads / 32;
 constexpr int kPageStepCluster = 8;
 
 constexpr uint32_t kPageFull = 1u, kPageLong = 2u, kPageSlots = 4u, kPageBad = 8u;
 
 // Shared memory: five words per row (old length, parent, kept | copy flag, first page wanted, first new token), the bitmap,
 // and one word for each of a slice of it.
-inline size_t page_step_smem(int batch, int n_pages, int ctas) {
+inline size_t page_step_smem(int batch, int n_pages) {
     const size_t words = ((size_t)n_pages + 31) / 32;
-    return sizeof(int32_t) * (5 * ((size_t)batch + 1) + words + (words + ctas - 1) / ctas);
+    return sizeof(int32_t) * (5 * ((size_t)batch + 1) + words + (words + kPageStepCluster - 1) / kPageStepCluster);
 }
 
-// Inclusive sums over the block of three values per thread; totals are returned to every thread.
-struct Sum3 {
-    long long a, b;
-    int m;                                             // (a maximum)
-};
-__device__ __forceinline__ Sum3 block_scan(Sum3 v, Sum3* s_warp, Sum3& total) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const long long a = __shfl_up_sync(0xffffffffu, v.a, d), b = __shfl_up_sync(0xffffffffu, v.b, d);
-        const int m = __shfl_up_sync(0xffffffffu, v.m, d);
-        if (lane >= d) v.a += a, v.b += b, v.m = max(v.m, m);
-    }
-    if (lane == 31) s_warp[warp] = v;
-    __syncthreads();
-    Sum3 w = s_warp[lane];                             // (one warp total per lane: 32 warps)
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const long long a = __shfl_up_sync(0xffffffffu, w.a, d), b = __shfl_up_sync(0xffffffffu, w.b, d);
-        const int m = __shfl_up_sync(0xffffffffu, w.m, d);
-        if (lane >= d) w.a += a, w.b += b, w.m = max(w.m, m);
-    }
-    const int before = max(warp - 1, 0);
-    const long long a = __shfl_sync(0xffffffffu, w.a, before), b = __shfl_sync(0xffffffffu, w.b, before);
-    if (warp > 0) v.a += a, v.b += b;
-    total.a = __shfl_sync(0xffffffffu, w.a, 31);
-    total.b = __shfl_sync(0xffffffffu, w.b, 31);
-    total.m = __shfl_sync(0xffffffffu, w.m, 31);
-    return v;
-}
+// Sums that stay at 2^32 - 1 instead of passing it: pages and tokens are counted up to limits far below.
+__device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return a + b < a ? 0xffffffffu : a + b; }
 
 // The last row whose first item is at or before `item` (first[0] = 0; rows without items are passed over).
 __device__ __forceinline__ int row_of(const int32_t* first, int rows, int item) {
@@ -77,8 +49,8 @@ __device__ __forceinline__ int row_of(const int32_t* first, int rows, int item) 
 __global__ void __launch_bounds__(kPageStepThreads, 1) k_page_step(const PageStepParams P) {
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
-    const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    constexpr int kCtas = kPageStepCluster, kWarps = kPageStepWarps, kThreads = kPageStepThreads;
+    const int rank = (int)cluster.block_rank(), tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     extern __shared__ __align__(16) int32_t s_mem[];
     const int B = P.batch, S = P.page_size;
     int32_t* s_old = s_mem;                            // [B] tokens taken over
@@ -89,164 +61,205 @@ __global__ void __launch_bounds__(kPageStepThreads, 1) k_page_step(const PageSte
     const int words = (P.n_pages + 31) / 32;
     uint32_t* s_map = reinterpret_cast<uint32_t*>(s_cu + B + 1);   // [words] pages listed, by this CTA's part of the tables
     uint32_t* s_before = s_map + words;                // [w1 - w0] free pages of this slice before a word
-    const int per_cta = (words + ctas - 1) / ctas, w0 = min(words, rank * per_cta), w1 = min(words, w0 + per_cta);
-    __shared__ Sum3 s_scan[32];
-    __shared__ uint32_t s_flags;
-    __shared__ int s_free[kPageStepCluster];           // free pages of every slice
-    __shared__ int s_warp_free[kPageStepWarps];
+    const int per_cta = (words + kCtas - 1) / kCtas, w0 = min(words, rank * per_cta), w1 = min(words, w0 + per_cta);
+    __shared__ uint32_t s_scan[2][kWarps];
+    __shared__ int s_most[kWarps], s_warp_free[kWarps];
+    __shared__ uint32_t s_flags;                       // the same in all CTAs after the first exchange
+    __shared__ int s_free[kCtas];                      // free pages of every slice
 
-    pdl_launch_dependents();
     if (tid == 0) s_flags = 0;
-    for (int w = tid; w < words; w += kPageStepThreads) s_map[w] = 0;
+    cluster.barrier_arrive();                          // (before another CTA's memory is written, all of them have to be there)
+    pdl_launch_dependents();
+    for (int w = tid; w < words; w += kThreads) s_map[w] = 0;
     pdl_wait();
 
     // ---- rows: every CTA for itself
-    for (int b = tid; b < B; b += kPageStepThreads) {
-        s_old[b] = P.lens_in[b];
-        s_kept[b] = 0x7fffffff;                        // first child, for now
-        s_par[b] = P.parents ? P.parents[b] : b;
+    for (int b = tid; b < B; b += kThreads) {
+        const int len = P.lens_in[b], parent = P.parents ? P.parents[b] : b, more = P.new_lens[b];
+        s_old[b] = len;
+        s_par[b] = parent;
+        s_cu[b] = more;                                // for now
+        s_kept[b] = P.parents ? 0x7fffffff : b;        // first child, for now
+    }
+    // meanwhile the pages of this CTA's slice that are held by somebody else, one bit each: sixteen pages a thread
+    for (int h = tid; h < 2 * (w1 - w0); h += kThreads) {
+        const int page = w0 * 32 + 16 * h;
+        uint32_t bits = 0;
+        if (page + 16 > P.n_pages || (P.held && (reinterpret_cast<uintptr_t>(P.held) & 15u))) {
+            uint8_t v[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) v[k] = page + k >= P.n_pages ? 1 : P.held ? P.held[page + k] : 0;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) bits |= (v[k] ? 1u : 0u) << k;
+        } else if (P.held) {
+            const uint4 v = *reinterpret_cast<const uint4*>(P.held + page);
+            const uint32_t word[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                if ((word[k / 4] >> (8 * (k & 3))) & 0xffu) bits |= 1u << k;
+        }
+        reinterpret_cast<uint16_t*>(s_before)[h] = (uint16_t)bits;
     }
     __syncthreads();
     uint32_t flags = 0;
     const long long room = (long long)P.width * S;
-    for (int b = tid; b < B; b += kPageStepThreads) {
-        const int p = s_par[b];
-        if (p < -1 || p >= B) flags |= kPageBad;
-        else if (p >= 0) {
-            atomicMin(&s_kept[p], b);
-            if (s_old[p] < 0 || (long long)s_old[p] > room) flags |= kPageBad;
+    if (P.parents) {
+        for (int b = tid; b < B; b += kThreads) {
+            const int p = s_par[b];
+            if (p < -1 || p >= B) flags |= kPageBad;
+            else if (p >= 0) atomicMin(&s_kept[p], b);
         }
+        __syncthreads();
     }
-    __syncthreads();
-    const int per = (B + kPageStepThreads - 1) / kPageStepThreads;         // at most kMaxPageRows / kPageStepThreads
-    constexpr int kPer = kMaxPageRows / kPageStepThreads;
-    int old[kPer], kept[kPer], want[kPer], more[kPer];
-    Sum3 mine = {0, 0, 0}, total;
+    const int per = (B + kThreads - 1) / kThreads;     // at most kPer
+    constexpr int kPer = kMaxPageRows / kThreads;
+    int old[kPer], kept[kPer], more[kPer];
+    uint32_t want[kPer], sum_want = 0, sum_more = 0;
+    int most = 0;
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
+        if (k >= per) break;
         const int b = tid * per + k;
-        old[k] = kept[k] = want[k] = more[k] = 0;
-        if (k >= per || b >= B) continue;
+        old[k] = kept[k] = more[k] = 0;
+        want[k] = 0;
+        if (b >= B) continue;
         const int p = s_par[b];
-        if (p >= 0 && p < B && s_old[p] >= 0 && (long long)s_old[p] <= room) {
-            old[k] = s_old[p];
-            const int full = (int)P.by_page.div((uint32_t)old[k]);
-            const bool part = full * (long long)S != old[k], copy = part && s_kept[p] != b;
-            kept[k] = copy ? full | (int)0x80000000u : full + (part ? 1 : 0);
+        if (p >= 0 && p < B) {
+            const int n = s_old[p];
+            if (n < 0 || (long long)n > room) flags |= kPageBad;
+            else {
+                const int full = (int)P.by_page.div((uint32_t)n);
+                const bool part = full * (long long)S != n, copy = part && s_kept[p] != b;
+                old[k] = n;
+                kept[k] = copy ? full | (int)0x80000000u : full + (part ? 1 : 0);
+            }
         }
-        more[k] = P.new_lens[b];
+        more[k] = s_cu[b];
         if (more[k] < 0) {
             flags |= kPageBad;
             more[k] = 0;
         }
         const long long after = (long long)old[k] + more[k];
         if (after > room || after > 0x7fffffffll) flags |= kPageLong;
-        else want[k] = (int)((after + S - 1) / S) - (kept[k] & 0x7fffffff);
-        mine.a += want[k];
-        mine.b += more[k];
-        mine.m = max(mine.m, kept[k] & 0x7fffffff);
+        else want[k] = P.by_page.div((uint32_t)after) + (P.by_page.div((uint32_t)after) * (long long)S != after ? 1u : 0u) - (uint32_t)(kept[k] & 0x7fffffff);
+        sum_want = add_sat(sum_want, want[k]);
+        sum_more = add_sat(sum_more, (uint32_t)more[k]);
+        most = max(most, kept[k] & 0x7fffffff);
     }
     if (flags) atomicOr(&s_flags, flags);
-    const Sum3 upto = block_scan(mine, s_scan, total); // (its barrier: s_old and s_kept have been read)
-    const bool fits = total.a <= P.n_pages && total.b <= P.max_new;
-    if (tid == 0 && total.a > P.n_pages) atomicOr(&s_flags, kPageFull);
-    if (tid == 0 && total.b > P.max_new) atomicOr(&s_flags, kPageSlots);
-    {
-        long long a = upto.a - mine.a, t = upto.b - mine.b;
+    uint32_t upto_want = sum_want, upto_more = sum_more;
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) {
-            const int b = tid * per + k;
-            if (k >= per || b >= B) continue;
-            s_old[b] = old[k];
-            s_kept[b] = kept[k];
-            s_want[b] = fits ? (int)a : 0;
-            s_cu[b] = fits ? (int)t : 0;
-            a += want[k];
-            t += more[k];
-        }
-        if (tid == 0) {
-            s_want[B] = fits ? (int)total.a : 0;
-            s_cu[B] = fits ? (int)total.b : 0;
-        }
+    for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t a = __shfl_up_sync(0xffffffffu, upto_want, d), t = __shfl_up_sync(0xffffffffu, upto_more, d);
+        if (lane >= d) upto_want = add_sat(upto_want, a), upto_more = add_sat(upto_more, t);
+    }
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 31) s_scan[0][warp] = upto_want, s_scan[1][warp] = upto_more, s_most[warp] = most;
+    __syncthreads();                                   // (and all have read s_old, s_kept and s_cu of other rows)
+    uint32_t all_want = 0, all_more = 0, before_want = 0, before_more = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        if (w == warp) before_want = all_want, before_more = all_more;
+        all_want = add_sat(all_want, s_scan[0][w]);
+        all_more = add_sat(all_more, s_scan[1][w]);
+        most = max(most, s_most[w]);
+    }
+    const bool fits = all_want <= (uint32_t)P.n_pages && all_more <= (uint32_t)P.max_new;
+    if (tid == 0 && all_want > (uint32_t)P.n_pages) atomicOr(&s_flags, kPageFull);
+    if (tid == 0 && all_more > (uint32_t)P.max_new) atomicOr(&s_flags, kPageSlots);
+    before_want += upto_want - sum_want;               // (what is used below did not reach the limit)
+    before_more += upto_more - sum_more;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        if (k >= per) break;
+        const int b = tid * per + k;
+        if (b >= B) continue;
+        s_old[b] = old[k];
+        s_kept[b] = kept[k];
+        s_want[b] = fits ? (int)before_want : 0;
+        s_cu[b] = fits ? (int)before_more : 0;
+        before_want += want[k];
+        before_more += (uint32_t)more[k];
+    }
+    if (tid == 0) {
+        s_want[B] = fits ? (int)all_want : 0;
+        s_cu[B] = fits ? (int)all_more : 0;
     }
     __syncthreads();
 
-    // ---- the pages that the rows list: stretches of 256 entries, one per warp of the cluster at a time
-    const int gwarp = rank * kPageStepWarps + warp, warps = ctas * kPageStepWarps;
-    const long long stretches = (long long)((total.m + 255) / 256) * B;
+    // ---- the pages that the rows list, stretches of 256 entries to a warp of the cluster at a time: marked, and on their way to
+    // where the tables go
+    const int gwarp = rank * kWarps + warp;
+    const bool moves = P.tables_out != P.tables_in;
+    const long long stretches = (long long)((most + 255) / 256) * B;
     flags = 0;
-    for (long long i = gwarp; i < stretches; i += warps) {
-        const int b = (int)(i % B), j0 = (int)(i / B) * 256, n = min(s_kept[b] & 0x7fffffff, j0 + 256);
+    for (long long i = gwarp; i < stretches; i += kCtas * kWarps) {
+        const int b = i < B ? (int)i : (int)(i % B), j0 = i < B ? 0 : (int)(i / B) * 256, n = min(s_kept[b] & 0x7fffffff, j0 + 256);
         if (j0 >= n) continue;
-        const int32_t* row = P.tables_in + (size_t)s_par[b] * P.width;
+        const int32_t* row = P.tables_in + (size_t)s_par[b] * P.width + j0;
         int page[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) page[k] = j0 + 32 * k + lane < n ? row[j0 + 32 * k + lane] : 0;
+        for (int k = 0; k < 8; ++k) page[k] = j0 + 32 * k + lane < n ? row[32 * k + lane] : 0;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             if (j0 + 32 * k + lane >= n) continue;
             if ((uint32_t)page[k] < (uint32_t)P.n_pages) atomicOr(&s_map[page[k] >> 5], 1u << (page[k] & 31));
             else flags = kPageBad;
+            if (moves) P.tables_out[(size_t)b * P.width + j0 + 32 * k + lane] = page[k];
         }
     }
     // a page to be copied has to be one, too
-    for (int b = rank * kPageStepThreads + tid; b < B; b += ctas * kPageStepThreads)
+    for (int b = rank * kThreads + tid; b < B; b += kCtas * kThreads)
         if (s_kept[b] < 0) {
             const int page = P.tables_in[(size_t)s_par[b] * P.width + (s_kept[b] & 0x7fffffff)];
             if ((uint32_t)page >= (uint32_t)P.n_pages) flags = kPageBad;
         }
-    if (flags) atomicOr(&s_flags, flags);
-    // the pages of this CTA's slice that are held by somebody else, one bit each
-    for (int w = w0 + warp; w < w1; w += kPageStepWarps) {
-        const int page = w * 32 + lane;
-        const uint32_t bits = __ballot_sync(0xffffffffu, page >= P.n_pages || (P.held && P.held[page] != 0));
-        if (lane == 0) s_before[w - w0] = bits;
-    }
+    cluster.barrier_wait();                            // (all CTAs are there)
+    if (flags)
+        for (int c = 0; c < kCtas; ++c) atomicOr(cluster.map_shared_rank(&s_flags, c), flags);
     cluster.sync();
 
     // ---- free pages of the slice: their bits replace this CTA's own map of it, which no other CTA reads; s_before becomes
     // their number before each word
-    const int per_thread = (w1 - w0 + kPageStepThreads - 1) / kPageStepThreads;
+    const int per_thread = (w1 - w0 + kThreads - 1) / kThreads;
     int count = 0;
     for (int k = 0; k < per_thread; ++k) {
         const int w = w0 + tid * per_thread + k;
         if (w >= w1) break;
         uint32_t used = s_before[w - w0];
-        for (int c = 0; c < ctas; ++c) used |= cluster.map_shared_rank(s_map, c)[w];
+#pragma unroll
+        for (int c = 0; c < kCtas; ++c) used |= cluster.map_shared_rank(s_map, c)[w];
         s_map[w] = ~used;
         count += __popc(~used);
     }
-    flags = 0;
-    for (int c = 0; c < ctas; ++c) flags |= *cluster.map_shared_rank(&s_flags, c);
-    int upto_me = count;
+    flags = s_flags;
+    int upto = count;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const int o = __shfl_up_sync(0xffffffffu, upto_me, d);
-        if (lane >= d) upto_me += o;
+        const int o = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += o;
     }
-    if (lane == 31) s_warp_free[warp] = upto_me;
+    if (lane == 31) s_warp_free[warp] = upto;
     __syncthreads();
-    int upto_warp = s_warp_free[lane];
+    int first_free = upto - count, slice_free = 0;
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const int o = __shfl_up_sync(0xffffffffu, upto_warp, d);
-        if (lane >= d) upto_warp += o;
+    for (int w = 0; w < kWarps; ++w) {
+        if (w == warp) first_free += slice_free;
+        slice_free += s_warp_free[w];
     }
-    int first_free = upto_me - count;
-    const int warps_before = __shfl_sync(0xffffffffu, upto_warp, max(warp - 1, 0)), slice_free = __shfl_sync(0xffffffffu, upto_warp, 31);
-    if (warp > 0) first_free += warps_before;
+    if (tid < kCtas) cluster.map_shared_rank(s_free, tid)[rank] = slice_free;
     for (int k = 0; k < per_thread; ++k) {
         const int w = w0 + tid * per_thread + k;
         if (w >= w1) break;
         s_before[w - w0] = (uint32_t)first_free;
         first_free += __popc(s_map[w]);
     }
-    if (tid < ctas) cluster.map_shared_rank(s_free, tid)[rank] = slice_free;
     cluster.sync();
 
-    // ---- the pages wanted are handed out, and the entries taken over move where the tables do
+    // ---- the pages wanted are handed out
     int slice0 = 0, all_free = 0;
-    for (int c = 0; c < ctas; ++c) {
+#pragma unroll
+    for (int c = 0; c < kCtas; ++c) {
         if (c < rank) slice0 += s_free[c];
         all_free += s_free[c];
     }
@@ -254,7 +267,7 @@ __global__ void __launch_bounds__(kPageStepThreads, 1) k_page_step(const PageSte
     if (wanted > all_free) flags |= kPageFull;
     const bool ok = flags == 0;
     if (ok) {
-        for (int w = w0 + warp; w < w1; w += kPageStepWarps) {
+        for (int w = w0 + warp; w < w1; w += kWarps) {
             const int i0 = slice0 + (int)s_before[w - w0];
             if (i0 >= wanted) break;                   // (the words of a slice are in order)
             const uint32_t bits = s_map[w];
@@ -263,35 +276,20 @@ __global__ void __launch_bounds__(kPageStepThreads, 1) k_page_step(const PageSte
             const int b = row_of(s_want, B, i);
             P.tables_out[(size_t)b * P.width + (s_kept[b] & 0x7fffffff) + (i - s_want[b])] = w * 32 + lane;
         }
-    }
-    if (P.tables_out != P.tables_in) {                 // (without a step the rows stay as they were)
-        for (int b = gwarp; b < B; b += warps) {
-            const int len = ok ? 0 : P.lens_in[b];
-            const int n = ok ? s_kept[b] & 0x7fffffff : len < 0 || (long long)len > room ? 0 : (int)(((long long)len + S - 1) / S);
-            const int32_t* from = P.tables_in + (size_t)(ok ? s_par[b] : b) * P.width;
-            int32_t* to = P.tables_out + (size_t)b * P.width;
-#pragma unroll 8
-            for (int j = lane; j < n; j += 32) to[j] = from[j];
+    } else if (moves) {                                // without a step the rows are those that came in
+        for (int b = gwarp; b < B; b += kCtas * kWarps) {
+            const int len = P.lens_in[b];
+            const int n = len < 0 || (long long)len > room ? 0 : (int)(((long long)len + S - 1) / S);
+            for (int j = lane; j < n; j += 32) P.tables_out[(size_t)b * P.width + j] = P.tables_in[(size_t)b * P.width + j];
         }
     }
     cluster.sync();
 
-    // ---- slots of the new tokens, lengths, copies
-    const int thread = rank * kPageStepThreads + tid, threads = ctas * kPageStepThreads;
-    const int fresh = ok ? s_cu[B] : 0;
-    for (long long t = thread; t < P.max_new; t += threads) {
-        long long slot = -1;
-        int pos = -1;
-        if (t < fresh) {
-            const int b = row_of(s_cu, B, (int)t);
-            pos = s_old[b] + (int)t - s_cu[b];
-            const int entry = (int)P.by_page.div((uint32_t)pos);
-            slot = (long long)__ldcg(P.tables_out + (size_t)b * P.width + entry) * S + (pos - entry * S);
-        }
-        P.slots[t] = slot;
-        if (P.positions) P.positions[t] = pos;
-    }
-    for (int b = thread; b < B; b += threads) {
+    // ---- slots of the new tokens, four neighbours a thread, and lengths and copies, by other CTAs if there are few tokens
+    const int thread = rank * kThreads + tid, threads = kCtas * kThreads, fresh = ok ? s_cu[B] : 0;
+    for (int b = (kCtas - 1 - rank) * kThreads + tid; b <= B; b += threads) {
+        P.cu_new[b] = ok ? s_cu[b] : 0;
+        if (b == B) break;
         P.lens_out[b] = ok ? s_old[b] + s_cu[b + 1] - s_cu[b] : P.lens_in[b];
         if (!P.copies) continue;
         int32_t* c = P.copies + 3 * (size_t)b;
@@ -301,8 +299,39 @@ __global__ void __launch_bounds__(kPageStepThreads, 1) k_page_step(const PageSte
         c[1] = copy ? __ldcg(P.tables_out + (size_t)b * P.width + full) : -1;
         c[2] = copy ? s_old[b] - full * S : 0;
     }
-    for (int b = thread; b <= B; b += threads) P.cu_new[b] = ok ? s_cu[b] : 0;
     if (thread == 0) *P.status = flags;
+    const bool vectors = ((reinterpret_cast<uintptr_t>(P.slots) | reinterpret_cast<uintptr_t>(P.positions)) & 15u) == 0;
+    for (long long t0 = 4ll * thread; t0 < P.max_new; t0 += 4ll * threads) {
+        int pos[4], offset[4], page[4];
+        int b = t0 < fresh ? row_of(s_cu, B, (int)t0) : B;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const long long t = t0 + k;
+            pos[k] = page[k] = -1;
+            offset[k] = 0;
+            if (t >= fresh) continue;
+            while (s_cu[b + 1] <= (int)t) ++b;         // (there is a row with this token)
+            pos[k] = s_old[b] + (int)t - s_cu[b];
+            const int entry = (int)P.by_page.div((uint32_t)pos[k]);
+            offset[k] = pos[k] - entry * S;
+            page[k] = __ldcg(P.tables_out + (size_t)b * P.width + entry);
+        }
+        long long slot[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) slot[k] = pos[k] < 0 ? -1ll : (long long)page[k] * S + offset[k];
+        if (t0 + 4 <= P.max_new && vectors) {
+            *reinterpret_cast<longlong2*>(P.slots + t0) = make_longlong2(slot[0], slot[1]);
+            *reinterpret_cast<longlong2*>(P.slots + t0 + 2) = make_longlong2(slot[2], slot[3]);
+            if (P.positions) *reinterpret_cast<int4*>(P.positions + t0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (t0 + k >= P.max_new) break;
+                P.slots[t0 + k] = slot[k];
+                if (P.positions) P.positions[t0 + k] = pos[k];
+            }
+        }
+    }
 }
 
 // Rows to their slots, and the used part of the pages that a step copied: 16-byte vectors, no row is touched twice.  The first

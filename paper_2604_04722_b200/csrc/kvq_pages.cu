@@ -189,7 +189,7 @@ int kvq_page_step(const int32_t* tables_in, int32_t* tables_out, int table_width
     p.page_size = page_size;
     p.max_new = max_new;
     p.by_page = FastDiv((uint32_t)page_size);
-    return launch(k_page_step, kPageStepCluster, kPageStepThreads, page_step_smem(batch, n_pages, kPageStepCluster), kPageStepCluster, p, stream);
+    return launch(k_page_step, kPageStepCluster, kPageStepThreads, page_step_smem(batch, n_pages), kPageStepCluster, p, stream);
 }
 
 int kvq_page_append(const kvq_page_cache* cache, const void* K, const void* V, const int64_t* slots, int n_new,
