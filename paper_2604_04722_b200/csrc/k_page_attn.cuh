@@ -27,40 +27,31 @@
 namespace kvq {
 
 constexpr int kAttnTile = 16;                          // tokens
-constexpr int kAttnMaxCtas = 1024;                     // arrival counters of a workspace
-#ifndef SNAP
-#define SNAP 16
-#endif
-#ifndef UT
-#define UT 20
-#endif
-constexpr int kAttnUnitTiles = UT;
+constexpr int kAttnMaxCtas = 512;                      // of a launch
+constexpr int kAttnAbreast = 2;                        // units that a CTA's warps take side by side at most
+constexpr int kAttnCounters = kAttnMaxCtas * kAttnAbreast;     // arrival counters of a workspace
+constexpr int kAttnUnitTiles = 20;                     // of a warp at most, where clusters take a unit each
 constexpr int kAttnMaxCluster = 16;
-#ifndef MINT
-#define MINT 1
-#endif
-constexpr int kAttnMinTilesLog2 = MINT;
-constexpr int kAttnSnap = SNAP;                           // see `border`
-constexpr int kAttnMinTiles = 1 << kAttnMinTilesLog2;                       // of a warp, where the work does not fill the launch
+constexpr int kAttnMinTilesLog2 = 1, kAttnMinTiles = 1 << kAttnMinTilesLog2;   // of a warp, where the work does not fill the launch
+constexpr int kAttnSnapBytes = 2048;                   // times 64: see `border`
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLn2 = 0.69314718055994531f;
 
-template <int D>
+// CTAs of 8 or 16 warps; 16 warps of 64 channels, or 8 of 128, fill an SM's shared memory.
+template <int D, int W>
 struct AttnGeom {
-    static constexpr int kWarps = D == 64 ? 16 : 8, kThreads = 32 * kWarps;
+    static constexpr int kWarps = W, kThreads = 32 * W, kCtas = 1024 / (D * W);
     static constexpr int kStages = 3;
     static constexpr int kRowBytes = 2 * D, kTensorBytes = kAttnTile * kRowBytes, kStageBytes = 2 * kTensorBytes;
     static constexpr int kRingBytes = kStages * kStageBytes;               // of a warp
 };
-constexpr int kJoinAt = (16 * (kAttnMaxCtas + 2) * (int)sizeof(float) + 127) / 128 * 128;      // behind the factors of a join
-static_assert(kJoinAt + AttnGeom<64>::kThreads * 16 <= AttnGeom<64>::kWarps * AttnGeom<64>::kRingBytes, "a join works in the rings");
 template <int D, int NT>
 __host__ __device__ constexpr int attn_record_floats() { return 8 * NT * (D + 2); }            // o [D][8 NT], m [8 NT], l [8 NT]
 
 // Shared memory: the rings, and the rows' place on the axis.
-template <int D>
+template <int D, int W>
 inline size_t attn_smem(int batch) {
-    return (size_t)AttnGeom<D>::kWarps * AttnGeom<D>::kRingBytes + sizeof(int64_t) * ((size_t)batch + 1);
+    return (size_t)W * AttnGeom<D, W>::kRingBytes + sizeof(int64_t) * ((size_t)batch + 1);
 }
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
@@ -109,7 +100,7 @@ __device__ __forceinline__ uint16_t round16(float v) {
     return (uint16_t)(pack16<BF>(v, 0.f) & 0xffffu);
 }
 
-// A place on the axis: tile t of unit u (head and block) of row b.
+// A place on the axis: tile t of unit (or bundle of units) u of row b.
 struct AttnCursor {
     int b, u, t, tiles, len;
 };
@@ -121,9 +112,9 @@ struct AttnPiece {
 };
 
 // grid: at most kAttnMaxCtas resident CTAs; those that the lengths leave without work return.
-template <bool BF, int D, int NT>
-__global__ void __launch_bounds__(AttnGeom<D>::kThreads, 1) k_page_attn(const PageAttnParams P) {
-    using G = AttnGeom<D>;
+template <bool BF, int D, int NT, int W>
+__global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCtas) k_page_attn(const PageAttnParams P) {
+    using G = AttnGeom<D, W>;
     constexpr int kMt = D / 16, kR = 8 * NT, kStages = G::kStages, kAttnWarps = G::kWarps, kAttnThreads = G::kThreads;
     namespace cg = cooperative_groups;
     const int C = P.cluster, rank = C > 1 ? (int)cg::this_cluster().block_rank() : 0, group = (int)blockIdx.x / C, groups = (int)gridDim.x / C;
@@ -139,7 +130,9 @@ __global__ void __launch_bounds__(AttnGeom<D>::kThreads, 1) k_page_attn(const Pa
     __shared__ int s_longest[kAttnWarps];
     __shared__ uint32_t s_there[kAttnWarps][kStages];  // tokens of a stage that exist
     __shared__ AttnPiece s_piece[2 * kAttnWarps];      // a warp's first and last piece
-    __shared__ uint32_t s_last[2];
+    // Of every unit abreast, two may go on in other CTAs, one from before and one beyond: their first pieces, or -1
+    __shared__ int s_open[2 * kAttnAbreast];
+    __shared__ int s_first[2 * kAttnAbreast], s_last[2 * kAttnAbreast];    // stretches of such a unit that this CTA joins (last: -1, another does)
 
     pdl_launch_dependents();
     pdl_wait();
@@ -171,6 +164,7 @@ __global__ void __launch_bounds__(AttnGeom<D>::kThreads, 1) k_page_attn(const Pa
         }
         if (lane == 31) s_scan[warp] = upto;
         if (tid < 2 * kAttnWarps) s_piece[tid].unit = -1;
+        if (tid < 2 * kAttnAbreast) s_open[tid] = -1;
         __syncthreads();
         int64_t at = upto - sum;
         for (int w = 0; w < warp; ++w) at += s_scan[w];
@@ -192,34 +186,39 @@ __global__ void __launch_bounds__(AttnGeom<D>::kThreads, 1) k_page_attn(const Pa
         if (P.lse)
             for (int h = tid; h < P.q_heads; h += kAttnThreads) P.lse[(size_t)b * P.q_heads + h] = -INFINITY;
     }
-    const int64_t total = tiles_before(P.batch) * units_per_row;
-    if (total == 0) return;
+    if (s_place[P.batch] == 0) return;
     // A cluster of CTAs (or one CTA) works on a stretch of the axis: a unit each, where there are no more units than clusters and
     // none is long; otherwise equal shares.
     int longest = 0;
 #pragma unroll
     for (int w = 0; w < kAttnWarps; ++w) longest = max(longest, s_longest[w]);
-    const int units = P.batch * units_per_row, warps = C * kAttnWarps, warps_log2 = __ffs(warps) - 1;      // (a power of two)
-    const bool unit_each = units <= groups && longest <= kAttnUnitTiles * warps;
+    const int units = P.batch * units_per_row;
+    const bool unit_each = units <= groups && longest <= kAttnUnitTiles * C * kAttnWarps;
+    // With equal shares `abreast` units of a row that lie side by side in memory go abreast, each with its share of the CTA's warps
+    // (member: which of them this warp works on); the axis then consists of such bundles of units.
+    const int abreast = unit_each ? 1 : P.abreast, team = kAttnWarps / abreast, member = warp / team;
+    const int bundles_per_row = units_per_row / abreast, snap = kAttnSnapBytes / D / abreast;
+    const int warps = C * team, warps_log2 = __ffs(warps) - 1;             // that share a stretch (a power of two)
+    const int64_t total = tiles_before(P.batch) * bundles_per_row;
     const int stretches = unit_each ? units : (int)min((int64_t)groups, ((total + warps * kAttnMinTiles - 1) >> (warps_log2 + kAttnMinTilesLog2)));
     if (group >= stretches) return;
     auto locate = [&](int64_t at) -> AttnCursor {
         int b0 = 0, b1 = P.batch;
         while (b1 - b0 > 1) {
             const int mid = (b0 + b1) >> 1;
-            if (tiles_before(mid) * units_per_row <= at) b0 = mid;
+            if (tiles_before(mid) * bundles_per_row <= at) b0 = mid;
             else b1 = mid;
         }
         AttnCursor c;
         c.b = b0;
         c.tiles = tiles_of(b0);
         c.len = len_of(b0);
-        const int64_t rest = at - tiles_before(b0) * units_per_row;
+        const int64_t rest = at - tiles_before(b0) * bundles_per_row;
         c.u = (rest >> 32) == 0 ? (int)((uint32_t)rest / (uint32_t)c.tiles) : (int)(rest / c.tiles);
         c.t = (int)(rest - (int64_t)c.u * c.tiles);
         return c;
     };
-    // The borders between equal shares move to the border of a unit that is no more than kAttnSnap tiles away.
+    // The borders between equal shares move to the border of a unit that is no more than snap tiles away.
     const int64_t share_size = unit_each ? 0 : (total >> 32) == 0 ? (int64_t)((uint32_t)total / (uint32_t)stretches) : total / stretches, share_more = total - share_size * stretches;     // (the first share_more have one tile more)
     auto share = [&](int c) -> int64_t { return share_size * c + min((int64_t)c, share_more); };
     auto border = [&](int c) -> int64_t {
@@ -231,18 +230,19 @@ __global__ void __launch_bounds__(AttnGeom<D>::kThreads, 1) k_page_attn(const Pa
         const int64_t at = share(c);
         const AttnCursor x = locate(at);
         const int back = x.t, ahead = x.tiles - x.t;
-        return min(back, ahead) > kAttnSnap ? at : back <= ahead ? at - back : at + ahead;
+        return min(back, ahead) > snap ? at : back <= ahead ? at - back : at + ahead;
     };
     const int64_t lo = border(group), hi = border(group + 1);
     if (lo == hi) return;                              // (the same for the whole cluster)
     auto warp_border = [&](int w) -> int64_t { return lo + (((hi - lo) * w) >> warps_log2); };     // of the cluster's warps
-    auto cta_border = [&](int r) { return warp_border(r * kAttnWarps); };
-    const int64_t wlo = warp_border(rank * kAttnWarps + warp), whi = warp_border(rank * kAttnWarps + warp + 1);
+    auto cta_border = [&](int r) { return warp_border(r * team); };
+    const int64_t wlo = warp_border(rank * team + warp % team), whi = warp_border(rank * team + warp % team + 1);
     const int64_t cta_lo = cta_border(rank), cta_hi = cta_border(rank + 1);
 
+    auto unit_of = [&](const AttnCursor& c) { return c.u * abreast + member; };        // this warp's, of the row
     auto next_unit = [&](AttnCursor& c) {
         c.t = 0;
-        if (++c.u < units_per_row) return;
+        if (++c.u < bundles_per_row) return;
         c.u = 0;
         do ++c.b; while (c.b < P.batch && tiles_of(c.b) == 0);
         if (c.b >= P.batch) return;                    // (behind the last tile)
@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(AttnGeom<D>::kThreads, 1) k_page_attn(const Pa
     };
     auto piece_at = [&](const AttnCursor& c, int64_t last) {       // behind its tile `last` of the axis
         AttnPiece p;
-        p.unit = c.b * units_per_row + c.u;
+        p.unit = c.b * units_per_row + unit_of(c);
         p.begin = last + 1 - c.t;
         p.end = p.begin + c.tiles;
         return p;
@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(AttnGeom<D>::kThreads, 1) k_page_attn(const Pa
             page = -1;
             if (looked >= count) return;
             const int pos = ahead.t * kAttnTile + (lane & 15);
-            head = ahead.u / P.head_blocks;
+            head = P.head_blocks == 1 ? unit_of(ahead) : unit_of(ahead) / P.head_blocks;
             if (pos < ahead.len) {
                 const int entry = (int)P.by_page.div((uint32_t)pos);
                 slot = pos - entry * P.page_size;
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(AttnGeom<D>::kThreads, 1) k_page_attn(const Pa
         uint32_t qf[kMt][NT][2];
         float o[kMt][NT][4], m[NT][2], l[NT][2];
         auto start_unit = [&]() {
-            const int h0 = at.u / P.head_blocks, hb = at.u - h0 * P.head_blocks;
+            const int h0 = P.head_blocks == 1 ? unit_of(at) : unit_of(at) / P.head_blocks, hb = unit_of(at) - h0 * P.head_blocks;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const int r = hb * kR + nt * 8 + g;    // head within the group
@@ -348,7 +348,7 @@ __global__ void __launch_bounds__(AttnGeom<D>::kThreads, 1) k_page_attn(const Pa
             }
         };
         auto write_unit = [&]() {
-            const int h0 = at.u / P.head_blocks, hb = at.u - h0 * P.head_blocks;
+            const int h0 = P.head_blocks == 1 ? unit_of(at) : unit_of(at) / P.head_blocks, hb = unit_of(at) - h0 * P.head_blocks;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const float i0 = l[nt][0] > 0.f || l[nt][0] != l[nt][0] ? 1.f / l[nt][0] : 0.f;
@@ -547,6 +547,7 @@ __global__ void __launch_bounds__(AttnGeom<D>::kThreads, 1) k_page_attn(const Pa
                 s_f.m[j][r] = top;
                 s_f.l[j][r] = closed ? inverse(sum) : sum;
                 if (closed) put_lse(place_of(mine.unit), r, top, sum);
+                else if (r == 0) s_open[2 * ((j >> 1) / team) + (mine.begin < cta_lo ? 0 : 1)] = j;
             }
         }
     }
@@ -554,14 +555,7 @@ __global__ void __launch_bounds__(AttnGeom<D>::kThreads, 1) k_page_attn(const Pa
     // what goes on in other CTAs of the cluster waits in shared memory (behind the pieces of warps 1 and 2), what goes on in other
     // stretches in the workspace
     auto cluster_rec = [&](int w) { return reinterpret_cast<float*>(s_ring_all + (size_t)(w + 2) * G::kRingBytes) - kRec; };
-    auto group_rec = [&](int w) { return P.cta_rec + ((size_t)group * 2 + w) * kRec; };
-    int open[2] = {-1, -1};                            // first pieces of units that go on in other CTAs: one from before, one beyond
-    if (leads) {
-        const int i0 = __ffs((int)leads) - 1, i1 = 31 - __clz((int)leads);
-        if (s_piece[i0].begin < cta_lo) open[0] = i0;
-        if (s_piece[i1].begin >= cta_lo && s_piece[i1].end > cta_hi) open[1] = i1;
-        if (open[0] < 0 && s_piece[i0].begin >= cta_lo && s_piece[i0].end > cta_hi) open[1] = i0;
-    }
+    auto group_rec = [&](int g, int w) { return P.cta_rec + ((size_t)g * 2 * kAttnAbreast + w) * kRec; };        // (w = 2 member + 0 or 1)
     // threads over the units of the CTA, quads of heads, channels
     const int quads = min(kR, P.group + 3) / 4;        // (at most what the group needs)
     for (int e = tid; e < __popc(leads) * quads * D; e += kAttnThreads) {
@@ -579,7 +573,14 @@ __global__ void __launch_bounds__(AttnGeom<D>::kThreads, 1) k_page_attn(const Pa
             const float4 f = *reinterpret_cast<const float4*>(&s_f.factor[k][r]), y = *reinterpret_cast<const float4*>(first_piece(k >> 1) + d * kR + r);
             so = make_float4(f.x * y.x, f.y * y.y, f.z * y.z, f.w * y.w);
         }
-        if (lasts) {
+        auto add = [&](int k) {
+            const float4 f = *reinterpret_cast<const float4*>(&s_f.factor[2 * k + 1][r]), y = *reinterpret_cast<const float4*>(last_piece(k) + d * kR + r);
+            so.x += f.x * y.x, so.y += f.y * y.y, so.z += f.z * y.z, so.w += f.w * y.w;
+        };
+        if (__popc(lasts) <= 2) {
+            if (lasts) add((__ffs((int)lasts) - 1) >> 1);
+            if (lasts & (lasts - 1)) add((31 - __clz((int)lasts)) >> 1);
+        } else {
             const int some = (__ffs((int)lasts) - 1) >> 1;
 #pragma unroll
             for (int w0 = 0; w0 < kAttnWarps; w0 += 8) {
@@ -596,137 +597,28 @@ __global__ void __launch_bounds__(AttnGeom<D>::kThreads, 1) k_page_attn(const Pa
                 for (int w = 0; w < 8; ++w) so.x += f[w].x * y[w].x, so.y += f[w].y * y[w].y, so.z += f[w].z * y[w].z, so.w += f[w].w * y[w].w;
             }
         }
-        const int which = i == open[0] ? 0 : i == open[1] ? 1 : -1;
-        if (which < 0) {
+        if (s_piece[i].begin >= cta_lo && s_piece[i].end <= cta_hi) {
             put(place_of(s_piece[i].unit), r, d, so, &s_f.l[i][r]);
         } else {
-            float* rec = C > 1 ? cluster_rec(which) : group_rec(which);
+            const int which = 2 * ((i >> 1) / team) + (s_piece[i].begin < cta_lo ? 0 : 1);
+            float* rec = C > 1 ? cluster_rec(which) : group_rec(group, which);
             *reinterpret_cast<float4*>(rec + d * kR + r) = so;
             if (d < 2) *reinterpret_cast<float4*>(rec + (D + d) * kR + r) = *reinterpret_cast<const float4*>(d == 0 ? &s_f.m[i][r] : &s_f.l[i][r]);
         }
     }
-    // ---- units that several stretches share: the CTA with the last record joins them.  A border inside a unit is more than
-    // kAttnSnap tiles away from both its ends, so the stretches that share it follow from the equal shares alone.
-    auto join_stretches = [&]() {
-        const double shares_per_tile = (double)stretches / (double)total;
-        int first_group[2] = {0, 0}, parts[2] = {0, 0};
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-            if (open[w] < 0) continue;
-            auto cta_of = [&](int64_t t) {                 // the last CTA whose share begins at or before tile t
-                int c = min(stretches - 1, (int)((double)t * shares_per_tile));
-                while (c + 1 < stretches && share(c + 1) <= t) ++c;
-                while (share(c) > t) --c;
-                return c;
-            };
-            first_group[w] = cta_of(s_piece[open[w]].begin + kAttnSnap);
-            parts[w] = cta_of(s_piece[open[w]].end - kAttnSnap - 1) - first_group[w] + 1;
-        }
-        __syncthreads();
-        if (tid < 2 && open[tid] >= 0) {
-            __threadfence();                               // (the whole CTA's records, which the barrier has ordered before)
-            const uint32_t most = (uint32_t)(tid == 0 ? parts[0] : parts[1]) - 1u;
-            s_last[tid] = atomicInc(&P.arrivals[tid == 0 ? first_group[0] : first_group[1]], most) == most;
-            __threadfence();
-        }
-        __syncthreads();
-        // Factors 2^(m_c - m) of the records and the sum of weights, a warp per head; the outputs, four heads of a channel per thread and as
-        // many records at once as there are threads for (the rings are free by now).
-        float* const s_m = reinterpret_cast<float*>(s_ring_all);               // [kR][stretches], then the factors
-        float* const s_sum = s_m + kR * stretches;                                  // [kR] inverse sums of weights
-        float4* const s_part = reinterpret_cast<float4*>(s_ring_all + kJoinAt);        // [kAttnThreads]
-#pragma unroll 1
-        for (int w = 0; w < 2; ++w) {
-            if (open[w] < 0 || !s_last[w]) continue;
-            const int n = parts[w];
-            const Place at = place_of(s_piece[open[w]].unit);
-            // (only the first part begins with the unit)
-            auto record = [&](int i) -> const float* { return P.cta_rec + ((size_t)(first_group[w] + i) * 2 + (i == 0 ? 1 : 0)) * kRec; };
-            const int quads = (at.heads + 3) / 4, vecs = quads * D, at_once = max(1, kAttnThreads / vecs), stride = min(vecs, kAttnThreads);
-            const int part0 = tid / stride;
-            constexpr int kEarly = 16;                     // outputs on their way while the factors are worked out
-            float4 early[kEarly];
-            {
-                const int v = tid - part0 * stride, d = v / quads, r = (v - d * quads) * 4;
-#pragma unroll
-                for (int k = 0; k < kEarly; ++k) {
-                    const int i = part0 + k * at_once;
-                    if (part0 < at_once && i < n) early[k] = __ldcg(reinterpret_cast<const float4*>(record(i) + d * kR + r));
-                }
-            }
-            for (int r = warp; r < at.heads; r += kAttnWarps) {
-                float top = kLowest, sum = 0.f;
-                for (int i0 = lane; i0 < n; i0 += 128) {
-                    float m[4], l[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const bool in = i0 + 32 * k < n;
-                        m[k] = in ? __ldcg(record(i0 + 32 * k) + D * kR + r) : kLowest;
-                        l[k] = in ? __ldcg(record(i0 + 32 * k) + (D + 1) * kR + r) : 0.f;
-                    }
-                    const float now = fmaxf(top, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])));
-                    sum *= fast_exp2(top - now);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        if (i0 + 32 * k < n) s_m[r * stretches + i0 + 32 * k] = m[k];
-                        sum += l[k] * fast_exp2(m[k] - now);
-                    }
-                    top = now;
-                }
-                const float all = warp_max(top);
-                sum = warp_sum(sum * fast_exp2(top - all));
-                for (int i0 = lane; i0 < n; i0 += 32) s_m[r * stretches + i0] = fast_exp2(s_m[r * stretches + i0] - all);
-                if (lane == 0) s_sum[r] = inverse(sum), put_lse(at, r, all, sum);
-            }
-            __syncthreads();
-#pragma unroll 1
-            for (int v0 = 0; v0 < vecs; v0 += kAttnThreads) {
-                const int v = v0 + tid - part0 * stride, d = v / quads, r = (v - d * quads) * 4;
-                float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-                auto add = [&](int i, const float4& x) {
-                    const float* f = s_m + r * stretches + i;
-                    sum.x += f[0] * x.x;
-                    if (r + 1 < at.heads) sum.y += f[stretches] * x.y;
-                    if (r + 2 < at.heads) sum.z += f[2 * stretches] * x.z;
-                    if (r + 3 < at.heads) sum.w += f[3 * stretches] * x.w;
-                };
-                if (part0 < at_once && v < vecs) {
-                    if (v0 == 0) {
-#pragma unroll
-                        for (int k = 0; k < kEarly; ++k)
-                            if (part0 + k * at_once < n) add(part0 + k * at_once, early[k]);
-                    }
-#pragma unroll 4
-                    for (int i = part0 + (v0 == 0 ? kEarly * at_once : 0); i < n; i += at_once)
-                        add(i, __ldcg(reinterpret_cast<const float4*>(record(i) + d * kR + r)));
-                }
-                if (at_once > 1) {
-                    s_part[tid] = sum;
-                    __syncthreads();
-                    if (part0 == 0)
-                        for (int i = 1; i < at_once; ++i) {
-                            const float4 x = s_part[i * stride + tid];
-                            sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
-                        }
-                }
-                if (part0 == 0 && v < vecs) {
-                    put(at, r, d, sum, s_sum + r);
-                }
-            }
-            __syncthreads();                               // (the factors are read; the next unit's may be written)
-        }
-    };
     if (C > 1) {
         // ---- units that several CTAs of the cluster share: the first of them adds up, lanes and threads as above
         cg::cluster_group cluster = cg::this_cluster();
         cluster.sync();
 #pragma unroll 1
         for (int w = 0; w < 2; ++w) {
-            if (open[w] < 0) continue;
-            const AttnPiece unit = s_piece[open[w]];
+            const int lead = s_open[w];
+            if (lead < 0) continue;                    // (the same for all threads)
+            const AttnPiece unit = s_piece[lead];
             const int64_t from = max(unit.begin, lo), to = min(unit.end, hi);
             if (from < cta_lo) {                       // another CTA's
-                open[w] = -1;
+                __syncthreads();
+                if (tid == 0) s_open[w] = -1;
                 continue;
             }
             const int part = rank + (lane & 15);       // of this lane
@@ -770,17 +662,66 @@ __global__ void __launch_bounds__(AttnGeom<D>::kThreads, 1) k_page_attn(const Pa
                 if (closed) {
                     put(at, r, d, so, &s_f.l[0][r]);
                 } else {
-                    float* rec = group_rec(w);
+                    float* rec = group_rec(group, w);
                     *reinterpret_cast<float4*>(rec + d * kR + r) = so;
                     if (d < 2) *reinterpret_cast<float4*>(rec + (D + d) * kR + r) = *reinterpret_cast<const float4*>(d == 0 ? &s_f.m[0][r] : &s_f.l[0][r]);
                 }
             }
             __syncthreads();
-            if (closed) open[w] = -1;
+            if (closed && tid == 0) s_open[w] = -1;
         }
         cluster.sync();                                // (nobody leaves, or uses its rings, while its records may be read)
     }
-    if (open[0] >= 0 || open[1] >= 0) join_stretches();
+    // ---- units that several stretches share: the CTA with the last record joins them.  A border inside a unit is more than
+    // snap tiles away from both its ends, so the stretches that share it follow from the equal shares alone.
+    __syncthreads();                                   // (the records are written)
+    const double shares_per_tile = (double)stretches / (double)total;
+    auto share_of = [&](int64_t t) {                   // the last stretch whose share begins at or before tile t
+        int c = min(stretches - 1, (int)((double)t * shares_per_tile));
+        while (c + 1 < stretches && share(c + 1) <= t) ++c;
+        while (share(c) > t) --c;
+        return c;
+    };
+    if (tid < 2 * abreast && s_open[tid] >= 0) {
+        const AttnPiece unit = s_piece[s_open[tid]];
+        const int c0 = share_of(unit.begin + snap), c1 = share_of(unit.end - snap - 1);
+        __threadfence();                               // (the whole CTA's records, which the barrier has ordered before)
+        const bool last = atomicInc(&P.arrivals[c0 * kAttnAbreast + (tid >> 1)], (uint32_t)(c1 - c0)) == (uint32_t)(c1 - c0);
+        __threadfence();
+        s_first[tid] = c0;
+        s_last[tid] = last ? c1 : -1;
+    }
+    __syncthreads();
+    for (int e = tid; e < 2 * abreast * quads * D; e += kAttnThreads) {
+        const int d = e % D, x = e / D, which = quads == 1 ? x : quads == 2 ? x / 2 : quads == 3 ? x / 3 : x / 4, r = 4 * (x - which * quads);
+        const int lead = s_open[which];
+        if (lead < 0 || s_last[which] < 0) continue;
+        // one record after the other, in the order of the axis; only the first begins with the unit
+        float m[4] = {kLowest, kLowest, kLowest, kLowest}, l[4] = {0.f, 0.f, 0.f, 0.f}, o[4] = {0.f, 0.f, 0.f, 0.f};
+        const int c0 = s_first[which], c1 = s_last[which];
+#pragma unroll 4
+        for (int c = c0; c <= c1; ++c) {
+            const float* rec = group_rec(c, (which & ~1) + (c == c0 ? 1 : 0));
+            const float4 m4 = __ldcg(reinterpret_cast<const float4*>(rec + D * kR + r)), l4 = __ldcg(reinterpret_cast<const float4*>(rec + (D + 1) * kR + r));
+            const float4 o4 = __ldcg(reinterpret_cast<const float4*>(rec + d * kR + r));
+            const float mc[4] = {m4.x, m4.y, m4.z, m4.w}, lc[4] = {l4.x, l4.y, l4.z, l4.w}, oc[4] = {o4.x, o4.y, o4.z, o4.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float top = fmaxf(m[k], mc[k]), f0 = fast_exp2(m[k] - top), f1 = fast_exp2(mc[k] - top);
+                l[k] = l[k] * f0 + lc[k] * f1;
+                o[k] = o[k] * f0 + oc[k] * f1;
+                m[k] = top;
+            }
+        }
+        const Place at = place_of(s_piece[lead].unit);
+        float inv[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            inv[k] = inverse(l[k]);
+            if (d == 0) put_lse(at, r + k, m[k], l[k]);
+        }
+        put(at, r, d, make_float4(o[0], o[1], o[2], o[3]), inv);
+    }
 }
 
 }  // namespace kvq

@@ -27,7 +27,7 @@ bool overlap(const void* a, const void* b, size_t bytes) {
 struct PagesDevice {
     int sm_count = 0;
     int beam_clusters[5] = {};                         // resident clusters of 2^i CTAs of the selection ...
-    int attn_clusters[4][5] = {};                      // ... and of the attention, by channels (64, 128) and blocks of heads (1, 2)
+    int attn_clusters[6][5] = {};                      // ... and of the attention: see attn_variant
 };
 int log2_of(int c) { return c <= 1 ? 0 : 1 + log2_of(c / 2); }
 
@@ -65,11 +65,11 @@ cudaError_t ask_clusters(Kernel kernel, int threads, size_t smem, int (&clusters
 }
 
 // Both types of a shape are the same to the device; the batch's share of the shared memory is small.
-template <int D, int NT>
+template <int D, int NT, int W>
 cudaError_t set_up_attn(int (&clusters)[5]) {
-    cudaError_t e = allow_smem(k_page_attn<true, D, NT>, true);
-    if (e == cudaSuccess) e = allow_smem(k_page_attn<false, D, NT>, true);
-    return e == cudaSuccess ? ask_clusters(k_page_attn<false, D, NT>, AttnGeom<D>::kThreads, attn_smem<D>(64), clusters) : e;
+    cudaError_t e = allow_smem(k_page_attn<true, D, NT, W>, true);
+    if (e == cudaSuccess) e = allow_smem(k_page_attn<false, D, NT, W>, true);
+    return e == cudaSuccess ? ask_clusters(k_page_attn<false, D, NT, W>, AttnGeom<D, W>::kThreads, attn_smem<D, W>(64), clusters) : e;
 }
 
 const PagesDevice* device_of_call() {
@@ -83,10 +83,12 @@ const PagesDevice* device_of_call() {
         if (err == cudaSuccess) err = allow_smem(k_beam_select<__nv_bfloat16>, true);
         if (err == cudaSuccess) err = allow_smem(k_beam_select<float>, true);
         if (err == cudaSuccess) err = ask_clusters(k_beam_select<float>, kBeamThreads, beam_smem(kMaxBeams), d.beam_clusters);
-        if (err == cudaSuccess) err = set_up_attn<64, 1>(d.attn_clusters[0]);
-        if (err == cudaSuccess) err = set_up_attn<64, 2>(d.attn_clusters[1]);
-        if (err == cudaSuccess) err = set_up_attn<128, 1>(d.attn_clusters[2]);
-        if (err == cudaSuccess) err = set_up_attn<128, 2>(d.attn_clusters[3]);
+        if (err == cudaSuccess) err = set_up_attn<64, 1, 8>(d.attn_clusters[0]);
+        if (err == cudaSuccess) err = set_up_attn<64, 2, 8>(d.attn_clusters[1]);
+        if (err == cudaSuccess) err = set_up_attn<64, 1, 16>(d.attn_clusters[2]);
+        if (err == cudaSuccess) err = set_up_attn<64, 2, 16>(d.attn_clusters[3]);
+        if (err == cudaSuccess) err = set_up_attn<128, 1, 8>(d.attn_clusters[4]);
+        if (err == cudaSuccess) err = set_up_attn<128, 2, 8>(d.attn_clusters[5]);
         return err;
     });
     if (e != cudaSuccess) cudaGetLastError();          // (reported by the call's return code)
@@ -124,20 +126,22 @@ bool cache_ok(const kvq_page_cache* c) {
     return c->dtype == KVQ_FP16 || c->dtype == KVQ_BF16;
 }
 
-// Resident CTAs of the attention, and what it keeps in the workspace: arrival counters, then two kinds of records.
-int attn_warps(int head_dim) { return head_dim == 64 ? AttnGeom<64>::kWarps : AttnGeom<128>::kWarps; }
+// The kernel's variants: 64 channels with 8 or 16 warps a CTA, 128 with 8; one or two blocks of eight heads.
+int attn_variant(int head_dim, int nt, int warps) { return (head_dim == 128 ? 4 : warps == 16 ? 2 : 0) + nt - 1; }
+int attn_resident(int sm_count, int head_dim, int warps) { return std::min(kAttnMaxCtas, sm_count * (1024 / (head_dim * warps))); }
+
+// What the attention keeps in the workspace: arrival counters, then two kinds of records.
 struct AttnSpace {
-    int ctas, nt;
-    size_t record, warp_at, cta_at, bytes;
+    int nt;
+    size_t warp_at, cta_at, bytes;
 };
 AttnSpace attn_space(int sm_count, int group, int head_dim) {
     AttnSpace s;
-    s.ctas = std::min(kAttnMaxCtas, sm_count);
     s.nt = group <= 8 ? 1 : 2;
-    s.record = (size_t)8 * s.nt * (head_dim + 2) * sizeof(float);
-    s.warp_at = (size_t)kAttnMaxCtas * sizeof(uint32_t);
-    s.cta_at = s.warp_at + (size_t)s.ctas * attn_warps(head_dim) * s.record;
-    s.bytes = s.cta_at + (size_t)s.ctas * 2 * s.record;
+    const size_t record = (size_t)8 * s.nt * (head_dim + 2) * sizeof(float), ctas = (size_t)attn_resident(sm_count, head_dim, 8);
+    s.warp_at = (size_t)kAttnCounters * sizeof(uint32_t);
+    s.cta_at = s.warp_at + ctas * 8 * record;          // (half as many CTAs of 16 warps need as much)
+    s.bytes = s.cta_at + ctas * 2 * kAttnAbreast * record;
     return s;
 }
 bool attn_shape_ok(int batch, int q_heads, int kv_heads, int head_dim) {
@@ -145,9 +149,12 @@ bool attn_shape_ok(int batch, int q_heads, int kv_heads, int head_dim) {
            q_heads % kv_heads == 0 && (head_dim == 64 || head_dim == 128);
 }
 
-template <bool BF, int D, int NT>
-int launch_attn(const PageAttnParams& p, uint64_t ctas, void* stream) {
-    return launch(k_page_attn<BF, D, NT>, ctas, AttnGeom<D>::kThreads, attn_smem<D>(p.batch), p.cluster > 1 ? p.cluster : 0, p, stream);
+template <bool BF, int D, int W>
+int launch_attn(const PageAttnParams& p, int nt, uint64_t ctas, void* stream) {
+    const size_t smem = attn_smem<D, W>(p.batch);
+    const int threads = AttnGeom<D, W>::kThreads, cluster = p.cluster > 1 ? p.cluster : 0;
+    return nt == 1 ? launch(k_page_attn<BF, D, 1, W>, ctas, threads, smem, cluster, p, stream)
+                   : launch(k_page_attn<BF, D, 2, W>, ctas, threads, smem, cluster, p, stream);
 }
 
 }  // namespace
@@ -270,21 +277,33 @@ int kvq_page_attn(const kvq_page_cache* cache, const void* Q, void* O, float* ls
     p.head_blocks = (p.group + 8 * space.nt - 1) / (8 * space.nt);
     p.scale2 = scale * kLog2e;
     p.by_page = FastDiv((uint32_t)cache->page_size);
-    // Clusters as wide as leaves one for every unit, with two tiles for every warp of the longest that the table could hold;
-    // as many CTAs as the tables could give a tile to every warp of, as far as they are resident together.
+    // Clusters as wide as leaves one for every unit, with two tiles for every warp of the longest that the table could hold.  CTAs
+    // of 8 warps, two to an SM, where that is enough (1 x 3000 tokens of 3 heads: 9.6 us, with 16 warps 12 us); of 16, so that a cluster
+    // has more warps, where the longest unit would give more than eight tiles to a warp of the widest (1 x 32768 of 5 heads: 16.6 us, with 8 18.7).
     const double units = (double)batch * p.kv_heads * p.head_blocks, longest = std::ceil((double)table_width * cache->page_size / kAttnTile);
-    const int warps = attn_warps(D), which = (D == 64 ? 0 : 2) + space.nt - 1;
-    p.cluster = 1;
-    while (p.cluster < kAttnMaxCluster && longest >= 2.0 * warps * (2 * p.cluster) && units <= d->attn_clusters[which][log2_of(2 * p.cluster)]) p.cluster *= 2;
-    const uint64_t most = p.cluster > 1 ? (uint64_t)d->attn_clusters[which][log2_of(p.cluster)] * p.cluster : (uint64_t)space.ctas;
-    const double wanted = std::max(units, std::ceil(units * longest / (warps * p.cluster))) * p.cluster;
-    const uint64_t ctas = (uint64_t)std::max((double)p.cluster, std::min((double)std::min<uint64_t>(most, space.ctas) / p.cluster * p.cluster, wanted));
+    auto widest = [&](int warps) {
+        const int* clusters = d->attn_clusters[attn_variant(D, space.nt, warps)];
+        int c = 1;
+        while (c < kAttnMaxCluster && longest >= 2.0 * warps * (2 * c) && units <= clusters[log2_of(2 * c)]) c *= 2;
+        return c;
+    };
+    int warps = 8;
+    p.cluster = widest(warps);
+    if (D == 64 && p.cluster == kAttnMaxCluster && longest > 8.0 * warps * p.cluster) p.cluster = widest(warps = 16);
+    // Where CTAs take equal shares of many units, two heads side by side in memory are read at the same time: 128 bytes of a row here and
+    // there cost DRAM more than 256 (16 x 8192 tokens of 32 heads, slot by slot: 173 us, with one at a time 199, four 174, sixteen 179).
+    p.abreast = p.cluster == 1 && p.slot_stride > p.head_stride && D == 64 && p.kv_heads * p.head_blocks % 2 == 0 ? kAttnAbreast : 1;
+    // as many CTAs as the tables could give a tile to every warp of, as far as they are resident together
+    const int resident = attn_resident(d->sm_count, D, warps);
+    const int most = p.cluster > 1 ? std::min(resident, p.cluster * d->attn_clusters[attn_variant(D, space.nt, warps)][log2_of(p.cluster)]) : resident;
+    const double wanted = std::max(units, std::ceil(units * longest / (warps * p.cluster)));       // clusters
+    const uint64_t ctas = (uint64_t)std::max(1.0, std::min((double)(most / p.cluster), wanted)) * p.cluster;
     if (cache->dtype == KVQ_BF16) {
-        if (D == 64) return space.nt == 1 ? launch_attn<true, 64, 1>(p, ctas, stream) : launch_attn<true, 64, 2>(p, ctas, stream);
-        return space.nt == 1 ? launch_attn<true, 128, 1>(p, ctas, stream) : launch_attn<true, 128, 2>(p, ctas, stream);
+        if (D == 128) return launch_attn<true, 128, 8>(p, space.nt, ctas, stream);
+        return warps == 8 ? launch_attn<true, 64, 8>(p, space.nt, ctas, stream) : launch_attn<true, 64, 16>(p, space.nt, ctas, stream);
     }
-    if (D == 64) return space.nt == 1 ? launch_attn<false, 64, 1>(p, ctas, stream) : launch_attn<false, 64, 2>(p, ctas, stream);
-    return space.nt == 1 ? launch_attn<false, 128, 1>(p, ctas, stream) : launch_attn<false, 128, 2>(p, ctas, stream);
+    if (D == 128) return launch_attn<false, 128, 8>(p, space.nt, ctas, stream);
+    return warps == 8 ? launch_attn<false, 64, 8>(p, space.nt, ctas, stream) : launch_attn<false, 64, 16>(p, space.nt, ctas, stream);
 }
 
 int kvq_beam_select(const void* logits, int dtype, const float* scores, const uint8_t* finished_opt, int batch, int beams,

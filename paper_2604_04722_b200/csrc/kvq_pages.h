@@ -59,10 +59,11 @@ struct PageAttnParams {
     float* lse;                    // [batch][q_heads] or nullptr
     const int32_t* tables;         // [batch][width]
     const int32_t* lens;           // [batch]
-    uint32_t* arrivals;            // [CTAs], zero between launches
+    uint32_t* arrivals;            // [CTAs][2], zero between launches
     float* warp_rec;               // [CTAs][warps] records of R (D + 2) floats
-    float* cta_rec;                // [CTAs][2] records
+    float* cta_rec;                // [CTAs][2 abreast][2] records
     int width, batch, n_pages, page_size, q_heads, kv_heads, group, head_blocks;
+    int abreast;                   // units of a row that a CTA's warps may take side by side: 1 or 2, divides kv_heads * head_blocks
     int cluster;                   // CTAs that share a stretch of the axis and meet through shared memory (1: no clusters)
     float scale2;                  // softmax scale in log2 units
     FastDiv by_page;
