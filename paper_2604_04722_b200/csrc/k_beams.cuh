@@ -84,29 +84,25 @@ __device__ __noinline__ void warp_best(BeamPick* buffer, int count, int n) {
     __syncwarp();
 }
 
-// A score that n of a warp's candidates (0: none, K per lane) reach, and few more: distances from the best one in steps of 2^-10,
-// the smallest number of steps that n of them keep within, one bit after the other.  0: fewer than n within 64.
+// A score that n of a warp's candidates (0: none, K per lane) reach, and not many more: the n-th best of the lanes' best ones, rounded down to
+// fp32; 0 if fewer than n lanes have one.  (256 candidates, n = 4 / 16 / 32: about 4 / 21 / 90 reach it if they lie as they please; an
+// exact bound took 1.8 us, this one 0.4.)
 template <int K>
 __device__ __forceinline__ uint64_t warp_bound(const uint64_t (&mine)[K], int n) {
+    const int lane = threadIdx.x & 31;
     uint64_t top = mine[0];
 #pragma unroll
     for (int k = 1; k < K; ++k) top = mine[k] > top ? mine[k] : top;
-    const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(top >> 32));
-    const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(top >> 32) == hi ? (uint32_t)top : 0u);
-    const double best = key_score(((uint64_t)hi << 32) | lo);
-    uint32_t left[K];                                  // 2^16 - 1 less the steps; 0: farther away, or none
+    float v = top ? __double2float_rd(key_score(top)) : -INFINITY;
 #pragma unroll
-    for (int k = 0; k < K; ++k) left[k] = mine[k] ? 65535u - (uint32_t)fmin((best - key_score(mine[k])) * 1024.0, 65535.0) : 0u;
-    uint32_t prefix = 0;
-#pragma unroll 1
-    for (int bit = 15; bit >= 0; --bit) {
-        const uint32_t next = prefix | (1u << bit);
-        int reach = 0;
+    for (int size = 2; size <= 32; size <<= 1)         // a bitonic sort, descending
 #pragma unroll
-        for (int k = 0; k < K; ++k) reach += left[k] >= next;
-        if (__reduce_add_sync(0xffffffffu, reach) >= n) prefix = next;
-    }
-    return prefix == 0 ? 0ull : score_key(best - (double)(65537u - prefix) * (1.0 / 1024.0));      // (one step for the roundings)
+        for (int d = size >> 1; d > 0; d >>= 1) {
+            const float o = __shfl_xor_sync(0xffffffffu, v, d);
+            v = ((lane & d) == 0) == ((lane & size) == 0) ? fmaxf(v, o) : fminf(v, o);
+        }
+    v = __shfl_sync(0xffffffffu, v, n - 1);
+    return v > -INFINITY ? score_key((double)v) : 0ull;
 }
 
 // Two fp32 operations in one instruction.
@@ -180,7 +176,8 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
     __shared__ double s_sum[kBeamMaxSlices];           // ... and sum of exponentials relative to it
     __shared__ float s_row_top[kMaxBeams];
     __shared__ double s_row_off[kMaxBeams];            // score - log of the sum
-    __shared__ uint8_t s_alive[kMaxBeams];
+    __shared__ uint8_t s_alive[kMaxBeams], s_over[kMaxBeams];
+    __shared__ float s_score[kMaxBeams];
     __shared__ float s_group_top[kBeamWarps * kBeamGroups];
     __shared__ uint64_t s_group_best[kBeamWarps * kBeamGroups];            // score of that logit, 0 without candidates
     __shared__ uint64_t s_bound;
@@ -190,8 +187,9 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
     const int n = P.n_out;
     const int tasks = P.beams * P.slices, warps = ctas * kBeamWarps, gwarp = rank * kBeamWarps + warp;
     const int rounds = (tasks + warps - 1) / warps;    // slices of a warp, at most kBeamTasks
-    const int per_slice = kBeamGroups / rounds;        // groups
-    const int group_len = ((P.slice_len + kBeamChunk * per_slice - 1) / (kBeamChunk * per_slice)) * kBeamChunk;        // entries
+    const int most_groups = kBeamGroups / rounds, chunks = (P.slice_len + kBeamChunk - 1) / kBeamChunk;
+    const int group_len = (chunks + most_groups - 1) / most_groups * kBeamChunk;           // entries of a group
+    const int per_slice = (P.slice_len + group_len - 1) / group_len, groups = kBeamWarps * rounds * per_slice;     // groups of a slice, of the CTA
     BeamPick* s_buffers = reinterpret_cast<BeamPick*>(s_dyn);              // [warps][kBeamBuffer]
     BeamPick* s_picks = s_buffers + kBeamWarps * kBeamBuffer;              // [threads]
     BeamPick* s_sent = s_picks + kBeamThreads;                             // [CTAs][n]
@@ -203,6 +201,11 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
     cluster.barrier_arrive();                          // (before another CTA's memory is written, all of them have to be there)
     pdl_launch_dependents();
     pdl_wait();
+    if (tid < P.beams) {
+        const size_t r = (size_t)b * P.beams + tid;
+        s_score[tid] = P.scores[r];
+        s_over[tid] = P.finished && P.finished[r] != 0;
+    }
 
     // a warp's view of a slice: whole vectors, if they lie within the tensor
     struct Slice {
@@ -248,13 +251,13 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
         if (task < tasks) {
             const int row = task % P.beams;
             const size_t r = (size_t)b * P.beams + row;
-            float* groups = s_group_top + warp * kBeamGroups + j * per_slice;
+            float* tops = s_group_top + (warp * rounds + j) * per_slice;
             const Slice v = slice_of(task);
             uint4 raw[kLoads];
             load(v, v.lo, raw);                        // (of rows that are out no more than this is read)
             const bool over = P.finished && P.finished[r] != 0, alive = isfinite(P.scores[r]);
             if (over) {                                // one candidate: the end token at the score as it is
-                if (task < P.beams) top = 0.f, sum = lane == 0 ? 1.0 : 0.0, groups[0] = 0.f;
+                if (task < P.beams) top = 0.f, sum = lane == 0 ? 1.0 : 0.0, tops[0] = 0.f;
             } else if (alive) {
                 float most = -INFINITY;
                 int g = 0, next = v.lo + group_len;
@@ -282,7 +285,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
                     most = fmaxf(most, here);
                     if (c0 + kBeamChunk >= min(next, v.hi)) {
                         most = warp_max(most);
-                        if (lane == 0) groups[g] = most;
+                        if (lane == 0) tops[g] = most;
                         ++g;
                         next += group_len;
                         most = -INFINITY;
@@ -314,7 +317,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         if (lane == 0) {
-            const float score = P.scores[(size_t)b * P.beams + row];
+            const float score = s_score[row];
             s_row_top[row] = top;
             s_row_off[row] = (double)score - log(sum);
             s_alive[row] = isfinite(score) && isfinite(sum) && sum > 0.0 && isfinite(top);
@@ -322,11 +325,17 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
     }
     __syncthreads();
     // ---- a bound: the n-th best of the CTA's groups' largest entries, which n of its candidates reach
+    auto slice_of_group = [&](int group, int& g) {     // the slice (task) of a group and its number there
+        const int slot = group / per_slice, w = rounds == 1 ? slot : slot / rounds;
+        g = group - slot * per_slice;
+        return rank * kBeamWarps + w + (slot - w * rounds) * warps;
+    };
     uint64_t best = 0;                                 // of this thread's group
     if (tid < kBeamWarps * kBeamGroups) {
-        const int w = tid / kBeamGroups, j = tid % kBeamGroups / per_slice, task = rank * kBeamWarps + w + j * warps, row = task % P.beams;
+        int g;
+        const int task = slice_of_group(min(tid, groups - 1), g), row = task % P.beams;
         const float top = s_group_top[tid];
-        if (j < rounds && task < tasks && s_alive[row] && top > -INFINITY) best = score_key(s_row_off[row] + ((double)top - (double)s_row_top[row]));
+        if (tid < groups && task < tasks && s_alive[row] && top > -INFINITY) best = score_key(s_row_off[row] + ((double)top - (double)s_row_top[row]));
         s_group_best[tid] = best;
     }
     __syncthreads();
@@ -351,8 +360,8 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
             const int listed = s_listed;
 #pragma unroll 1
             for (int i = warp; i < listed; i += kBeamWarps) {
-                const int group = s_list[i], j = group % kBeamGroups / per_slice;
-                const int task = rank * kBeamWarps + group / kBeamGroups + j * warps, row = task % P.beams;
+                int g;
+                const int task = slice_of_group(s_list[i], g), row = task % P.beams;
                 const double off = s_row_off[row];
                 const float row_top = s_row_top[row];
                 auto score_of = [&](float x) { return score_key(off + ((double)x - (double)row_top)); };
@@ -369,7 +378,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
                     if (mine_in) buffer[count + __popc(in & ((1u << lane) - 1))] = p;
                     count += __popc(in);
                 };
-                if (P.finished && P.finished[(size_t)b * P.beams + row] != 0) {
+                if (s_over[row]) {
                     keep(lane == 0, BeamPick{score_of(0.f), (uint32_t)row, (uint32_t)P.end_token});
                     continue;
                 }
@@ -378,7 +387,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
                 float least = -FLT_MAX;
                 if (at_least != 0) least = fmaxf(least, nextafterf(__double2float_rd((key_score(at_least) - off) + (double)row_top), -INFINITY));
                 const Slice v = slice_of(task);
-                const int begin = v.lo + (group % kBeamGroups - j * per_slice) * group_len;
+                const int begin = v.lo + g * group_len;
 #pragma unroll 1
                 for (int c0 = begin; c0 < min(v.hi, begin + group_len); c0 += kBeamChunk) {
                     uint4 raw[kLoads];
@@ -423,47 +432,48 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
     // Ranks `count` candidates, one per thread at most, and calls put(rank, candidate) in one lane for each of the n best: those
     // that reach the bound are listed, then a warp per candidate counts the better ones.  (The order in which they lie does not matter.)
     auto rank_all = [&](const BeamPick* list, int count, auto put) {
-        const uint64_t mine = tid < count ? list[tid].score : 0ull;
-        if (warp == 0) {
-            uint64_t least = 0;
-            if (count > 2 * n) {
+        const bool few = count <= 96;                  // (looking for the bound takes as long as ranking so many)
+        int listed = count;
+        if (!few) {
+            if (warp == 0) {
                 uint64_t some[kBeamThreads / 32];
 #pragma unroll
                 for (int k = 0; k < kBeamThreads / 32; ++k) some[k] = 32 * k + lane < count ? list[32 * k + lane].score : 0ull;
-                least = warp_bound(some, n);
+                const uint64_t least = warp_bound(some, n);
+                if (lane == 0) s_bound = least, s_listed = 0;
             }
-            if (lane == 0) s_bound = least, s_listed = 0;
+            __syncthreads();
+            const uint64_t mine = tid < count ? list[tid].score : 0ull;
+            if (mine != 0 && mine >= s_bound) s_list[atomicAdd(&s_listed, 1)] = (uint16_t)tid;
+            __syncthreads();
+            listed = s_listed;
         }
-        __syncthreads();
-        const uint64_t least = s_bound;
-        if (mine != 0 && mine >= least) s_list[atomicAdd(&s_listed, 1)] = (uint16_t)tid;
-        __syncthreads();
-        const int listed = s_listed;
         for (int i = warp; i < listed; i += kBeamWarps) {
-            const BeamPick p = list[s_list[i]];
+            const BeamPick p = list[few ? i : s_list[i]];
+            if (p.score == 0) continue;
             int better = 0;
-            for (int o = lane; o < listed; o += 32) better += list[s_list[o]].before(p);
+            for (int o = lane; o < listed; o += 32) better += list[few ? o : s_list[o]].before(p);
             better = __reduce_add_sync(0xffffffffu, better);
             if (better < n && lane == 0) put(better, p);
         }
-        return listed;
     };
     static_assert(kBeamWarps * kMaxBeams <= kBeamThreads && kBeamMaxCluster * kMaxBeams <= kBeamThreads, "a thread per candidate");
     // ---- the CTA's n best go to the first CTA, which joins those of all
     {
         BeamPick* to = cluster.map_shared_rank(s_sent, 0) + rank * n;
-        const int listed = rank_all(s_picks, s_picked, [&](int i, const BeamPick& p) { to[i] = p; });
-        for (int i = listed + tid; i < n; i += kBeamThreads) to[i] = no_pick();
+        rank_all(s_picks, s_picked, [&](int i, const BeamPick& p) { to[i] = p; });
+        for (int i = s_picked + tid; i < n; i += kBeamThreads) to[i] = no_pick();
     }
     cluster.sync();
     if (rank != 0) return;
-    const int found = rank_all(s_sent, ctas * n, [&](int i, const BeamPick& p) {
+    rank_all(s_sent, ctas * n, [&](int i, const BeamPick& p) {
         const size_t at = (size_t)b * n + i, from = (size_t)b * P.beams + p.row;
         P.parents[at] = (int32_t)from;
         P.tokens[at] = (int32_t)p.token;
         P.scores_out[at] = (float)key_score(p.score);
-        if (P.finished_out) P.finished_out[at] = (int32_t)p.token == P.end_token || (P.finished && P.finished[from] != 0);
+        if (P.finished_out) P.finished_out[at] = (int32_t)p.token == P.end_token || s_over[p.row];
     });
+    const int found = __syncthreads_count(tid < ctas * n && s_sent[tid].score != 0);   // candidates in all
     for (int i = found + tid; i < n; i += kBeamThreads) {
         const size_t at = (size_t)b * n + i;
         P.parents[at] = P.tokens[at] = -1;
