@@ -3,9 +3,9 @@
 // kRescaleSlack, so that the sums are rescaled a few times per unit instead of at every tile.
 //
 // A UNIT is a (sequence, KV head, block of 8 NT query heads).  The tiles of 16 tokens of all units lie end to end on an axis that
-// is cut into equal stretches, one per warp of the launch, whatever the lengths: a warp streams the rows of its stretch through
-// a ring of shared-memory stages of its own (16-byte asynchronous copies; page numbers are looked up one tile ahead) and never
-// waits for another warp.  The lengths are on the device, so every CTA adds them up for itself.
+// is cut into stretches for the launch's CTAs, and those into equal parts for their warps, whatever the lengths: a warp streams the
+// rows of its part through a ring of shared-memory stages of its own (16-byte asynchronous copies; page numbers are looked up one
+// tile ahead) and never waits for another warp before its last tile.  The lengths are on the device, so every CTA adds them up for itself.
 //
 // Heads are the columns of the matrix instructions (m16n8k16): logits = K q^T with the 16 tokens of a tile as rows, and
 // o^T = V^T w^T with the channels as rows, so that up to 8 query heads cost the same as one, K and V fragments are read with one
@@ -14,9 +14,15 @@
 // bytes the second product costs nothing, and with 8-bit mantissas (bf16) one rounding of the weights would be as large as the
 // output's own.  Sums are fp32.
 //
-// A unit that ends inside a warp's stretch is written by that warp.  Pieces of a unit meet in their CTA, and what is left
-// over at the borders of a CTA's stretch meets in records of the workspace: the CTA that delivers a unit's last record joins them,
-// in the order of the axis whoever comes last.  Bound: the rows' bytes, 4 D per token and KV head.
+// A unit that begins and ends with one warp is written by that warp.  Pieces of a unit meet in their CTA.  Where there are few
+// units a cluster of up to 16 CTAs takes one, and its CTAs meet through shared memory (1 x 32768 tokens of 5 KV heads: 16.6 us; the same
+// through global records 27, and before the borders below moved, 130).  Where there are more units than that, CTAs take equal shares of
+// the axis, a share's border moves to a unit's if that is near, and what is left over meets in records of the workspace: the CTA that
+// delivers a unit's last record joins them, in the order of the axis whoever comes last.
+//
+// Bound: the rows' bytes, 4 D per token and KV head.  1.07 GB of 32 heads of 64 channels (16 x 8192 tokens, fp16, slot by slot) take 173 us,
+// 6.2 TB/s or 0.94 of the copy rate; 0.79 GB of 8 heads of 128 (64 x 4096 at most, bf16) 134 us, 0.90.  Small calls are a chain of memory
+// round trips (lengths, tables, rows), a tile's dependent instructions and the joins: 1 x 512 tokens 8 us.
 #pragma once
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
@@ -33,7 +39,8 @@ constexpr int kAttnCounters = kAttnMaxCtas * kAttnAbreast;     // arrival counte
 constexpr int kAttnUnitTiles = 20;                     // of a warp at most, where clusters take a unit each
 constexpr int kAttnMaxCluster = 16;
 constexpr int kAttnMinTilesLog2 = 1, kAttnMinTiles = 1 << kAttnMinTilesLog2;   // of a warp, where the work does not fill the launch
-constexpr int kAttnSnapBytes = 2048;                   // times 64: see `border`
+// How far a border may be from a unit's to move there: what a CTA streams in about the time that a join takes (3 us).
+constexpr int kAttnSnapBytes = 131072;
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLn2 = 0.69314718055994531f;
 
@@ -140,17 +147,18 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
     // ---- lengths, and tiles before every row
     const int units_per_row = P.kv_heads * P.head_blocks;
     {
-        const int per = (P.batch + kAttnThreads - 1) / kAttnThreads;
+        const int per = (P.batch + kAttnThreads - 1) / kAttnThreads;       // neighbouring rows of a thread
         const long long room = (long long)P.width * P.page_size;
-        auto read_len = [&](int b) { return (int)min((long long)max(P.lens[b], 0), room); };
         auto tiles = [&](int n) { return (n + (long long)kAttnTile - 1) / kAttnTile; };
+#pragma unroll 4
+        for (int b = tid; b < P.batch; b += kAttnThreads) s_place[b] = min((long long)max(P.lens[b], 0), room);        // for now
+        if (per > 1) __syncthreads();
         int64_t sum = 0;
         int most = 0;
         for (int k = 0; k < per; ++k) {
             const int b = tid * per + k;
             if (b >= P.batch) break;
-            const int n = read_len(b);
-            s_place[b] = n;                            // for now
+            const int n = (int)s_place[b];
             sum += tiles(n);
             most = max(most, (int)tiles(n));
         }
@@ -179,6 +187,7 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
         __syncthreads();
     }
     uint16_t* const O = static_cast<uint16_t*>(P.O);
+    auto inverse = [](float l) { return l > 0.f || l != l ? 1.f / l : 0.f; };      // (a row that sees nothing gives zeros, a NaN stays one)
     // rows without a token
     for (int b = blockIdx.x; b < P.batch; b += gridDim.x) {
         if (tiles_of(b) != 0) continue;
@@ -197,7 +206,7 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
     // With equal shares `abreast` units of a row that lie side by side in memory go abreast, each with its share of the CTA's warps
     // (member: which of them this warp works on); the axis then consists of such bundles of units.
     const int abreast = unit_each ? 1 : P.abreast, team = kAttnWarps / abreast, member = warp / team;
-    const int bundles_per_row = units_per_row / abreast, snap = kAttnSnapBytes / D / abreast;
+    const int bundles_per_row = units_per_row / abreast, snap = kAttnSnapBytes / (G::kStageBytes * abreast);
     const int warps = C * team, warps_log2 = __ffs(warps) - 1;             // that share a stretch (a power of two)
     const int64_t total = tiles_before(P.batch) * bundles_per_row;
     const int stretches = unit_each ? units : (int)min((int64_t)groups, ((total + warps * kAttnMinTiles - 1) >> (warps_log2 + kAttnMinTilesLog2)));
@@ -219,7 +228,8 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
         return c;
     };
     // The borders between equal shares move to the border of a unit that is no more than snap tiles away.
-    const int64_t share_size = unit_each ? 0 : (total >> 32) == 0 ? (int64_t)((uint32_t)total / (uint32_t)stretches) : total / stretches, share_more = total - share_size * stretches;     // (the first share_more have one tile more)
+    const int64_t share_size = unit_each ? 0 : (total >> 32) == 0 ? (int64_t)((uint32_t)total / (uint32_t)stretches) : total / stretches;
+    const int64_t share_more = total - share_size * stretches;             // (the first share_more have one tile more)
     auto share = [&](int c) -> int64_t { return share_size * c + min((int64_t)c, share_more); };
     auto border = [&](int c) -> int64_t {
         if (c == stretches) return total;
@@ -351,8 +361,7 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
             const int h0 = P.head_blocks == 1 ? unit_of(at) : unit_of(at) / P.head_blocks, hb = unit_of(at) - h0 * P.head_blocks;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                const float i0 = l[nt][0] > 0.f || l[nt][0] != l[nt][0] ? 1.f / l[nt][0] : 0.f;
-                const float i1 = l[nt][1] > 0.f || l[nt][1] != l[nt][1] ? 1.f / l[nt][1] : 0.f;
+                const float i0 = inverse(l[nt][0]), i1 = inverse(l[nt][1]);
                 const int r = hb * kR + nt * 8 + g;
                 const size_t row = (size_t)at.b * P.q_heads + h0 * P.group + r;
 #pragma unroll
@@ -488,7 +497,6 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
     Factors& s_f = *reinterpret_cast<Factors*>(s_ring_all + G::kRingBytes - sizeof(Factors));
     auto last_piece = [&](int w) { return reinterpret_cast<const float*>(s_ring_all + (size_t)w * G::kRingBytes); };
     auto first_piece = [&](int w) -> const float* { return P.warp_rec + ((size_t)blockIdx.x * kAttnWarps + w) * kRec; };
-    auto inverse = [](float l) { return l > 0.f || l != l ? 1.f / l : 0.f; };
     struct Place {
         size_t row;                                    // of the block's first head
         int heads;
