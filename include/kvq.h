@@ -345,7 +345,7 @@ int kvq_verify_tree(const float* target, const float* draft_opt, const int32_t* 
  * Keys and values of one layer lie in n_pages pages of page_size slots; element (page, slot, head, channel) is at
  * K + page * page_stride + slot * slot_stride + head * head_stride + channel (in elements; V the same), so that pages may be kept slot by slot or
  * head by head, and keys and values in one tensor.  K and V dev, 16-byte aligned; strides multiples of 8, not negative.
- * head_dim a multiple of 8 (kvq_page_attn: 64 or 128); dtype KVQ_FP16 or KVQ_BF16; n_pages <= KVQ_MAX_PAGES.  A request's
+ * head_dim a multiple of 8 (kvq_page_attn: 64 or 128); dtype KVQ_FP16 or KVQ_BF16.  A request's
  * row of a block table (int32) lists its pages in order; its token at position t is in slot t % page_size of entry t / page_size.  A page
  * that is not full is listed by one row only; full ones may be shared.
  */
@@ -353,7 +353,7 @@ int kvq_verify_tree(const float* target, const float* draft_opt, const int32_t* 
 #define KVQ_BF16 1
 #define KVQ_FP32 2
 #define KVQ_MAX_PAGE_ROWS 4096                /* requests (beams) of a batch */
-#define KVQ_MAX_PAGES 1048576                 /* pages of a cache */
+#define KVQ_MAX_PAGES 1048576                 /* pages of kvq_page_step */
 typedef struct kvq_page_cache {
     void* K;
     void* V;
@@ -379,7 +379,8 @@ typedef struct kvq_page_cache {
  *   status        dev uint32 [1]: 0, or KVQ_PAGE_* bits, and then the step did not take place: tables_out and lens_out hold
  *                 what tables_in and lens_in hold, cu_new zeros, slots, positions and copies -1
  * New pages are the free ones in ascending order, taken in row order.  Entries of tables_out behind a row's pages are left as
- * they were (unspecified after a step that did not take place, unless tables_out is tables_in).  table_width >= 1, 0 <= batch <= KVQ_MAX_PAGE_ROWS.  One launch.
+ * they were (unspecified after a step that did not take place, unless tables_out is tables_in).  table_width, page_size >= 1,
+ * 1 <= n_pages <= KVQ_MAX_PAGES, 0 <= batch <= KVQ_MAX_PAGE_ROWS.  One launch.
  */
 #define KVQ_PAGE_FULL 1u                      /* not enough free pages */
 #define KVQ_PAGE_LONG 2u                      /* a row would not fit table_width pages */

@@ -119,7 +119,7 @@ int launch(Kernel kernel, uint64_t ctas, int threads, size_t smem, int cluster, 
 
 bool cache_ok(const kvq_page_cache* c) {
     if (!c || !c->K || !c->V || !aligned(c->K, 16) || !aligned(c->V, 16)) return false;
-    if (c->n_pages < 1 || c->n_pages > KVQ_MAX_PAGES || c->page_size < 1 || c->kv_heads < 1 || c->kv_heads > 1024) return false;
+    if (c->n_pages < 1 || c->page_size < 1 || c->kv_heads < 1 || c->kv_heads > 1024) return false;
     if (c->head_dim < 8 || c->head_dim % 8 != 0 || c->head_dim > 1024) return false;
     for (int64_t s : {c->page_stride, c->slot_stride, c->head_stride})
         if (s < 0 || s % 8 != 0) return false;

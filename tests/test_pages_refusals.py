@@ -34,7 +34,7 @@ def test_step_refusals(kq, change):
 
 CACHE = dict(K=A, V=2 * A, page_stride=16 * 3 * 64, slot_stride=3 * 64, head_stride=64, n_pages=8, page_size=16, kv_heads=3, head_dim=64, dtype=0)
 BAD_CACHES = [dict(K=None), dict(V=None), dict(K=A + 8), dict(V=A + 2), dict(page_stride=4), dict(slot_stride=-64), dict(head_stride=65),
-              dict(n_pages=0), dict(n_pages=(1 << 20) + 1), dict(page_size=0), dict(kv_heads=0), dict(head_dim=0), dict(head_dim=60), dict(dtype=2),
+              dict(n_pages=0), dict(n_pages=-1), dict(page_size=0), dict(kv_heads=0), dict(head_dim=0), dict(head_dim=60), dict(dtype=2),
               dict(dtype=-1)]
 
 
