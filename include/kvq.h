@@ -340,7 +340,8 @@ int kvq_verify_tree(const float* target, const float* draft_opt, const int32_t* 
 /*
  * A paged 16-bit cache: requests that come and go one by one, and that share the pages of a prompt.  (The paper's FP16
  * baseline in the form in which a server holds it, beside the mixed-precision cache above, whose rows live until kvq_reset.)
- * The caller owns all memory; none of these calls needs a handle, and the buffers belong to the current device.
+ * The caller owns all memory; none of these calls needs a handle, and the buffers belong to the current device.  The first of these calls on a
+ * device asks it for its limits and belongs before any stream capture; captured ones follow lengths, tables and parents, which are on the device.
  *
  * Keys and values of one layer lie in n_pages pages of page_size slots; element (page, slot, head, channel) is at
  * K + page * page_stride + slot * slot_stride + head * head_stride + channel (in elements; V the same), so that pages may be kept slot by slot or
@@ -402,11 +403,14 @@ int kvq_page_append(const kvq_page_cache* cache, const void* K, const void* V, c
 /*
  * Attention of one new token per request over its pages: O = Softmax(scale * q K^T) V over the first lens[b] tokens, query head h
  * reading KV head h / (q_heads / kv_heads).  Q, O: dev [batch][q_heads][head_dim] of the cache's type, 16-byte aligned; lse_opt
- * dev fp32 [batch][q_heads] or NULL: the logarithm of the sum of exponentials.  A row of length 0 (or less) gets zeros and -inf; lengths beyond
- * the table count as its width.  Slots behind a row's length may hold anything, and tokens on pages outside the cache (such as
- * -1) do not take part.  Sums are fp32; the cut of the work does not depend on the order in which CTAs run, so equal calls give equal bits.
- * workspace: dev, 16-byte aligned, at least kvq_page_attn_workspace_bytes (host uint64; KVQ_ERR_NOMEM if less), zero before its first use; every
- * call leaves it ready for the next, of any shape.  Calls that may overlap on the device need a workspace each.  One launch.
+ * dev fp32 [batch][q_heads] or NULL: the logarithm of the sum of exponentials.  A row of length 0 (or less) gets zeros and
+ * -inf; lengths beyond the table count as its width.  Slots behind a row's length may hold anything, and tokens on pages outside
+ * the cache (such as -1) do not take part.  A value that is not finite makes NaN of its channel, and a key that is not of the
+ * whole row, in the heads that read it.  Sums are fp32; equal calls give equal bits (the cut of the work does not depend on the
+ * order in which CTAs run).
+ * workspace: dev, 16-byte aligned, at least kvq_page_attn_workspace_bytes (host uint64; KVQ_ERR_NOMEM if less), zero before its
+ * first use; every call leaves it ready for the next, of any shape.  Calls that may overlap on the device, captured ones too,
+ * need a workspace each.  0 <= batch <= KVQ_MAX_PAGE_ROWS (0 is a no-op), scale finite, table_width >= 1.  One launch.
  */
 int kvq_page_attn_workspace_bytes(int batch, int q_heads, int kv_heads, int head_dim, uint64_t* bytes_out);
 int kvq_page_attn(const kvq_page_cache* cache, const void* Q, void* O, float* lse_opt, const int32_t* tables, int table_width,

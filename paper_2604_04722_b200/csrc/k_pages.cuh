@@ -10,8 +10,10 @@
 // One cluster does it all; every CTA computes what concerns rows for itself (lengths, prefix sums: no exchange), and marks
 // in a bitmap of its own (one bit a page, shared memory) the pages that its part of the tables lists.  After a cluster barrier CTA r joins
 // slice r of all bitmaps; the free pages of the slices are counted, one more barrier, and a warp hands out the free pages of a
-// word with one bit per lane.  The last barrier makes the tables visible to the threads that write the slots.  The kernel is a chain of
-// round trips (lengths, tables, three cluster barriers, slots): see the figures at kPageStepCluster.
+// word with one bit per lane.  The last barrier makes the tables visible to the threads that write the slots.
+//
+// Bound: a chain of round trips (lengths, tables, three cluster barriers, slots) and scans: 7 us for 8 rows of 2048 tokens, 10 us for 256
+// rows of 4 beams and up to 4096, 11 us for 36096 slots; what it reads and writes would take 0.1.
 #pragma once
 #include <cooperative_groups.h>
 #include "kvq_common.cuh"
@@ -19,6 +21,7 @@
 
 namespace kvq {
 
+// 512 rows of 8192 tokens take 18 us, with 4 CTAs 26 and with 2 39; 8 rows 7 us with any of them.  1024 threads a CTA: 8 rows 10 us, 256: 512 rows 25 us.
 constexpr int kPageStepThreads = 512, kPageStepWarps = kPageStepThreads / 32;
 constexpr int kPageStepCluster = 8;
 
@@ -335,7 +338,8 @@ __global__ void __launch_bounds__(kPageStepThreads, 1) k_page_step(const PageSte
 }
 
 // Rows to their slots, and the used part of the pages that a step copied: 16-byte vectors, no row is touched twice.  The first
-// copy_blocks CTAs take a copy each.  Bound by the rows' bytes, once in and once out.
+// copy_blocks CTAs take a copy each.  Bound by the rows' bytes, once in and once out: 15000 rows of 32 heads (246 MB) take 38.9 us, 6.3 TB/s or
+// 0.97 of the copy rate; a few rows 2 us.
 constexpr int kPageAppendThreads = 256, kPageAppendVecs = 4;
 
 __global__ void __launch_bounds__(kPageAppendThreads) k_page_append(const PageAppendParams P) {

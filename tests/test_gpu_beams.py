@@ -75,6 +75,27 @@ def test_selection(kq, B, W, n, V, kind):
     _check(kq, _logits(V + W, B, W, V, dtype), _scores(V, B, W), None, n, -1)
 
 
+@pytest.mark.parametrize("seed", range(40))
+def test_selection_of_any_shape(kq, seed):
+    """Any shape, spread of logits and scores (one beam may hold all of the best), masks, ended beams, first steps, rounded logits with ties."""
+    import torch
+    rng = np.random.default_rng(seed)
+    B, W, V = int(np.exp(rng.uniform(0, np.log(120)))), int(rng.integers(1, 33)), int(np.exp(rng.uniform(0, np.log(60000))))
+    while B * W * V > 3e6:
+        B, V = max(1, B // 2), V if B > 1 else V // 2
+    z = _logits(seed, B, W, V, _dtypes()[rng.integers(3)], float(rng.choice([0.01, 1, 3, 10])))
+    if rng.random() < 0.2:
+        z = z.round()
+    if rng.random() < 0.2:
+        z[torch.rand(z.shape, device="cuda") < 0.5] = -math.inf
+    s = -rng.uniform(0, float(rng.choice([0.1, 3, 30])), (B, W)).astype(np.float32)
+    if rng.random() < 0.2:
+        s[:, 1:] = -np.inf
+    end = int(rng.integers(-1, V))
+    finished = (rng.random((B, W)) < rng.choice([0.2, 0.9])).astype(np.uint8) if end >= 0 and rng.random() < 0.5 else None
+    _check(kq, z, s, finished, int(rng.choice([W, rng.integers(1, 33)])), end)
+
+
 @pytest.mark.parametrize("B", [18, 40, 100, 300])
 def test_many_requests(kq, B):
     """Every width of the cluster that the launch picks."""

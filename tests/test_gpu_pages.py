@@ -293,14 +293,15 @@ class Attn:
         self.kq.kvq_page_attn(self.cache, self.Q, self.O, self.lse if lse else None, self.tables, self.width, self.n, len(self.lens), self.Hq,
                               self.scale, self.work, self.bytes)
 
-    def check(self, heads=None):
+    def check(self, heads=None, pairs=None):
+        """Every (row, KV head), those of some heads, or only some pairs."""
         import torch
         torch.cuda.synchronize()
         O, lse, Q = self.O.double().cpu().numpy(), self.lse.double().cpu().numpy(), self.Q.double().cpu().numpy()
         G, worst = self.Hq // self.H, 0.0
         for b, (k, v) in enumerate(self.rows):
             k, v = k[self.live[b]], v[self.live[b]]
-            for h in heads or range(self.H):
+            for h in [h for h in (heads or range(self.H)) if pairs is None or (b, h) in pairs]:
                 at = slice(h * G, h * G + G)
                 o, l, err, lerr = pr.attend(Q[b, at], k[:, h], v[:, h], self.scale, self.mantissa)
                 assert np.all(np.isfinite(O[b, at])), (b, h)
@@ -311,7 +312,7 @@ class Attn:
                     worst = max(worst, over.max())
                 else:
                     assert np.all(lse[b, at] == -math.inf) and not O[b, at].any()
-        assert not self.work[:4096].any()              # the counters are back at zero
+        assert not self.work[:8192].any()              # the counters are back at zero
         return worst
 
 
@@ -340,6 +341,34 @@ def test_attention_split_over_many_warps(kq, lens, q_heads, kv_heads, D):
     a = Attn(kq, lens, q_heads, kv_heads, D, 16, "fp16", seed=len(lens))
     a.call()
     a.check(heads=range(min(kv_heads, 3)))
+
+
+@pytest.mark.parametrize("q_heads,kv_heads,D,rows", [(42, 2, 64, 90), (33, 1, 64, 100), (64, 2, 128, 90), (10, 10, 64, 40), (6, 6, 64, 33)])
+@pytest.mark.parametrize("order", ["slots", "heads"])
+def test_attention_of_many_rows_and_heads_side_by_side(kq, q_heads, kv_heads, D, rows, order):
+    """Equal shares of the work, of one unit at a time and of two, with borders inside units and moved ones."""
+    rng = np.random.default_rng(rows)
+    lens = np.where(rng.random(rows) < 0.2, 0, rng.integers(1, 1500, rows))
+    a = Attn(kq, lens, q_heads, kv_heads, D, 16, "fp16", order, seed=rows)
+    a.call()
+    a.check(pairs={(b, h) for b in range(0, rows, 3) for h in range(kv_heads)})
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_attention_of_any_shape(kq, seed):
+    rng = np.random.default_rng(seed)
+    kv, group, D = int(rng.choice([1, 2, 3, 4, 5, 8, 12])), int(rng.choice([1, 2, 3, 7, 8, 9, 16, 17, 33])), int(rng.choice([64, 64, 128]))
+    rows, top = int(np.exp(rng.uniform(0, np.log(300)))), int(np.exp(rng.uniform(0, np.log(20000))))
+    while rows * kv * top * D > 5e7:
+        rows, top = max(1, rows // 2), top if rows > 1 else top // 2
+    kind = rng.integers(3)
+    lens = [rng.integers(0, top + 1, rows), np.full(rows, top), np.where(rng.random(rows) < 0.1, top, rng.integers(0, max(2, top // 20), rows))][kind]
+    page = int(rng.choice([1, 5, 8, 16, 24, 64, 200]))
+    a = Attn(kq, lens, kv * group, kv, D, page, str(rng.choice(["fp16", "bf16"])), str(rng.choice(["slots", "heads", "together"])), seed=seed,
+             width=max(1, -(-int(max(lens)) // page)) * int(rng.choice([1, 1, 4])), bad=float(rng.choice([0, 0, 0.1])))
+    a.call()
+    a.call()                                           # (the workspace is as good as new)
+    a.check(pairs={(int(b), int(rng.integers(kv))) for b in [*rng.integers(0, rows, 6), 0, rows - 1, int(np.argmax(lens))]})
 
 
 def test_attention_of_the_largest_batch(kq):
