@@ -432,7 +432,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
     }
     __syncthreads();
     // Ranks `count` candidates, one per thread at most, and calls put(rank, candidate) in one lane for each of the n best: those
-    // that reach the bound are listed, then a warp per candidate counts the better ones.  (The order in which they lie does not matter.)
+    // that reach the bound are listed, then the better ones of each are counted.  (The order in which they lie does not matter.)
     auto rank_all = [&](const BeamPick* list, int count, auto put) {
         const bool few = count <= 96;                  // (looking for the bound takes as long as ranking so many)
         int listed = count;
@@ -450,13 +450,15 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
             __syncthreads();
             listed = s_listed;
         }
-        for (int i = warp; i < listed; i += kBeamWarps) {
-            const BeamPick p = list[few ? i : s_list[i]];
-            if (p.score == 0) continue;
+        for (int i0 = 0; i0 < listed; i0 += kBeamThreads / 8) {            // eight threads per candidate
+            const int i = i0 + (tid >> 3);
+            const BeamPick p = i < listed ? list[few ? i : s_list[i]] : no_pick();
             int better = 0;
-            for (int o = lane; o < listed; o += 32) better += list[few ? o : s_list[o]].before(p);
-            better = __reduce_add_sync(0xffffffffu, better);
-            if (better < n && lane == 0) put(better, p);
+#pragma unroll 4
+            for (int o = tid & 7; o < listed; o += 8) better += list[few ? o : s_list[o]].before(p);
+#pragma unroll
+            for (int d = 1; d < 8; d <<= 1) better += __shfl_xor_sync(0xffffffffu, better, d);
+            if (p.score != 0 && better < n && (tid & 7) == 0) put(better, p);
         }
     };
     static_assert(kBeamWarps * kMaxBeams <= kBeamThreads && kBeamMaxCluster * kMaxBeams <= kBeamThreads, "a thread per candidate");
