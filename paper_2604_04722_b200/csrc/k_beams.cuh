@@ -121,19 +121,16 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
     return r;
 }
 
-// Eight (16-bit) or four (fp32) neighbouring entries of a row as they lie in memory, `off` bytes (the same for a whole row)
-// behind a 16-byte border: two aligned loads and a shift where the row is not aligned.
-__device__ __forceinline__ uint4 load_shifted(const uint4* p, uint32_t off) {
-    const uint4 u = __ldg(p);
-    if (off == 0) return u;
-    const uint4 w = __ldg(p + 1);
+// The 16 bytes that begin `off` bytes (the same for all lanes) into u, which w follows in memory.
+__device__ __forceinline__ uint4 shifted(const uint4& u, const uint4& w, uint32_t off) {
     uint32_t x0 = u.x, x1 = u.y, x2 = u.z, x3 = u.w, x4 = w.x, x5 = w.y, x6 = w.z;
     if (off & 8u) x0 = x2, x1 = x3, x2 = x4, x3 = x5, x4 = x6, x5 = w.w;
     if (off & 4u) x0 = x1, x1 = x2, x2 = x3, x3 = x4, x4 = x5;
     const uint32_t bits = (off & 3u) * 8u;
     return make_uint4(__funnelshift_r(x0, x1, bits), __funnelshift_r(x1, x2, bits), __funnelshift_r(x2, x3, bits), __funnelshift_r(x3, x4, bits));
 }
-// The same one by one, for the ends of the tensor: `n` entries, the rest is zero.
+// Eight (16-bit) or four (fp32) neighbouring entries of a row as they lie in memory, one by one, for the ends of the tensor: `n` of
+// them, the rest is zero.
 template <class T>
 __device__ __noinline__ uint4 load_few(const T* src, int n) {
     constexpr int kN = 16 / sizeof(T);
@@ -165,8 +162,8 @@ __device__ __forceinline__ void widen(const uint4& v, float* x) {
     }
 }
 
-// grid = batch clusters, block = kBeamThreads.
-template <class T>
+// grid = batch clusters, block = kBeamThreads.  ALIGNED: every row starts on a 16-byte border.
+template <class T, bool ALIGNED>
 __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParams P) {
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
@@ -209,13 +206,23 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
         s_over[tid] = P.finished && P.finished[r] != 0;
     }
 
-    // a warp's view of a slice: whole vectors, if they lie within the tensor
+    // a warp's view of a slice
     struct Slice {
         int lo, hi;
         const T* z;
-        const uint4* vecs;
+        const uint4* vecs;                             // the row from the 16-byte border before its start
         uint32_t off;
-        bool inside;
+        bool inside;                                   // whole vectors lie within the tensor
+    };
+    // A chunk on its way.  Where rows are not aligned an entry lies in a lane's vector or in the one after it; both are loaded and
+    // shifted when they are used (for fp32, which would take twice the registers, at once).
+    constexpr bool kPairs = !ALIGNED && sizeof(T) == 2;
+    struct Raw {
+        uint4 v[kLoads][kPairs ? 2 : 1];
+    };
+    auto ends_inside = [&](const uint4* vecs, uint32_t off, int from, int to) {
+        return reinterpret_cast<uintptr_t>(vecs + from / kVec) >= reinterpret_cast<uintptr_t>(P.logits) &&
+               reinterpret_cast<uintptr_t>(vecs + (to + kVec - 1) / kVec + (off ? 1 : 0)) <= reinterpret_cast<uintptr_t>(P.logits_end);
     };
     auto slice_of = [&](int task) {
         Slice v;
@@ -224,22 +231,41 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
         v.hi = (int)min((long long)v.lo + P.slice_len, (long long)P.vocab);
         v.z = static_cast<const T*>(P.logits) + ((size_t)b * P.beams + row) * (size_t)P.vocab;
         const uintptr_t at = reinterpret_cast<uintptr_t>(v.z);
-        v.off = (uint32_t)(at & 15u);
+        v.off = ALIGNED ? 0u : (uint32_t)(at & 15u);
         v.vecs = reinterpret_cast<const uint4*>(at - v.off);
-        v.inside = reinterpret_cast<uintptr_t>(v.vecs + v.lo / kVec) >= reinterpret_cast<uintptr_t>(P.logits) &&
-                   reinterpret_cast<uintptr_t>(v.vecs + (v.hi + kVec - 1) / kVec + (v.off ? 1 : 0)) <= reinterpret_cast<uintptr_t>(P.logits_end);
+        v.inside = ends_inside(v.vecs, v.off, v.lo, v.hi);
         return v;
     };
-    auto load = [&](const Slice& v, int c0, uint4 (&raw)[kLoads]) {
+    auto load = [&](const Slice& v, int c0, Raw& raw) {
+        const bool inside = v.inside || ends_inside(v.vecs, v.off, c0, min(v.hi, c0 + kBeamChunk));    // (only the tensor's first and last chunk are not)
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
             const int t = c0 + (k * 32 + lane) * kVec;
-            if (t < v.hi) raw[k] = v.inside ? load_shifted(v.vecs + t / kVec, v.off) : load_few<T>(v.z + t, P.vocab - t);
+            if (t >= v.hi) continue;
+            if (!inside) {
+                const uint4 few = load_few<T>(v.z + t, P.vocab - t);
+                raw.v[k][0] = few;
+                if constexpr (kPairs) {                // as if it had been read behind the border
+                    raw.v[k][0] = shifted(make_uint4(0, 0, 0, 0), few, 16u - v.off);
+                    if (v.off == 0) raw.v[k][0] = few;
+                    raw.v[k][1] = shifted(few, make_uint4(0, 0, 0, 0), 16u - v.off);
+                }
+            } else if constexpr (kPairs) {
+                raw.v[k][0] = __ldg(v.vecs + t / kVec);
+                if (v.off) raw.v[k][1] = __ldg(v.vecs + t / kVec + 1);
+            } else {
+                const uint4 u = __ldg(v.vecs + t / kVec);
+                raw.v[k][0] = u;
+                if (!ALIGNED && v.off) raw.v[k][0] = shifted(u, __ldg(v.vecs + t / kVec + 1), v.off);
+            }
         }
     };
-    auto values = [&](const Slice& v, int c0, const uint4 (&raw)[kLoads], float (&x)[16]) {
+    auto values = [&](const Slice& v, int c0, const Raw& raw, float (&x)[16]) {
 #pragma unroll
-        for (int k = 0; k < kLoads; ++k) widen<T>(raw[k], x + k * kVec);
+        for (int k = 0; k < kLoads; ++k) {
+            if constexpr (kPairs) widen<T>(v.off ? shifted(raw.v[k][0], raw.v[k][1], v.off) : raw.v[k][0], x + k * kVec);
+            else widen<T>(raw.v[k][0], x + k * kVec);
+        }
         if (c0 + kBeamChunk > v.hi) {
 #pragma unroll
             for (int k = 0; k < 16; ++k)
@@ -255,7 +281,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
             const size_t r = (size_t)b * P.beams + row;
             float* tops = s_group_top + (warp * rounds + j) * per_slice;
             const Slice v = slice_of(task);
-            uint4 raw[kLoads];
+            Raw raw;
             load(v, v.lo, raw);                        // (of rows that are out no more than this is read)
             const bool over = P.finished && P.finished[r] != 0, alive = isfinite(P.scores[r]);
             if (over) {                                // one candidate: the end token at the score as it is
@@ -392,7 +418,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
                 const int begin = v.lo + g * group_len;
 #pragma unroll 1
                 for (int c0 = begin; c0 < min(v.hi, begin + group_len); c0 += kBeamChunk) {
-                    uint4 raw[kLoads];
+                    Raw raw;
                     float x[16];
                     load(v, c0, raw);
                     values(v, c0, raw, x);

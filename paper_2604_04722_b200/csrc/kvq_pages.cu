@@ -64,6 +64,14 @@ cudaError_t ask_clusters(Kernel kernel, int threads, size_t smem, int (&clusters
     return e;
 }
 
+// (All of them have the same threads, registers and shared memory.)
+template <class T>
+cudaError_t set_up_beams(int (&clusters)[5]) {
+    cudaError_t e = allow_smem(k_beam_select<T, true>, true);
+    if (e == cudaSuccess) e = allow_smem(k_beam_select<T, false>, true);
+    return e == cudaSuccess ? ask_clusters(k_beam_select<T, false>, kBeamThreads, beam_smem(kMaxBeams), clusters) : e;
+}
+
 // Both types of a shape are the same to the device; the batch's share of the shared memory is small.
 template <int D, int NT, int W>
 cudaError_t set_up_attn(int (&clusters)[5]) {
@@ -79,10 +87,9 @@ const PagesDevice* device_of_call() {
     const cudaError_t e = g_device.make(device, [&](PagesDevice& d) {
         cudaError_t err = cudaDeviceGetAttribute(&d.sm_count, cudaDevAttrMultiProcessorCount, device);
         if (err == cudaSuccess) err = allow_smem(k_page_step, false);
-        if (err == cudaSuccess) err = allow_smem(k_beam_select<__half>, true);
-        if (err == cudaSuccess) err = allow_smem(k_beam_select<__nv_bfloat16>, true);
-        if (err == cudaSuccess) err = allow_smem(k_beam_select<float>, true);
-        if (err == cudaSuccess) err = ask_clusters(k_beam_select<float>, kBeamThreads, beam_smem(kMaxBeams), d.beam_clusters);
+        if (err == cudaSuccess) err = set_up_beams<__half>(d.beam_clusters);
+        if (err == cudaSuccess) err = set_up_beams<__nv_bfloat16>(d.beam_clusters);
+        if (err == cudaSuccess) err = set_up_beams<float>(d.beam_clusters);
         if (err == cudaSuccess) err = set_up_attn<64, 1, 8>(d.attn_clusters[0]);
         if (err == cudaSuccess) err = set_up_attn<64, 2, 8>(d.attn_clusters[1]);
         if (err == cudaSuccess) err = set_up_attn<64, 1, 16>(d.attn_clusters[2]);
@@ -155,6 +162,13 @@ int launch_attn(const PageAttnParams& p, int nt, uint64_t ctas, void* stream) {
     const int threads = AttnGeom<D, W>::kThreads, cluster = p.cluster > 1 ? p.cluster : 0;
     return nt == 1 ? launch(k_page_attn<BF, D, 1, W>, ctas, threads, smem, cluster, p, stream)
                    : launch(k_page_attn<BF, D, 2, W>, ctas, threads, smem, cluster, p, stream);
+}
+
+template <class T>
+int launch_beams(const BeamParams& p, bool rows_aligned, int ctas, void* stream) {
+    const uint64_t grid = (uint64_t)p.batch * ctas;
+    return rows_aligned ? launch(k_beam_select<T, true>, grid, kBeamThreads, beam_smem(p.n_out), ctas, p, stream)
+                        : launch(k_beam_select<T, false>, grid, kBeamThreads, beam_smem(p.n_out), ctas, p, stream);
 }
 
 }  // namespace
@@ -338,11 +352,9 @@ int kvq_beam_select(const void* logits, int dtype, const float* scores, const ui
     // slices of at least a chunk, at most as many as there are warps (a row each where there are more rows)
     p.slices = std::max(1, std::min(ctas * kBeamWarps / beams, (vocab + kBeamChunk - 1) / kBeamChunk));
     p.slice_len = (int)((((int64_t)vocab + p.slices - 1) / p.slices + 255) / 256 * 256);
-    const uint64_t grid = (uint64_t)batch * ctas;
-    const size_t smem = beam_smem(n_out);
-    if (dtype == KVQ_FP32) return launch(k_beam_select<float>, grid, kBeamThreads, smem, ctas, p, stream);
-    if (dtype == KVQ_BF16) return launch(k_beam_select<__nv_bfloat16>, grid, kBeamThreads, smem, ctas, p, stream);
-    return launch(k_beam_select<__half>, grid, kBeamThreads, smem, ctas, p, stream);
+    const bool rows_aligned = aligned(logits, 16) && (size_t)vocab * size % 16 == 0;
+    if (dtype == KVQ_FP32) return launch_beams<float>(p, rows_aligned, ctas, stream);
+    return dtype == KVQ_BF16 ? launch_beams<__nv_bfloat16>(p, rows_aligned, ctas, stream) : launch_beams<__half>(p, rows_aligned, ctas, stream);
 }
 
 }  // extern "C"
