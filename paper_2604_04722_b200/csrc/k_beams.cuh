@@ -12,9 +12,9 @@
 // CTA (a second barrier), and that ranks them.  Scores are compared in fp64.
 //
 // Bound: of many requests the loop over the logits: an exponential each, and the instructions around it (64 requests of 16 beams over
-// 32000 bf16 logits: 29.5 us, the bytes alone 10; over 32003, where rows are not aligned and every load becomes two and a shift, 42).
-// Of few requests the chain of the rows' loads, two cluster barriers, the bound, a second read and two rankings: 10.5 us for one
-// request of 4 beams over 49152 logits.  Keeping the slices' best entries in the first pass took 94 us where this takes 42.
+// 32000 bf16 logits: 28 us, the bytes alone 10; without the exponentials 21; over 32003, where rows are not aligned and every load becomes
+// two, 33).  Of few requests the chain of the rows' loads, two cluster barriers, the bound, a second read and two rankings: 9.8 us for
+// one request of 4 beams over 49152 logits.  Keeping the slices' best entries in the first pass took 94 us where this takes 33.
 #pragma once
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
@@ -162,6 +162,19 @@ __device__ __forceinline__ void widen(const uint4& v, float* x) {
     }
 }
 
+// The eight 16-bit entries that begin OFF bytes into two neighbouring vectors, from where they lie.
+template <class T, int OFF>
+__device__ __forceinline__ void widen_at(const uint4& u, const uint4& v, float* x) {
+    const uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int at = OFF + 2 * i;
+        const uint32_t word = w[at / 4];
+        if constexpr (std::is_same<T, __nv_bfloat16>::value) x[i] = __uint_as_float(at % 4 ? word & 0xffff0000u : word << 16);
+        else x[i] = __half2float(__ushort_as_half((unsigned short)(at % 4 ? word >> 16 : word & 0xffffu)));
+    }
+}
+
 // grid = batch clusters, block = kBeamThreads.  ALIGNED: every row starts on a 16-byte border.
 template <class T, bool ALIGNED>
 __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParams P) {
@@ -214,8 +227,8 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
         uint32_t off;
         bool inside;                                   // whole vectors lie within the tensor
     };
-    // A chunk on its way.  Where rows are not aligned an entry lies in a lane's vector or in the one after it; both are loaded and
-    // shifted when they are used (for fp32, which would take twice the registers, at once).
+    // A chunk on its way.  Where rows are not aligned an entry lies in a lane's vector or in the one after it; both are loaded, and
+    // entries taken from where they lie when they are used (for fp32, which would take twice the registers, shifted at once).
     constexpr bool kPairs = !ALIGNED && sizeof(T) == 2;
     struct Raw {
         uint4 v[kLoads][kPairs ? 2 : 1];
@@ -261,10 +274,24 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
         }
     };
     auto values = [&](const Slice& v, int c0, const Raw& raw, float (&x)[16]) {
+        if constexpr (kPairs) {
+            auto at = [&](auto off) {
 #pragma unroll
-        for (int k = 0; k < kLoads; ++k) {
-            if constexpr (kPairs) widen<T>(v.off ? shifted(raw.v[k][0], raw.v[k][1], v.off) : raw.v[k][0], x + k * kVec);
-            else widen<T>(raw.v[k][0], x + k * kVec);
+                for (int k = 0; k < kLoads; ++k) widen_at<T, decltype(off)::value>(raw.v[k][0], raw.v[k][1], x + k * kVec);
+            };
+            switch (v.off) {
+            case 0: at(std::integral_constant<int, 0>()); break;
+            case 2: at(std::integral_constant<int, 2>()); break;
+            case 4: at(std::integral_constant<int, 4>()); break;
+            case 6: at(std::integral_constant<int, 6>()); break;
+            case 8: at(std::integral_constant<int, 8>()); break;
+            case 10: at(std::integral_constant<int, 10>()); break;
+            case 12: at(std::integral_constant<int, 12>()); break;
+            default: at(std::integral_constant<int, 14>()); break;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kLoads; ++k) widen<T>(raw.v[k][0], x + k * kVec);
         }
         if (c0 + kBeamChunk > v.hi) {
 #pragma unroll

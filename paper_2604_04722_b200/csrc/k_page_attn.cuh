@@ -233,16 +233,24 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
     auto share = [&](int c) -> int64_t { return share_size * c + min((int64_t)c, share_more); };
     auto border = [&](int c) -> int64_t {
         if (c == stretches) return total;
-        if (unit_each) {
-            const int b = c / units_per_row;
-            return tiles_before(b) * units_per_row + (int64_t)(c - b * units_per_row) * tiles_of(b);
-        }
         const int64_t at = share(c);
         const AttnCursor x = locate(at);
         const int back = x.t, ahead = x.tiles - x.t;
         return min(back, ahead) > snap ? at : back <= ahead ? at - back : at + ahead;
     };
-    const int64_t lo = border(group), hi = border(group + 1);
+    int64_t lo, hi;
+    AttnCursor first = {};                             // the unit, where there is one
+    if (unit_each) {
+        first.b = group / units_per_row;
+        first.u = group - first.b * units_per_row;
+        first.tiles = tiles_of(first.b);
+        first.len = len_of(first.b);
+        lo = tiles_before(first.b) * units_per_row + (int64_t)first.u * first.tiles;
+        hi = lo + first.tiles;
+    } else {
+        lo = border(group);
+        hi = border(group + 1);
+    }
     if (lo == hi) return;                              // (the same for the whole cluster)
     auto warp_border = [&](int w) -> int64_t { return lo + (((hi - lo) * w) >> warps_log2); };     // of the cluster's warps
     auto cta_border = [&](int r) { return warp_border(r * team); };
@@ -271,7 +279,9 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
     const int count = (int)(whi - wlo);
     if (count > 0) {
         // ---- copies: `ahead` is the tile whose page numbers are being looked up
-        AttnCursor ahead = locate(wlo);
+        AttnCursor ahead = first;
+        if (unit_each) ahead.t = (int)(wlo - lo);
+        else ahead = locate(wlo);
         int looked = 0;                                // tiles looked up so far
         int page = -1, slot = 0, head = 0;
         auto look_up = [&]() {
