@@ -86,24 +86,27 @@ __device__ __noinline__ void warp_best(BeamPick* buffer, int count, int n) {
     __syncwarp();
 }
 
-// A score that n of a warp's candidates (0: none, K per lane) reach, and not many more: the n-th best of the lanes' best ones, rounded down to
-// fp32; 0 if fewer than n lanes have one.  (256 candidates, n = 4 / 16 / 32: about 4 / 21 / 90 reach it if they lie as they please; an
-// exact bound took 1.8 us, this one 0.4.)
-template <int K>
-__device__ __forceinline__ uint64_t warp_bound(const uint64_t (&mine)[K], int n) {
+// The n-th largest of the lanes' numbers: a bitonic sort, descending.
+__device__ __forceinline__ float warp_nth(float v, int n) {
     const int lane = threadIdx.x & 31;
-    uint64_t top = mine[0];
 #pragma unroll
-    for (int k = 1; k < K; ++k) top = mine[k] > top ? mine[k] : top;
-    float v = top ? __double2float_rd(key_score(top)) : -INFINITY;
-#pragma unroll
-    for (int size = 2; size <= 32; size <<= 1)         // a bitonic sort, descending
+    for (int size = 2; size <= 32; size <<= 1)
 #pragma unroll
         for (int d = size >> 1; d > 0; d >>= 1) {
             const float o = __shfl_xor_sync(0xffffffffu, v, d);
             v = ((lane & d) == 0) == ((lane & size) == 0) ? fmaxf(v, o) : fminf(v, o);
         }
-    v = __shfl_sync(0xffffffffu, v, n - 1);
+    return __shfl_sync(0xffffffffu, v, n - 1);
+}
+// A score that n of a warp's candidates (0: none, K per lane) reach, and not many more: the n-th best of the lanes' best ones, rounded down to
+// fp32; 0 if fewer than n lanes have one.  (256 candidates, n = 4 / 16 / 32: about 4 / 21 / 90 reach it if they lie as they please; an
+// exact bound took 1.8 us, this one 0.4.)
+template <int K>
+__device__ __forceinline__ uint64_t warp_bound(const uint64_t (&mine)[K], int n) {
+    uint64_t top = mine[0];
+#pragma unroll
+    for (int k = 1; k < K; ++k) top = mine[k] > top ? mine[k] : top;
+    const float v = warp_nth(top ? __double2float_rd(key_score(top)) : -INFINITY, n);
     return v > -INFINITY ? score_key((double)v) : 0ull;
 }
 
@@ -410,6 +413,8 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
     {
         BeamPick* buffer = s_buffers + warp * kBeamBuffer;
         BeamPick worst = no_pick();                    // once the buffer was full: what has to be beaten
+        uint64_t reach = bound;                        // what has to be reached
+        float lane_top = -INFINITY;                    // score of the best entry that this lane has seen
         int count = 0;
         {
             const int listed = s_listed;
@@ -437,10 +442,12 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
                     keep(lane == 0, BeamPick{score_of(0.f), (uint32_t)row, (uint32_t)P.end_token});
                     continue;
                 }
-                // logits below this do not reach the bound (or what has to be beaten; exactly: below)
-                const uint64_t at_least = worst.score > bound ? worst.score : bound;
-                float least = -FLT_MAX;
-                if (at_least != 0) least = fmaxf(least, nextafterf(__double2float_rd((key_score(at_least) - off) + (double)row_top), -INFINITY));
+                // logits below this do not reach it (or what has to be beaten; exactly: below)
+                auto least_logit = [&]() {
+                    const uint64_t score = worst.score > reach ? worst.score : reach;
+                    return score == 0 ? -FLT_MAX : fmaxf(-FLT_MAX, nextafterf(__double2float_rd((key_score(score) - off) + (double)row_top), -INFINITY));
+                };
+                float least = least_logit();
                 const Slice v = slice_of(task);
                 const int begin = v.lo + g * group_len;
 #pragma unroll 1
@@ -449,10 +456,28 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
                     float x[16];
                     load(v, c0, raw);
                     values(v, c0, raw, x);
-                    uint32_t hits = 0;                 // entries of this lane that may count
+                    auto hits_of = [&]() {             // entries of this lane that may count
+                        uint32_t hits = 0;
 #pragma unroll
-                    for (int k = 0; k < 16; ++k)
-                        if (x[k] >= least) hits |= 1u << k;
+                        for (int k = 0; k < 16; ++k)
+                            if (x[k] >= least) hits |= 1u << k;
+                        return hits;
+                    };
+                    uint32_t hits = hits_of();
+                    // Where the bound is weak (one beam is far ahead, or has all the candidates) many reach it.  The n-th best of the lanes'
+                    // best entries so far is one that n of this warp's reach.
+                    float most = x[0];
+#pragma unroll
+                    for (int k = 1; k < 16; ++k) most = fmaxf(most, x[k]);
+                    if (most > -INFINITY) lane_top = fmaxf(lane_top, __double2float_rd(off + ((double)most - (double)row_top)));
+                    if (__reduce_add_sync(0xffffffffu, __popc(hits)) > 2 * n) {
+                        const float nth = warp_nth(lane_top, n);
+                        if (nth > -INFINITY && score_key((double)nth) > reach) {
+                            reach = score_key((double)nth);
+                            least = least_logit();
+                            hits = hits_of();
+                        }
+                    }
                     while (__any_sync(0xffffffffu, hits != 0)) {           // one of every lane at a time
                         const int k = __ffs((int)hits) - 1;
                         float z = x[0];
@@ -462,7 +487,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
                         p.score = score_of(z);
                         p.row = (uint32_t)row;
                         p.token = (uint32_t)(c0 + (k / kVec * 32 + lane) * kVec + k % kVec);
-                        keep(k >= 0 && p.score >= bound && (worst.score == 0 || p.before(worst)), p);
+                        keep(k >= 0 && p.score >= reach && (worst.score == 0 || p.before(worst)), p);
                         hits &= hits - 1;
                     }
                 }
