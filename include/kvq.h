@@ -402,8 +402,8 @@ int kvq_page_append(const kvq_page_cache* cache, const void* K, const void* V, c
 
 /*
  * Attention of one new token per request over its pages: O = Softmax(scale * q K^T) V over the first lens[b] tokens, query head h
- * reading KV head h / (q_heads / kv_heads).  Q, O: dev [batch][q_heads][head_dim] of the cache's type, 16-byte aligned; lse_opt
- * dev fp32 [batch][q_heads] or NULL: the logarithm of the sum of exponentials.  A row of length 0 (or less) gets zeros and
+ * reading KV head h / (q_heads / kv_heads).  Q, O: dev [batch][q_heads][head_dim] of the cache's type, 16-byte aligned
+ * (O may be Q); lse_opt dev fp32 [batch][q_heads] or NULL: the logarithm of the sum of exponentials.  A row of length 0 (or less) gets zeros and
  * -inf; lengths beyond the table count as its width.  Slots behind a row's length may hold anything, and tokens on pages outside
  * the cache (such as -1) do not take part.  A value that is not finite makes NaN of its channel, and a key that is not of the
  * whole row, in the heads that read it.  Sums are fp32; equal calls give equal bits (the cut of the work does not depend on the
@@ -423,11 +423,12 @@ int kvq_page_attn(const kvq_page_cache* cache, const void* Q, void* O, float* ls
  *   logits        dev [batch][beams][vocab] of dtype KVQ_FP16, KVQ_BF16 or KVQ_FP32
  *   scores        dev fp32 [batch][beams]: sums of log-probabilities so far
  *   finished_opt  dev uint8 [batch][beams] or NULL: a beam that has ended (not zero) has one candidate, end_token at its score as it is;
- *                 its logits are not read
+ *                 its logits do not matter
  *   end_token     0 <= end_token < vocab, or -1 (none; finished_opt is then NULL)
  *   parents, tokens, scores_out  dev int32, int32, fp32 [batch][n_out], best first: the row b * beams + w (kvq_page_step's parents where
  *                 n_out == beams), the token and the score; -1, -1 and -inf where candidates run out
  *   finished_out_opt  dev uint8 [batch][n_out] or NULL: 1 for a beam that had ended, takes end_token or is missing
+ * Where n_out == beams, scores_out may be scores and finished_out_opt finished_opt; otherwise no output overlaps an input.
  * Candidates whose score is not finite do not count (masked tokens, beams of score -inf; a row with a NaN or +inf has
  * none).  1 <= beams, n_out <= KVQ_MAX_BEAMS; 1 <= vocab <= 2^30.  batch == 0 is a no-op.  One launch.
  */

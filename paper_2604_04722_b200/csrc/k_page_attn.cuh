@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
     int64_t* s_place = reinterpret_cast<int64_t*>(s_ring_all + (size_t)kAttnWarps * G::kRingBytes);
     auto tiles_before = [&](int b) -> int64_t { return s_place[b] >> 4; };
     auto tiles_of = [&](int b) -> int { return (int)(tiles_before(b + 1) - tiles_before(b)); };
-    auto len_of = [&](int b) -> int { return tiles_of(b) * kAttnTile - (int)(s_place[b] & 15); };
+    auto len_of = [&](int b) -> int { return (tiles_of(b) - 1) * kAttnTile + (kAttnTile - (int)(s_place[b] & 15)); };
     __shared__ int64_t s_scan[kAttnWarps];
     __shared__ int s_longest[kAttnWarps];
     __shared__ uint32_t s_there[kAttnWarps][kStages];  // tokens of a stage that exist

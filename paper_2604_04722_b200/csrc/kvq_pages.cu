@@ -18,14 +18,14 @@ static_assert(KVQ_MAX_PAGE_ROWS == kMaxPageRows && KVQ_MAX_PAGES == kMaxPages &&
 static_assert(KVQ_PAGE_FULL == kPageFull && KVQ_PAGE_LONG == kPageLong && KVQ_PAGE_SLOTS == kPageSlots && KVQ_PAGE_BAD == kPageBad, "status bits");
 
 bool aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
-bool overlap(const void* a, const void* b, size_t bytes) {
+bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x < y + bytes && y < x + bytes;
+    return x < y + b_bytes && y < x + a_bytes;
 }
 
 // What a device allows, asked for once; the kernels' shared-memory limits and cluster sizes are set on the way.
 struct PagesDevice {
-    int sm_count = 0;
+    int sm_count = 0, sm_smem = 0;                     // shared memory of an SM, bytes
     int beam_clusters[5] = {};                         // resident clusters of 2^i CTAs of the selection ...
     int attn_clusters[6][5] = {};                      // ... and of the attention: see attn_variant
 };
@@ -86,6 +86,7 @@ const PagesDevice* device_of_call() {
     if (const PagesDevice* d = g_device.of(device)) return d;
     const cudaError_t e = g_device.make(device, [&](PagesDevice& d) {
         cudaError_t err = cudaDeviceGetAttribute(&d.sm_count, cudaDevAttrMultiProcessorCount, device);
+        if (err == cudaSuccess) err = cudaDeviceGetAttribute(&d.sm_smem, cudaDevAttrMaxSharedMemoryPerMultiprocessor, device);
         if (err == cudaSuccess) err = allow_smem(k_page_step, false);
         if (err == cudaSuccess) err = set_up_beams<__half>(d.beam_clusters);
         if (err == cudaSuccess) err = set_up_beams<__nv_bfloat16>(d.beam_clusters);
@@ -188,8 +189,9 @@ int kvq_page_step(const int32_t* tables_in, int32_t* tables_out, int table_width
         if (!aligned(p, 4)) return KVQ_ERR_ARG;
     if (!aligned(slots, 8)) return KVQ_ERR_ARG;
     const size_t bytes = (size_t)batch * table_width * sizeof(int32_t);
-    if (batch > 0 && overlap(tables_in, tables_out, bytes) && (parents_opt || tables_in != tables_out)) return KVQ_ERR_ARG;
-    if (batch > 0 && overlap(lens_in, lens_out, batch * sizeof(int32_t)) && lens_in != lens_out) return KVQ_ERR_ARG;
+    if (batch > 0 && overlap(tables_in, bytes, tables_out, bytes) && (parents_opt || tables_in != tables_out)) return KVQ_ERR_ARG;
+    const size_t len_bytes = batch * sizeof(int32_t);
+    if (batch > 0 && overlap(lens_in, len_bytes, lens_out, len_bytes) && lens_in != lens_out) return KVQ_ERR_ARG;
     if (!device_of_call()) return KVQ_ERR_CUDA;
     PageStepParams p{};
     p.tables_in = tables_in;
@@ -304,6 +306,9 @@ int kvq_page_attn(const kvq_page_cache* cache, const void* Q, void* O, float* ls
     int warps = 8;
     p.cluster = widest(warps);
     if (D == 64 && p.cluster == kAttnMaxCluster && longest > 8.0 * warps * p.cluster) p.cluster = widest(warps = 16);
+    // Of very many rows the table of their places leaves no room for two CTAs of 8 warps (2 KB for what else a CTA has): one of 16 then
+    // (4096 rows of 122 tokens of 8 heads, 1.05 GB: 179 us, with 8 warps 214).
+    if (D == 64 && 2 * (attn_smem<64, 8>(batch) + 2048) > (size_t)d->sm_smem) warps = 16;
     // Where CTAs take equal shares of many units, two heads side by side in memory are read at the same time: 128 bytes of a row here and
     // there cost DRAM more than 256 (16 x 8192 tokens of 32 heads, slot by slot: 173 us, with one at a time 199, four 174, sixteen 179).
     p.abreast = p.cluster == 1 && p.slot_stride > p.head_stride && D == 64 && p.kv_heads * p.head_blocks % 2 == 0 ? kAttnAbreast : 1;
@@ -330,6 +335,12 @@ int kvq_beam_select(const void* logits, int dtype, const float* scores, const ui
     const size_t size = dtype == KVQ_FP32 ? 4 : 2;
     if (!logits || !scores || !parents || !tokens || !scores_out || (finished_opt && end_token < 0)) return KVQ_ERR_ARG;
     if (!aligned(logits, size) || !aligned(scores, 4) || !aligned(parents, 4) || !aligned(tokens, 4) || !aligned(scores_out, 4)) return KVQ_ERR_ARG;
+    // a request's scores and ends are read before its results are written, but other requests' may not be read yet
+    const size_t in = (size_t)batch * beams, out = (size_t)batch * n_out;
+    auto clash = [&](const void* from, void* to, size_t each) {
+        return from && to && !(from == to && n_out == beams) && overlap(from, in * each, to, out * each);
+    };
+    if (clash(scores, scores_out, sizeof(float)) || clash(finished_opt, finished_out_opt, 1)) return KVQ_ERR_ARG;
     const PagesDevice* d = device_of_call();
     if (!d) return KVQ_ERR_CUDA;
     // a cluster per request, as wide as leaves all of them resident together

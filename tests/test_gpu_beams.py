@@ -135,6 +135,20 @@ def test_masks_dead_beams_and_rows_without_a_distribution(kq):
             _check(kq, z, s, None, n, 2)
 
 
+@pytest.mark.parametrize("B,W,V", [(1, 4, 4099), (70, 5, 700), (400, 16, 90)])
+def test_selection_in_place(kq, B, W, V):
+    """Scores and ends over those of the step before; another request's inputs may not be read yet."""
+    import torch
+    z, s = _logits(B, B, W, V, torch.bfloat16), _scores(B, B, W)
+    f = (np.random.default_rng(B).random((B, W)) < 0.3).astype(np.uint8)
+    want = _check(kq, z, s, f, W, V // 2)
+    S, F = torch.from_numpy(s).cuda(), torch.from_numpy(f).cuda()
+    p, t = (torch.empty((B, W), dtype=torch.int32, device="cuda") for _ in range(2))
+    kq.kvq_beam_select(z, kq.KVQ_BF16, S, F, B, W, V, W, V // 2, p, t, S, F)
+    for got, w in zip((p, t, S, F), want):
+        assert np.array_equal(got.cpu().numpy(), w)
+
+
 def test_ties_go_to_the_lowest_beam_and_token(kq):
     import torch
     for dtype in _dtypes():

@@ -371,6 +371,25 @@ def test_attention_of_any_shape(kq, seed):
     a.check(pairs={(int(b), int(rng.integers(kv))) for b in [*rng.integers(0, rows, 6), 0, rows - 1, int(np.argmax(lens))]})
 
 
+@pytest.mark.parametrize("lens,q_heads,kv_heads", [([700], 9, 3), ([30000], 9, 3), ([900, 0, 77, 4000] * 6, 32, 8)])
+def test_attention_writes_over_its_queries(kq, lens, q_heads, kv_heads):
+    a = Attn(kq, lens, q_heads, kv_heads, 64, 16)
+    a.call()
+    want, a.O = a.O.clone(), a.Q
+    a.call()
+    assert want.equal(a.O)
+
+
+@pytest.mark.parametrize("rows,q_heads,kv_heads", [(4096, 4, 2), (2200, 3, 3), (2047, 12, 1)])
+def test_attention_of_very_many_rows(kq, rows, q_heads, kv_heads):
+    rng = np.random.default_rng(rows)
+    lens = rng.integers(0, 60, rows)
+    lens[[0, 7, rows // 2, rows - 1]] = 9000, 3, 17000, 1
+    a = Attn(kq, lens, q_heads, kv_heads, 64, 32)
+    a.call()
+    a.check()
+
+
 def test_attention_of_the_largest_batch(kq):
     rng = np.random.default_rng(5)
     a = Attn(kq, rng.integers(0, 40, 4096), 2, 2, 128, 8, "bf16")

@@ -97,6 +97,14 @@ def test_selection_refusals(kq, change):
     assert kq.lib().kvq_beam_select(*dict(SELECT, batch=0, logits=None).values(), None) == 0
 
 
+@pytest.mark.parametrize("change", [
+    dict(n_out=3), dict(n_out=5), dict(scores_out=A + 4), dict(scores=A + 28), dict(scores_out=A + 4096, finished=A, finished_out=A + 7, end=0),
+    dict(scores_out=A + 4096, finished=A, finished_out=A, end=0, n_out=1)])
+def test_selection_refuses_results_over_its_inputs(kq, change):
+    """In place is fine where every request has as many beams as before (on the GPU: test_selection_in_place)."""
+    assert kq.lib().kvq_beam_select(*dict(SELECT, **change).values(), None) == ARG
+
+
 def test_limits_of_the_header_and_of_the_binding_agree(kq):
     import os
     import re
