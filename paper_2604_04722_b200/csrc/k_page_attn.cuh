@@ -55,10 +55,16 @@ struct AttnGeom {
 template <int D, int NT>
 __host__ __device__ constexpr int attn_record_floats() { return 8 * NT * (D + 2); }            // o [D][8 NT], m [8 NT], l [8 NT]
 
-// Shared memory: the rings, and the rows' place on the axis.
-template <int D, int W>
-inline size_t attn_smem(int batch) {
-    return (size_t)W * AttnGeom<D, W>::kRingBytes + sizeof(int64_t) * ((size_t)batch + 1);
+// Shared memory: the rings, the rows' place on the axis and, where there are clusters, what CTAs send one another.
+template <int D, int NT>
+struct AttnSent {
+    float o[D * 8 * NT];                               // [CTA][channels of this CTA][head]
+    float m[kAttnMaxCluster][8 * NT], l[kAttnMaxCluster][8 * NT];
+};
+__host__ __device__ inline size_t attn_place_bytes(int batch) { return (sizeof(int64_t) * ((size_t)batch + 1) + 15) / 16 * 16; }
+template <int D, int NT, int W>
+inline size_t attn_smem(int batch, bool clusters) {
+    return (size_t)W * AttnGeom<D, W>::kRingBytes + attn_place_bytes(batch) + (clusters ? sizeof(AttnSent<D, NT>) : 0);
 }
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
@@ -252,6 +258,7 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
         hi = border(group + 1);
     }
     if (lo == hi) return;                              // (the same for the whole cluster)
+    if (unit_each && C > 1 && hi - lo > 1) cg::this_cluster().barrier_arrive();            // (before they write one another's memory, all have to be there)
     auto warp_border = [&](int w) -> int64_t { return lo + (((hi - lo) * w) >> warps_log2); };     // of the cluster's warps
     auto cta_border = [&](int r) { return warp_border(r * team); };
     const int64_t wlo = warp_border(rank * team + warp % team), whi = warp_border(rank * team + warp % team + 1);
@@ -524,6 +531,80 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
         for (int c = 0; c < 4; ++c)
             if (r + c < at.heads) O[(at.row + r + c) * D + d] = round16<BF>(x[c] * inv[c]);
     };
+    const int quads = min(kR, P.group + 3) / 4;        // of heads: at most what the group needs
+    if (unit_each) {
+        // ---- A unit for the whole cluster: the CTA's part, an equal share of whose channels goes to every CTA of the cluster; then
+        // every CTA adds up its channels.  (One CTA that fetched and added up everything took 4 us longer for 16 CTAs.)
+        if (hi - lo == 1) return;                      // (its warp has written it)
+        const Place at = place_of(group);
+        const uint32_t live = __ballot_sync(0xffffffffu, lane < kAttnWarps && s_piece[2 * (lane % kAttnWarps) + 1].unit >= 0);     // warps with a piece
+        AttnSent<D, NT>* const sent = reinterpret_cast<AttnSent<D, NT>*>(reinterpret_cast<uint8_t*>(s_place) + attn_place_bytes(P.batch));
+        if (C > 1) cg::this_cluster().barrier_wait();
+        if (warp < kR * kAttnWarps / 32) {             // kAttnWarps lanes for every head
+            const int r = tid / kAttnWarps, w = tid % kAttnWarps;
+            const bool in = (live >> w) & 1u;
+            const float* p = last_piece(w) + D * kR + r;
+            const float m = in ? p[0] : kLowest;
+            float top = m;
+#pragma unroll
+            for (int d = 1; d < kAttnWarps; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            const float f = in ? fast_exp2(m - top) : 0.f;
+            float sum = in ? f * p[kR] : 0.f;
+#pragma unroll
+            for (int d = 1; d < kAttnWarps; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            s_f.factor[w][r] = f;
+            if (C > 1) {
+                for (int c = w; c < C; c += kAttnWarps) {
+                    AttnSent<D, NT>* to = cg::this_cluster().map_shared_rank(sent, c);
+                    to->m[rank][r] = top, to->l[rank][r] = sum;
+                }
+            } else if (w == 0) {
+                s_f.l[0][r] = inverse(sum);
+                put_lse(at, r, top, sum);
+            }
+        }
+        __syncthreads();
+        const int channels = D / C;                    // of a CTA
+        for (int e = tid; e < quads * D; e += kAttnThreads) {
+            const int d = e % D, r = 4 * (e / D);
+            float4 so = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kAttnWarps; ++w) {
+                if (!((live >> w) & 1u)) continue;
+                const float4 y = *reinterpret_cast<const float4*>(last_piece(w) + d * kR + r), f = *reinterpret_cast<const float4*>(&s_f.factor[w][r]);
+                so.x += f.x * y.x, so.y += f.y * y.y, so.z += f.z * y.z, so.w += f.w * y.w;
+            }
+            if (C == 1) put(at, r, d, so, &s_f.l[0][r]);
+            else *reinterpret_cast<float4*>(cg::this_cluster().map_shared_rank(sent, d / channels)->o + (rank * channels + d % channels) * kR + r) = so;
+        }
+        if (C == 1) return;
+        cg::this_cluster().sync();                     // (from here on a CTA reads its own memory only)
+        if (warp < kR / 2) {                           // sixteen lanes for every head
+            const int r = tid >> 4, c = lane & 15;
+            const float m = c < C ? sent->m[c][r] : kLowest, l = c < C ? sent->l[c][r] : 0.f;
+            float top = m;
+#pragma unroll
+            for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            const float f = fast_exp2(m - top);
+            float sum = f * l;
+#pragma unroll
+            for (int d = 1; d < 16; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            s_f.factor[c][r] = f;
+            if (c == 0) {
+                s_f.l[0][r] = inverse(sum);
+                if (rank == 0) put_lse(at, r, top, sum);
+            }
+        }
+        __syncthreads();
+        for (int e = tid; e < at.heads * channels; e += kAttnThreads) {
+            const int r = e / channels, d = e - r * channels;
+            float so = 0.f;
+#pragma unroll 8
+            for (int c = 0; c < C; ++c) so += s_f.factor[c][r] * sent->o[(c * channels + d) * kR + r];
+            O[(at.row + r) * D + rank * channels + d] = round16<BF>(so * s_f.l[0][r]);
+        }
+        return;
+    }
     const int j = lane % kPieces;
     const AttnPiece mine = s_piece[j];
     constexpr uint32_t kAll = kPieces == 32 ? 0xffffffffu : 0xffffu;
@@ -575,7 +656,6 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
     auto cluster_rec = [&](int w) { return reinterpret_cast<float*>(s_ring_all + (size_t)(w + 2) * G::kRingBytes) - kRec; };
     auto group_rec = [&](int g, int w) { return P.cta_rec + ((size_t)g * 2 * kAttnAbreast + w) * kRec; };        // (w = 2 member + 0 or 1)
     // threads over the units of the CTA, quads of heads, channels
-    const int quads = min(kR, P.group + 3) / 4;        // (at most what the group needs)
     for (int e = tid; e < __popc(leads) * quads * D; e += kAttnThreads) {
         const int d = e % D, x = e / D, nth = quads == 1 ? x : quads == 2 ? x / 2 : quads == 3 ? x / 3 : x / 4, r = 4 * (x - nth * quads);
         uint32_t rest = leads;

@@ -77,7 +77,7 @@ template <int D, int NT, int W>
 cudaError_t set_up_attn(int (&clusters)[5]) {
     cudaError_t e = allow_smem(k_page_attn<true, D, NT, W>, true);
     if (e == cudaSuccess) e = allow_smem(k_page_attn<false, D, NT, W>, true);
-    return e == cudaSuccess ? ask_clusters(k_page_attn<false, D, NT, W>, AttnGeom<D, W>::kThreads, attn_smem<D, W>(64), clusters) : e;
+    return e == cudaSuccess ? ask_clusters(k_page_attn<false, D, NT, W>, AttnGeom<D, W>::kThreads, attn_smem<D, NT, W>(64, true), clusters) : e;
 }
 
 const PagesDevice* device_of_call() {
@@ -159,10 +159,9 @@ bool attn_shape_ok(int batch, int q_heads, int kv_heads, int head_dim) {
 
 template <bool BF, int D, int W>
 int launch_attn(const PageAttnParams& p, int nt, uint64_t ctas, void* stream) {
-    const size_t smem = attn_smem<D, W>(p.batch);
     const int threads = AttnGeom<D, W>::kThreads, cluster = p.cluster > 1 ? p.cluster : 0;
-    return nt == 1 ? launch(k_page_attn<BF, D, 1, W>, ctas, threads, smem, cluster, p, stream)
-                   : launch(k_page_attn<BF, D, 2, W>, ctas, threads, smem, cluster, p, stream);
+    return nt == 1 ? launch(k_page_attn<BF, D, 1, W>, ctas, threads, attn_smem<D, 1, W>(p.batch, cluster > 0), cluster, p, stream)
+                   : launch(k_page_attn<BF, D, 2, W>, ctas, threads, attn_smem<D, 2, W>(p.batch, cluster > 0), cluster, p, stream);
 }
 
 template <class T>
@@ -308,7 +307,7 @@ int kvq_page_attn(const kvq_page_cache* cache, const void* Q, void* O, float* ls
     if (D == 64 && p.cluster == kAttnMaxCluster && longest > 8.0 * warps * p.cluster) p.cluster = widest(warps = 16);
     // Of very many rows the table of their places leaves no room for two CTAs of 8 warps (2 KB for what else a CTA has): one of 16 then
     // (4096 rows of 122 tokens of 8 heads, 1.05 GB: 179 us, with 8 warps 214).
-    if (D == 64 && 2 * (attn_smem<64, 8>(batch) + 2048) > (size_t)d->sm_smem) warps = 16;
+    if (D == 64 && 2 * (attn_smem<64, 1, 8>(batch, false) + 2048) > (size_t)d->sm_smem) warps = 16;
     // Where CTAs take equal shares of many units, two heads side by side in memory are read at the same time: 128 bytes of a row here and
     // there cost DRAM more than 256 (16 x 8192 tokens of 32 heads, slot by slot: 173 us, with one at a time 199, four 174, sixteen 179).
     p.abreast = p.cluster == 1 && p.slot_stride > p.head_stride && D == 64 && p.kv_heads * p.head_blocks % 2 == 0 ? kAttnAbreast : 1;
