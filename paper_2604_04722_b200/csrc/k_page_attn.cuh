@@ -34,7 +34,7 @@ namespace kvq {
 
 constexpr int kAttnTile = 16;                          // tokens
 constexpr int kAttnMaxCtas = 512;                      // of a launch
-constexpr int kAttnAbreast = 2;                        // units that a CTA's warps take side by side at most
+constexpr int kAttnAbreastLog2 = 1, kAttnAbreast = 1 << kAttnAbreastLog2;      // units that a CTA's warps take side by side at most
 constexpr int kAttnCounters = kAttnMaxCtas * kAttnAbreast;     // arrival counters of a workspace
 constexpr int kAttnUnitTiles = 20;                     // of a warp at most, where clusters take a unit each
 constexpr int kAttnMaxCluster = 16;
@@ -128,9 +128,10 @@ struct AttnPiece {
 template <bool BF, int D, int NT, int W>
 __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCtas) k_page_attn(const PageAttnParams P) {
     using G = AttnGeom<D, W>;
-    constexpr int kMt = D / 16, kR = 8 * NT, kStages = G::kStages, kAttnWarps = G::kWarps, kAttnThreads = G::kThreads;
+    constexpr int kMt = D / 16, kR = 8 * NT, kStages = G::kStages, kAttnWarps = G::kWarps, kAttnThreads = G::kThreads, kWarpsLog2 = W == 8 ? 3 : 4;
     namespace cg = cooperative_groups;
-    const int C = P.cluster, rank = C > 1 ? (int)cg::this_cluster().block_rank() : 0, group = (int)blockIdx.x / C, groups = (int)gridDim.x / C;
+    // (powers of two throughout: a division of integers takes longer than all else between two round trips to memory)
+    const int C = 1 << P.cluster_log2, group = (int)blockIdx.x >> P.cluster_log2, groups = (int)gridDim.x >> P.cluster_log2, rank = (int)blockIdx.x & (C - 1);
     constexpr int kVecs = D / 8, kRowsAtOnce = 32 / kVecs, kCopies = kAttnTile / kRowsAtOnce;     // 16-byte vectors of a row
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
     extern __shared__ __align__(128) uint8_t s_ring_all[];
@@ -211,9 +212,10 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
     const bool unit_each = units <= groups && longest <= kAttnUnitTiles * C * kAttnWarps;
     // With equal shares `abreast` units of a row that lie side by side in memory go abreast, each with its share of the CTA's warps
     // (member: which of them this warp works on); the axis then consists of such bundles of units.
-    const int abreast = unit_each ? 1 : P.abreast, team = kAttnWarps / abreast, member = warp / team;
-    const int bundles_per_row = units_per_row / abreast, snap = kAttnSnapBytes / (G::kStageBytes * abreast);
-    const int warps = C * team, warps_log2 = __ffs(warps) - 1;             // that share a stretch (a power of two)
+    const int abreast_log2 = unit_each ? 0 : P.abreast_log2, abreast = 1 << abreast_log2, team = kAttnWarps >> abreast_log2;
+    const int team_log2 = kWarpsLog2 - abreast_log2, member = warp >> team_log2;
+    const int bundles_per_row = units_per_row >> abreast_log2, snap = (kAttnSnapBytes / G::kStageBytes) >> abreast_log2;
+    const int warps_log2 = P.cluster_log2 + team_log2, warps = 1 << warps_log2;            // that share a stretch
     const int64_t total = tiles_before(P.batch) * bundles_per_row;
     const int stretches = unit_each ? units : (int)min((int64_t)groups, ((total + warps * kAttnMinTiles - 1) >> (warps_log2 + kAttnMinTilesLog2)));
     if (group >= stretches) return;
@@ -247,7 +249,7 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
     int64_t lo, hi;
     AttnCursor first = {};                             // the unit, where there is one
     if (unit_each) {
-        first.b = group / units_per_row;
+        first.b = (int)P.by_units.div((uint32_t)group);
         first.u = group - first.b * units_per_row;
         first.tiles = tiles_of(first.b);
         first.len = len_of(first.b);
@@ -261,7 +263,7 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
     if (unit_each && C > 1 && hi - lo > 1) cg::this_cluster().barrier_arrive();            // (before they write one another's memory, all have to be there)
     auto warp_border = [&](int w) -> int64_t { return lo + (((hi - lo) * w) >> warps_log2); };     // of the cluster's warps
     auto cta_border = [&](int r) { return warp_border(r * team); };
-    const int64_t wlo = warp_border(rank * team + warp % team), whi = warp_border(rank * team + warp % team + 1);
+    const int64_t wlo = warp_border(rank * team + (warp & (team - 1))), whi = warp_border(rank * team + (warp & (team - 1)) + 1);
     const int64_t cta_lo = cta_border(rank), cta_hi = cta_border(rank + 1);
 
     auto unit_of = [&](const AttnCursor& c) { return c.u * abreast + member; };        // this warp's, of the row
@@ -295,7 +297,7 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
             page = -1;
             if (looked >= count) return;
             const int pos = ahead.t * kAttnTile + (lane & 15);
-            head = P.head_blocks == 1 ? unit_of(ahead) : unit_of(ahead) / P.head_blocks;
+            head = (int)P.by_blocks.div((uint32_t)unit_of(ahead));
             if (pos < ahead.len) {
                 const int entry = (int)P.by_page.div((uint32_t)pos);
                 slot = pos - entry * P.page_size;
@@ -334,7 +336,7 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
         uint32_t qf[kMt][NT][2];
         float o[kMt][NT][4], m[NT][2], l[NT][2];
         auto start_unit = [&]() {
-            const int h0 = P.head_blocks == 1 ? unit_of(at) : unit_of(at) / P.head_blocks, hb = unit_of(at) - h0 * P.head_blocks;
+            const int h0 = (int)P.by_blocks.div((uint32_t)unit_of(at)), hb = unit_of(at) - h0 * P.head_blocks;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const int r = hb * kR + nt * 8 + g;    // head within the group
@@ -375,7 +377,7 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
             }
         };
         auto write_unit = [&]() {
-            const int h0 = P.head_blocks == 1 ? unit_of(at) : unit_of(at) / P.head_blocks, hb = unit_of(at) - h0 * P.head_blocks;
+            const int h0 = (int)P.by_blocks.div((uint32_t)unit_of(at)), hb = unit_of(at) - h0 * P.head_blocks;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const float i0 = inverse(l[nt][0]), i1 = inverse(l[nt][1]);
@@ -519,7 +521,7 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
         int heads;
     };
     auto place_of = [&](int unit) {
-        const int b = unit / units_per_row, u = unit - b * units_per_row, h0 = P.head_blocks == 1 ? u : u / P.head_blocks, hb = u - h0 * P.head_blocks;
+        const int b = (int)P.by_units.div((uint32_t)unit), u = unit - b * units_per_row, h0 = (int)P.by_blocks.div((uint32_t)u), hb = u - h0 * P.head_blocks;
         return Place{(size_t)b * P.q_heads + h0 * P.group + hb * kR, min(kR, P.group - hb * kR)};
     };
     auto put_lse = [&](const Place& at, int r, float m, float l) {
@@ -564,7 +566,8 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
             }
         }
         __syncthreads();
-        const int channels = D / C;                    // of a CTA
+        constexpr int kDLog2 = D == 64 ? 6 : 7;
+        const int channels_log2 = kDLog2 - P.cluster_log2, channels = 1 << channels_log2;      // of a CTA
         for (int e = tid; e < quads * D; e += kAttnThreads) {
             const int d = e % D, r = 4 * (e / D);
             float4 so = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -575,7 +578,7 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
                 so.x += f.x * y.x, so.y += f.y * y.y, so.z += f.z * y.z, so.w += f.w * y.w;
             }
             if (C == 1) put(at, r, d, so, &s_f.l[0][r]);
-            else *reinterpret_cast<float4*>(cg::this_cluster().map_shared_rank(sent, d / channels)->o + (rank * channels + d % channels) * kR + r) = so;
+            else *reinterpret_cast<float4*>(cg::this_cluster().map_shared_rank(sent, d >> channels_log2)->o + (rank * channels + (d & (channels - 1))) * kR + r) = so;
         }
         if (C == 1) return;
         cg::this_cluster().sync();                     // (from here on a CTA reads its own memory only)
@@ -597,7 +600,7 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
         }
         __syncthreads();
         for (int e = tid; e < at.heads * channels; e += kAttnThreads) {
-            const int r = e / channels, d = e - r * channels;
+            const int r = e >> channels_log2, d = e & (channels - 1);
             float so = 0.f;
 #pragma unroll 8
             for (int c = 0; c < C; ++c) so += s_f.factor[c][r] * sent->o[(c * channels + d) * kR + r];
@@ -646,7 +649,7 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
                 s_f.m[j][r] = top;
                 s_f.l[j][r] = closed ? inverse(sum) : sum;
                 if (closed) put_lse(place_of(mine.unit), r, top, sum);
-                else if (r == 0) s_open[2 * ((j >> 1) / team) + (mine.begin < cta_lo ? 0 : 1)] = j;
+                else if (r == 0) s_open[2 * ((j >> 1) >> team_log2) + (mine.begin < cta_lo ? 0 : 1)] = j;
             }
         }
     }
@@ -698,7 +701,7 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
         if (s_piece[i].begin >= cta_lo && s_piece[i].end <= cta_hi) {
             put(place_of(s_piece[i].unit), r, d, so, &s_f.l[i][r]);
         } else {
-            const int which = 2 * ((i >> 1) / team) + (s_piece[i].begin < cta_lo ? 0 : 1);
+            const int which = 2 * ((i >> 1) >> team_log2) + (s_piece[i].begin < cta_lo ? 0 : 1);
             float* rec = C > 1 ? cluster_rec(which) : group_rec(group, which);
             *reinterpret_cast<float4*>(rec + d * kR + r) = so;
             if (d < 2) *reinterpret_cast<float4*>(rec + (D + d) * kR + r) = *reinterpret_cast<const float4*>(d == 0 ? &s_f.m[i][r] : &s_f.l[i][r]);

@@ -159,7 +159,7 @@ bool attn_shape_ok(int batch, int q_heads, int kv_heads, int head_dim) {
 
 template <bool BF, int D, int W>
 int launch_attn(const PageAttnParams& p, int nt, uint64_t ctas, void* stream) {
-    const int threads = AttnGeom<D, W>::kThreads, cluster = p.cluster > 1 ? p.cluster : 0;
+    const int threads = AttnGeom<D, W>::kThreads, cluster = p.cluster_log2 > 0 ? 1 << p.cluster_log2 : 0;
     return nt == 1 ? launch(k_page_attn<BF, D, 1, W>, ctas, threads, attn_smem<D, 1, W>(p.batch, cluster > 0), cluster, p, stream)
                    : launch(k_page_attn<BF, D, 2, W>, ctas, threads, attn_smem<D, 2, W>(p.batch, cluster > 0), cluster, p, stream);
 }
@@ -292,6 +292,8 @@ int kvq_page_attn(const kvq_page_cache* cache, const void* Q, void* O, float* ls
     p.head_blocks = (p.group + 8 * space.nt - 1) / (8 * space.nt);
     p.scale2 = scale * kLog2e;
     p.by_page = FastDiv((uint32_t)cache->page_size);
+    p.by_units = FastDiv((uint32_t)(p.kv_heads * p.head_blocks));
+    p.by_blocks = FastDiv((uint32_t)p.head_blocks);
     // Clusters as wide as leaves one for every unit, with two tiles for every warp of the longest that the table could hold.  CTAs
     // of 8 warps, two to an SM, where that is enough (1 x 3000 tokens of 3 heads: 9.6 us, with 16 warps 12 us); of 16, so that a cluster
     // has more warps, where the longest unit would give more than eight tiles to a warp of the widest (1 x 32768 of 5 heads: 16.6 us, with 8 18.7).
@@ -302,20 +304,20 @@ int kvq_page_attn(const kvq_page_cache* cache, const void* Q, void* O, float* ls
         while (c < kAttnMaxCluster && longest >= 2.0 * warps * (2 * c) && units <= clusters[log2_of(2 * c)]) c *= 2;
         return c;
     };
-    int warps = 8;
-    p.cluster = widest(warps);
-    if (D == 64 && p.cluster == kAttnMaxCluster && longest > 8.0 * warps * p.cluster) p.cluster = widest(warps = 16);
+    int warps = 8, cluster = widest(warps);
+    if (D == 64 && cluster == kAttnMaxCluster && longest > 8.0 * warps * cluster) cluster = widest(warps = 16);
+    p.cluster_log2 = log2_of(cluster);
     // Of very many rows the table of their places leaves no room for two CTAs of 8 warps (2 KB for what else a CTA has): one of 16 then
     // (4096 rows of 122 tokens of 8 heads, 1.05 GB: 179 us, with 8 warps 214).
     if (D == 64 && 2 * (attn_smem<64, 1, 8>(batch, false) + 2048) > (size_t)d->sm_smem) warps = 16;
     // Where CTAs take equal shares of many units, two heads side by side in memory are read at the same time: 128 bytes of a row here and
     // there cost DRAM more than 256 (16 x 8192 tokens of 32 heads, slot by slot: 173 us, with one at a time 199, four 174, sixteen 179).
-    p.abreast = p.cluster == 1 && p.slot_stride > p.head_stride && D == 64 && p.kv_heads * p.head_blocks % 2 == 0 ? kAttnAbreast : 1;
+    p.abreast_log2 = cluster == 1 && p.slot_stride > p.head_stride && D == 64 && p.kv_heads * p.head_blocks % 2 == 0 ? kAttnAbreastLog2 : 0;
     // as many CTAs as the tables could give a tile to every warp of, as far as they are resident together
     const int resident = attn_resident(d->sm_count, D, warps);
-    const int most = p.cluster > 1 ? std::min(resident, p.cluster * d->attn_clusters[attn_variant(D, space.nt, warps)][log2_of(p.cluster)]) : resident;
-    const double wanted = std::max(units, std::ceil(units * longest / (warps * p.cluster)));       // clusters
-    const uint64_t ctas = (uint64_t)std::max(1.0, std::min((double)(most / p.cluster), wanted)) * p.cluster;
+    const int most = cluster > 1 ? std::min(resident, cluster * d->attn_clusters[attn_variant(D, space.nt, warps)][p.cluster_log2]) : resident;
+    const double wanted = std::max(units, std::ceil(units * longest / (warps * cluster)));       // clusters
+    const uint64_t ctas = (uint64_t)std::max(1.0, std::min((double)(most / cluster), wanted)) * cluster;
     if (cache->dtype == KVQ_BF16) {
         if (D == 128) return launch_attn<true, 128, 8>(p, space.nt, ctas, stream);
         return warps == 8 ? launch_attn<true, 64, 8>(p, space.nt, ctas, stream) : launch_attn<true, 64, 16>(p, space.nt, ctas, stream);

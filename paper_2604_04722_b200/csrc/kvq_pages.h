@@ -63,10 +63,10 @@ struct PageAttnParams {
     float* warp_rec;               // [CTAs][warps] records of R (D + 2) floats
     float* cta_rec;                // [CTAs][2 abreast][2] records
     int width, batch, n_pages, page_size, q_heads, kv_heads, group, head_blocks;
-    int abreast;                   // units of a row that a CTA's warps may take side by side: 1 or 2, divides kv_heads * head_blocks
-    int cluster;                   // CTAs that share a stretch of the axis and meet through shared memory (1: no clusters)
+    int abreast_log2;              // of the units of a row that a CTA's warps may take side by side: 0 or 1, divides kv_heads * head_blocks
+    int cluster_log2;              // of the CTAs that share a stretch of the axis and meet through shared memory (0: no clusters)
     float scale2;                  // softmax scale in log2 units
-    FastDiv by_page;
+    FastDiv by_page, by_units, by_blocks;              // page_size, kv_heads * head_blocks, head_blocks
 };
 
 struct BeamParams {
