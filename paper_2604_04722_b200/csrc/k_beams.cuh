@@ -30,7 +30,8 @@ constexpr int kBeamThreads = 512, kBeamWarps = kBeamThreads / 32;
 constexpr int kBeamMaxCluster = 16;
 constexpr int kBeamChunk = 512;                        // entries that a warp works on at a time, 16 per lane
 constexpr int kBeamBuffer = 128;                       // entries of a warp's buffer, 4 per lane: at least n + 32
-constexpr int kBeamTasks = (kMaxBeams + kBeamWarps - 1) / kBeamWarps;      // slices of a warp at most: where there are more rows than warps
+constexpr int kBeamRounds = 2;                         // slices of a warp at most: where there are more rows than warps
+static_assert(kMaxBeams <= kBeamRounds * kBeamWarps, "every row has its warp");
 constexpr int kBeamMaxSlices = kBeamMaxCluster * kBeamWarps;
 constexpr int kBeamGroups = 16;                        // groups of chunks of a warp's slices at most
 constexpr float kBeamLowest = -FLT_MAX;
@@ -201,10 +202,9 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
     extern __shared__ __align__(16) uint8_t s_dyn[];
     const int n = P.n_out;
     const int tasks = P.beams * P.slices, warps = ctas * kBeamWarps, gwarp = rank * kBeamWarps + warp;
-    const int rounds = (tasks + warps - 1) / warps;    // slices of a warp, at most kBeamTasks
-    const int most_groups = kBeamGroups / rounds, chunks = (P.slice_len + kBeamChunk - 1) / kBeamChunk;
-    const int group_len = (chunks + most_groups - 1) / most_groups * kBeamChunk;           // entries of a group
-    const int per_slice = (P.slice_len + group_len - 1) / group_len, groups = kBeamWarps * rounds * per_slice;     // groups of a slice, of the CTA
+    const int rounds = P.rounds, group_len = P.group_len, per_slice = P.per_slice, groups = kBeamWarps * rounds * per_slice;       // groups of the CTA
+    auto slice_no = [&](int task) { return (int)P.by_beams.div((uint32_t)task); };
+    auto row_no = [&](int task) { return task - slice_no(task) * P.beams; };
     BeamPick* s_buffers = reinterpret_cast<BeamPick*>(s_dyn);              // [warps][kBeamBuffer]
     BeamPick* s_picks = s_buffers + kBeamWarps * kBeamBuffer;              // [threads]
     BeamPick* s_sent = s_picks + kBeamThreads;                             // [CTAs][n]
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
     };
     auto slice_of = [&](int task) {
         Slice v;
-        const int row = task % P.beams, slice = task / P.beams;
+        const int slice = slice_no(task), row = task - slice * P.beams;
         v.lo = (int)min((long long)slice * P.slice_len, (long long)P.vocab);
         v.hi = (int)min((long long)v.lo + P.slice_len, (long long)P.vocab);
         v.z = static_cast<const T*>(P.logits) + ((size_t)b * P.beams + row) * (size_t)P.vocab;
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
         float top = kBeamLowest;
         double sum = 0.0;
         if (task < tasks) {
-            const int row = task % P.beams;
+            const int row = row_no(task);
             const size_t r = (size_t)b * P.beams + row;
             float* tops = s_group_top + (warp * rounds + j) * per_slice;
             const Slice v = slice_of(task);
@@ -384,14 +384,14 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
     __syncthreads();
     // ---- a bound: the n-th best of the CTA's groups' largest entries, which n of its candidates reach
     auto slice_of_group = [&](int group, int& g) {     // the slice (task) of a group and its number there
-        const int slot = group / per_slice, w = rounds == 1 ? slot : slot / rounds;
+        const int slot = (int)P.by_groups.div((uint32_t)group), w = rounds == 1 ? slot : slot >> 1;
         g = group - slot * per_slice;
         return rank * kBeamWarps + w + (slot - w * rounds) * warps;
     };
     uint64_t best = 0;                                 // of this thread's group
     if (tid < kBeamWarps * kBeamGroups) {
         int g;
-        const int task = slice_of_group(min(tid, groups - 1), g), row = task % P.beams;
+        const int task = slice_of_group(min(tid, groups - 1), g), row = row_no(task);
         const float top = s_group_top[tid];
         if (tid < groups && task < tasks && s_alive[row] && top > -INFINITY) best = score_key(s_row_off[row] + ((double)top - (double)s_row_top[row]));
         s_group_best[tid] = best;
@@ -421,7 +421,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
 #pragma unroll 1
             for (int i = warp; i < listed; i += kBeamWarps) {
                 int g;
-                const int task = slice_of_group(s_list[i], g), row = task % P.beams;
+                const int task = slice_of_group(s_list[i], g), row = row_no(task);
                 const double off = s_row_off[row];
                 const float row_top = s_row_top[row];
                 auto score_of = [&](float x) { return score_key(off + ((double)x - (double)row_top)); };

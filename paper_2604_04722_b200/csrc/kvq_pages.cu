@@ -364,6 +364,12 @@ int kvq_beam_select(const void* logits, int dtype, const float* scores, const ui
     // slices of at least a chunk, at most as many as there are warps (a row each where there are more rows)
     p.slices = std::max(1, std::min(ctas * kBeamWarps / beams, (vocab + kBeamChunk - 1) / kBeamChunk));
     p.slice_len = (int)((((int64_t)vocab + p.slices - 1) / p.slices + 255) / 256 * 256);
+    p.rounds = (beams * p.slices + ctas * kBeamWarps - 1) / (ctas * kBeamWarps);
+    const int most_groups = kBeamGroups / p.rounds, slice_chunks = (p.slice_len + kBeamChunk - 1) / kBeamChunk;
+    p.group_len = (slice_chunks + most_groups - 1) / most_groups * kBeamChunk;
+    p.per_slice = (p.slice_len + p.group_len - 1) / p.group_len;
+    p.by_beams = FastDiv((uint32_t)beams);
+    p.by_groups = FastDiv((uint32_t)p.per_slice);
     const bool rows_aligned = aligned(logits, 16) && (size_t)vocab * size % 16 == 0;
     if (dtype == KVQ_FP32) return launch_beams<float>(p, rows_aligned, ctas, stream);
     return dtype == KVQ_BF16 ? launch_beams<__nv_bfloat16>(p, rows_aligned, ctas, stream) : launch_beams<__half>(p, rows_aligned, ctas, stream);

@@ -79,6 +79,9 @@ struct BeamParams {
     const void* logits_end;        // first byte behind the logits
     int batch, beams, vocab, n_out, end_token;
     int slices, slice_len;         // pieces of a row, entries of a piece (a multiple of 256)
+    int rounds;                    // slices of a warp
+    int group_len, per_slice;      // entries of a group of chunks, groups of a slice
+    FastDiv by_beams, by_groups;   // beams, per_slice
 };
 
 }  // namespace kvq
