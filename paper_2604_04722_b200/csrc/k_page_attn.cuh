@@ -36,7 +36,7 @@ constexpr int kAttnTile = 16;                          // tokens
 constexpr int kAttnMaxCtas = 512;                      // of a launch
 constexpr int kAttnAbreastLog2 = 1, kAttnAbreast = 1 << kAttnAbreastLog2;      // units that a CTA's warps take side by side at most
 constexpr int kAttnCounters = kAttnMaxCtas * kAttnAbreast;     // arrival counters of a workspace
-constexpr int kAttnUnitTiles = 20;                     // of a warp at most, where clusters take a unit each
+constexpr int kAttnJoinTiles = 10;                     // what a unit that goes on in another stretch costs, in tiles of a warp
 constexpr int kAttnMaxCluster = 16;
 constexpr int kAttnMinTilesLog2 = 1, kAttnMinTiles = 1 << kAttnMinTilesLog2;   // of a warp, where the work does not fill the launch
 // How far a border may be from a unit's to move there: what a CTA streams in about the time that a join takes (3 us).
@@ -204,12 +204,14 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
     }
     if (s_place[P.batch] == 0) return;
     // A cluster of CTAs (or one CTA) works on a stretch of the axis: a unit each, where there are no more units than clusters and
-    // none is long; otherwise equal shares.
+    // equal shares would not be shorter than the longest by more than joining them costs (2 units of 65536 tokens: 16.8 us in equal shares,
+    // 19.0 one each; 48 of up to 6000: 25.1 and 16.9).
     int longest = 0;
 #pragma unroll
     for (int w = 0; w < kAttnWarps; ++w) longest = max(longest, s_longest[w]);
     const int units = P.batch * units_per_row;
-    const bool unit_each = units <= groups && longest <= kAttnUnitTiles * C * kAttnWarps;
+    const bool unit_each = units <= groups &&
+                           (int64_t)longest * groups <= tiles_before(P.batch) * units_per_row + (int64_t)kAttnJoinTiles * C * kAttnWarps * groups;
     // With equal shares `abreast` units of a row that lie side by side in memory go abreast, each with its share of the CTA's warps
     // (member: which of them this warp works on); the axis then consists of such bundles of units.
     const int abreast_log2 = unit_each ? 0 : P.abreast_log2, abreast = 1 << abreast_log2, team = kAttnWarps >> abreast_log2;

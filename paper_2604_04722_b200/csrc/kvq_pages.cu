@@ -305,7 +305,7 @@ int kvq_page_attn(const kvq_page_cache* cache, const void* Q, void* O, float* ls
         return c;
     };
     int warps = 8, cluster = widest(warps);
-    if (D == 64 && cluster == kAttnMaxCluster && longest > 8.0 * warps * cluster) cluster = widest(warps = 16);
+    if (D == 64 && cluster == kAttnMaxCluster && longest > 8.0 * warps * cluster && widest(16) == cluster) warps = 16;
     p.cluster_log2 = log2_of(cluster);
     // Of very many rows the table of their places leaves no room for two CTAs of 8 warps (2 KB for what else a CTA has): one of 16 then
     // (4096 rows of 122 tokens of 8 heads, 1.05 GB: 179 us, with 8 warps 214).

@@ -343,6 +343,17 @@ def test_attention_split_over_many_warps(kq, lens, q_heads, kv_heads, D):
     a.check(heads=range(min(kv_heads, 3)))
 
 
+@pytest.mark.parametrize("lens,q_heads,kv_heads,D", [
+    ([65536], 8, 2, 64), ([70000, 3, 20000], 9, 3, 64), ([40000], 2, 2, 128), ([40000, 500, 0, 9000], 16, 1, 128), ([50000], 20, 1, 64),
+    ([20000, 100, 5000] * 8, 6, 2, 64), ([16000, 40] * 35, 4, 2, 64), ([9000, 33, 1] * 24, 2, 1, 128), ([31000, 17, 0] * 3, 33, 1, 128)])
+def test_attention_of_units_longer_than_equal_shares(kq, lens, q_heads, kv_heads, D):
+    """Clusters that share units with one another."""
+    a = Attn(kq, lens, q_heads, kv_heads, D, 16, "bf16", seed=len(lens))
+    for _ in range(2):
+        a.call()
+    a.check()
+
+
 @pytest.mark.parametrize("q_heads,kv_heads,D,rows", [(42, 2, 64, 90), (33, 1, 64, 100), (64, 2, 128, 90), (10, 10, 64, 40), (6, 6, 64, 33)])
 @pytest.mark.parametrize("order", ["slots", "heads"])
 def test_attention_of_many_rows_and_heads_side_by_side(kq, q_heads, kv_heads, D, rows, order):
