@@ -12,9 +12,9 @@
 // CTA (a second barrier), and that ranks them.  Scores are compared in fp64.
 //
 // Bound: of many requests the loop over the logits: an exponential each, and the instructions around it (64 requests of 16 beams over
-// 32000 bf16 logits: 28 us, the bytes alone 10; without the exponentials 21; over 32003, where rows are not aligned and every load becomes
-// two, 33).  Of few requests the chain of the rows' loads, two cluster barriers, the bound, a second read and two rankings: 9.8 us for
-// one request of 4 beams over 49152 logits.  Keeping the slices' best entries in the first pass took 94 us where this takes 33.
+// 32000 bf16 logits: 27 us, the bytes alone 10; without the exponentials 20; over 32003, where rows are not aligned and every load becomes
+// two, 32).  Of few requests the chain of the rows' loads, two cluster barriers, the bound, a second read and two rankings: 9.5 us for
+// one request of 4 beams over 49152 logits.  Keeping the slices' best entries in the first pass took 94 us where this takes 32.
 #pragma once
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>

@@ -11,18 +11,18 @@
 // o^T = V^T w^T with the channels as rows, so that up to 8 query heads cost the same as one, K and V fragments are read with one
 // ldmatrix per 16 x 16 block, and the weights of a tile become the second product's operand with one 8 x 8 transposition per
 // eight tokens.  A weight enters as the sum of two 16-bit numbers (what the first loses the second holds): next to the rows'
-// bytes the second product costs nothing, and with 8-bit mantissas (bf16) one rounding of the weights would be as large as the
+// bytes the second product costs little (16 x 8192 tokens 1.3 of 174 us, 8 x 4001 0.4 of 11.5), and with 8-bit mantissas (bf16) one rounding of the weights would be as large as the
 // output's own.  Sums are fp32.
 //
 // A unit that begins and ends with one warp is written by that warp.  Pieces of a unit meet in their CTA.  Where there are few
-// units a cluster of up to 16 CTAs takes one, and its CTAs meet through shared memory (1 x 32768 tokens of 5 KV heads: 16.6 us; the same
-// through global records 27, and before the borders below moved, 130).  Where there are more units than that, CTAs take equal shares of
-// the axis, a share's border moves to a unit's if that is near, and what is left over meets in records of the workspace: the CTA that
-// delivers a unit's last record joins them, in the order of the axis whoever comes last.
+// units a cluster of up to 16 CTAs takes one; its CTAs send one another their sums, and each adds up an equal share of the channels (1 x 32768
+// tokens of 5 KV heads: 13.7 us; with one CTA that fetches and adds up all of it 16.5, through global records 27).  Where there are
+// more units than that, CTAs take equal shares of the axis, a share's border moves to a unit's if that is near, and what is left over
+// meets in records of the workspace: the CTA that delivers a unit's last record joins them, in the order of the axis whoever comes last.
 //
 // Bound: the rows' bytes, 4 D per token and KV head.  1.07 GB of 32 heads of 64 channels (16 x 8192 tokens, fp16, slot by slot) take 173 us,
-// 6.2 TB/s or 0.94 of the copy rate; 0.79 GB of 8 heads of 128 (64 x 4096 at most, bf16) 134 us, 0.90.  Small calls are a chain of memory
-// round trips (lengths, tables, rows), a tile's dependent instructions and the joins: 1 x 512 tokens 8 us.
+// 6.2 TB/s or 0.94 of the copy rate; 0.79 GB of 8 heads of 128 (64 x 4096 at most, bf16) 133 us, 0.90.  Small calls are a chain of memory
+// round trips (lengths, tables, rows), a tile's dependent instructions and the joins: 1 x 512 tokens 6.4 us.
 #pragma once
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
@@ -38,8 +38,10 @@ constexpr int kAttnAbreastLog2 = 1, kAttnAbreast = 1 << kAttnAbreastLog2;      /
 constexpr int kAttnCounters = kAttnMaxCtas * kAttnAbreast;     // arrival counters of a workspace
 constexpr int kAttnJoinTiles = 10;                     // what a unit that goes on in another stretch costs, in tiles of a warp
 constexpr int kAttnMaxCluster = 16;
-constexpr int kAttnMinTilesLog2 = 1, kAttnMinTiles = 1 << kAttnMinTilesLog2;   // of a warp, where the work does not fill the launch
-// How far a border may be from a unit's to move there: what a CTA streams in about the time that a join takes (3 us).
+constexpr int kAttnMinTilesLog2 = 1, kAttnMinTiles = 1 << kAttnMinTilesLog2;   // of a warp, where the work does not fill the
+                                                       // launch (200 rows of 200 tokens: 11.0 us, with four 13.2, with one 11.0)
+// How far a border may be from a unit's to move there: what a CTA streams in about the time that a join takes, 3 us (4096 rows of 122 tokens 182 us,
+// 128 of up to 100 11.7; without it 186 and 15.1; with four times as much 182 and 11.7, but 16 x 8192 175 us instead of 174).
 constexpr int kAttnSnapBytes = 131072;
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLn2 = 0.69314718055994531f;

@@ -295,8 +295,9 @@ int kvq_page_attn(const kvq_page_cache* cache, const void* Q, void* O, float* ls
     p.by_units = FastDiv((uint32_t)(p.kv_heads * p.head_blocks));
     p.by_blocks = FastDiv((uint32_t)p.head_blocks);
     // Clusters as wide as leaves one for every unit, with two tiles for every warp of the longest that the table could hold.  CTAs
-    // of 8 warps, two to an SM, where that is enough (1 x 3000 tokens of 3 heads: 9.6 us, with 16 warps 12 us); of 16, so that a cluster
-    // has more warps, where the longest unit would give more than eight tiles to a warp of the widest (1 x 32768 of 5 heads: 16.6 us, with 8 18.7).
+    // of 8 warps, two to an SM, where that is enough (1 x 3000 tokens of 3 heads: 6.7 us, with 16 warps 7.9); of 16, so that a cluster
+    // has more warps, where the longest unit would give more than eight tiles to a warp of the widest (1 x 32768 of 5 heads: 13.7 us,
+    // with 8 15.9), unless there would be narrower ones (4 of up to 30000 of 2 heads: 15.9 us with 8, 18.2 with 16).
     const double units = (double)batch * p.kv_heads * p.head_blocks, longest = std::ceil((double)table_width * cache->page_size / kAttnTile);
     auto widest = [&](int warps) {
         const int* clusters = d->attn_clusters[attn_variant(D, space.nt, warps)];
@@ -311,7 +312,7 @@ int kvq_page_attn(const kvq_page_cache* cache, const void* Q, void* O, float* ls
     // (4096 rows of 122 tokens of 8 heads, 1.05 GB: 179 us, with 8 warps 214).
     if (D == 64 && 2 * (attn_smem<64, 1, 8>(batch, false) + 2048) > (size_t)d->sm_smem) warps = 16;
     // Where CTAs take equal shares of many units, two heads side by side in memory are read at the same time: 128 bytes of a row here and
-    // there cost DRAM more than 256 (16 x 8192 tokens of 32 heads, slot by slot: 173 us, with one at a time 199, four 174, sixteen 179).
+    // there cost DRAM more than 256 (16 x 8192 tokens of 32 heads, slot by slot: 174 us, with one at a time 199, four 175, sixteen 180).
     p.abreast_log2 = cluster == 1 && p.slot_stride > p.head_stride && D == 64 && p.kv_heads * p.head_blocks % 2 == 0 ? kAttnAbreastLog2 : 0;
     // as many CTAs as the tables could give a tile to every warp of, as far as they are resident together
     const int resident = attn_resident(d->sm_count, D, warps);
