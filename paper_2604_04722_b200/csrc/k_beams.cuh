@@ -230,9 +230,11 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
         uint32_t off;
         bool inside;                                   // whole vectors lie within the tensor
     };
-    // A chunk on its way.  Where rows are not aligned an entry lies in a lane's vector or in the one after it; both are loaded, and
-    // entries taken from where they lie when they are used (for fp32, which would take twice the registers, shifted at once).
-    constexpr bool kPairs = !ALIGNED && sizeof(T) == 2;
+    // A chunk on its way.  Where rows are not aligned a 16-bit entry lies in a lane's vector or in the one after it; both are loaded, and
+    // entries taken from where they lie when they are used.  fp32 entries are loaded one by one then, neighbours by neighbouring lanes (two
+    // vectors would take twice the registers; shifted as they arrive, every chunk is waited for: 15 x 15 beams over 42689 SHIFTED us, so PLAIN).
+    constexpr bool kPairs = !ALIGNED && sizeof(T) == 2, kSingle = !ALIGNED && sizeof(T) == 4;
+    auto place = [&](int k) { return kSingle ? k * 32 + lane : (k / kVec * 32 + lane) * kVec + k % kVec; };      // of a lane's k-th entry in its chunk
     struct Raw {
         uint4 v[kLoads][kPairs ? 2 : 1];
     };
@@ -253,6 +255,14 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
         return v;
     };
     auto load = [&](const Slice& v, int c0, Raw& raw) {
+        if constexpr (kSingle) {
+            uint32_t w[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) w[k] = c0 + place(k) < v.hi ? __float_as_uint(__ldg(reinterpret_cast<const float*>(v.z) + c0 + place(k))) : 0u;
+#pragma unroll
+            for (int k = 0; k < kLoads; ++k) raw.v[k][0] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+            return;
+        }
         const bool inside = v.inside || ends_inside(v.vecs, v.off, c0, min(v.hi, c0 + kBeamChunk));    // (only the tensor's first and last chunk are not)
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
@@ -270,9 +280,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
                 raw.v[k][0] = __ldg(v.vecs + t / kVec);
                 if (v.off) raw.v[k][1] = __ldg(v.vecs + t / kVec + 1);
             } else {
-                const uint4 u = __ldg(v.vecs + t / kVec);
-                raw.v[k][0] = u;
-                if (!ALIGNED && v.off) raw.v[k][0] = shifted(u, __ldg(v.vecs + t / kVec + 1), v.off);
+                raw.v[k][0] = __ldg(v.vecs + t / kVec);
             }
         }
     };
@@ -299,7 +307,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
         if (c0 + kBeamChunk > v.hi) {
 #pragma unroll
             for (int k = 0; k < 16; ++k)
-                if (c0 + ((k / kVec) * 32 + lane) * kVec + k % kVec >= v.hi) x[k] = -INFINITY;
+                if (c0 + place(k) >= v.hi) x[k] = -INFINITY;
         }
     };
 #pragma unroll 1
@@ -486,7 +494,7 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
                         BeamPick p;
                         p.score = score_of(z);
                         p.row = (uint32_t)row;
-                        p.token = (uint32_t)(c0 + (k / kVec * 32 + lane) * kVec + k % kVec);
+                        p.token = (uint32_t)(c0 + place(k));
                         keep(k >= 0 && p.score >= reach && (worst.score == 0 || p.before(worst)), p);
                         hits &= hits - 1;
                     }
