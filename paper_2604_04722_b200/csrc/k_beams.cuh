@@ -12,8 +12,8 @@
 // CTA (a second barrier), and that ranks them.  Scores are compared in fp64.
 //
 // Bound: of many requests the loop over the logits: an exponential each, and the instructions around it (64 requests of 16 beams over
-// 32000 bf16 logits: 27 us, the bytes alone 10; without the exponentials 20; over 32003, where rows are not aligned and every load becomes
-// two, 32).  Of few requests the chain of the rows' loads, two cluster barriers, the bound, a second read and two rankings: 9.5 us for
+// 32000 bf16 logits: 25.5 us, the bytes alone 10; the exponentials are 7 of it; over 32003, where rows are not aligned and every load becomes
+// two, 32).  Of few requests the chain of the rows' loads, two cluster barriers, the bound, a second read and two rankings: 9.1 us for
 // one request of 4 beams over 49152 logits.  Keeping the slices' best entries in the first pass took 94 us where this takes 32.
 #pragma once
 #include <cooperative_groups.h>
@@ -133,17 +133,14 @@ __device__ __forceinline__ uint4 shifted(const uint4& u, const uint4& w, uint32_
     const uint32_t bits = (off & 3u) * 8u;
     return make_uint4(__funnelshift_r(x0, x1, bits), __funnelshift_r(x1, x2, bits), __funnelshift_r(x2, x3, bits), __funnelshift_r(x3, x4, bits));
 }
-// Eight (16-bit) or four (fp32) neighbouring entries of a row as they lie in memory, one by one, for the ends of the tensor: `n` of
-// them, the rest is zero.
+// Eight neighbouring 16-bit entries of a row as they lie in memory, one by one, for the ends of the tensor: `n` of them, the rest is zero.
 template <class T>
 __device__ __noinline__ uint4 load_few(const T* src, int n) {
-    constexpr int kN = 16 / sizeof(T);
     uint32_t out[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {
+    for (int i = 0; i < 8; ++i) {
         if (i >= n) break;
-        if constexpr (sizeof(T) == 2) out[i / 2] |= (uint32_t)(*reinterpret_cast<const uint16_t*>(src + i)) << (16 * (i & 1));
-        else out[i] = *reinterpret_cast<const uint32_t*>(src + i);
+        out[i / 2] |= (uint32_t)(*reinterpret_cast<const uint16_t*>(src + i)) << (16 * (i & 1));
     }
     return make_uint4(out[0], out[1], out[2], out[3]);
 }
@@ -225,14 +222,15 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
     // a warp's view of a slice
     struct Slice {
         int lo, hi;
-        const T* z;
-        const uint4* vecs;                             // the row from the 16-byte border before its start
+        const T* z;                                    // its row
+        const uint4* vecs;                             // (kPairs) the row from the 16-byte border before its start
         uint32_t off;
         bool inside;                                   // whole vectors lie within the tensor
     };
-    // A chunk on its way.  Where rows are not aligned a 16-bit entry lies in a lane's vector or in the one after it; both are loaded, and
-    // entries taken from where they lie when they are used.  fp32 entries are loaded one by one then, neighbours by neighbouring lanes (two
-    // vectors would take twice the registers; shifted as they arrive, every chunk is waited for: 15 x 15 beams over 42689 SHIFTED us, so PLAIN).
+    // A chunk on its way: a vector for every 16 bytes.  Where rows are not aligned a 16-bit entry lies in a lane's vector or in the one after
+    // it; both are loaded, and entries taken from where they lie when they are used (64 x 16 beams over 32003 bf16 logits 32 us, loaded one
+    // by one 45).  fp32 entries are loaded one by one, neighbours by neighbouring lanes: two vectors would take twice the registers, and
+    // shifted as they arrive every chunk is waited for (15 x 15 beams over 42689 logits 42 us, so 30).
     constexpr bool kPairs = !ALIGNED && sizeof(T) == 2, kSingle = !ALIGNED && sizeof(T) == 4;
     auto place = [&](int k) { return kSingle ? k * 32 + lane : (k / kVec * 32 + lane) * kVec + k % kVec; };      // of a lane's k-th entry in its chunk
     struct Raw {
@@ -248,10 +246,12 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
         v.lo = (int)min((long long)slice * P.slice_len, (long long)P.vocab);
         v.hi = (int)min((long long)v.lo + P.slice_len, (long long)P.vocab);
         v.z = static_cast<const T*>(P.logits) + ((size_t)b * P.beams + row) * (size_t)P.vocab;
-        const uintptr_t at = reinterpret_cast<uintptr_t>(v.z);
-        v.off = ALIGNED ? 0u : (uint32_t)(at & 15u);
-        v.vecs = reinterpret_cast<const uint4*>(at - v.off);
-        v.inside = ends_inside(v.vecs, v.off, v.lo, v.hi);
+        if constexpr (kPairs) {
+            const uintptr_t at = reinterpret_cast<uintptr_t>(v.z);
+            v.off = (uint32_t)(at & 15u);
+            v.vecs = reinterpret_cast<const uint4*>(at - v.off);
+            v.inside = ends_inside(v.vecs, v.off, v.lo, v.hi);
+        }
         return v;
     };
     auto load = [&](const Slice& v, int c0, Raw& raw) {
@@ -261,27 +261,25 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
             for (int k = 0; k < 16; ++k) w[k] = c0 + place(k) < v.hi ? __float_as_uint(__ldg(reinterpret_cast<const float*>(v.z) + c0 + place(k))) : 0u;
 #pragma unroll
             for (int k = 0; k < kLoads; ++k) raw.v[k][0] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
-            return;
-        }
-        const bool inside = v.inside || ends_inside(v.vecs, v.off, c0, min(v.hi, c0 + kBeamChunk));    // (only the tensor's first and last chunk are not)
+        } else if constexpr (kPairs) {
+            const bool inside = v.inside || ends_inside(v.vecs, v.off, c0, min(v.hi, c0 + kBeamChunk));    // (only the tensor's first and last chunk are not)
 #pragma unroll
-        for (int k = 0; k < kLoads; ++k) {
-            const int t = c0 + (k * 32 + lane) * kVec;
-            if (t >= v.hi) continue;
-            if (!inside) {
-                const uint4 few = load_few<T>(v.z + t, P.vocab - t);
-                raw.v[k][0] = few;
-                if constexpr (kPairs) {                // as if it had been read behind the border
-                    raw.v[k][0] = shifted(make_uint4(0, 0, 0, 0), few, 16u - v.off);
-                    if (v.off == 0) raw.v[k][0] = few;
+            for (int k = 0; k < kLoads; ++k) {
+                const int t = c0 + (k * 32 + lane) * kVec;
+                if (t >= v.hi) continue;
+                if (inside) {
+                    raw.v[k][0] = __ldg(v.vecs + t / kVec);
+                    if (v.off) raw.v[k][1] = __ldg(v.vecs + t / kVec + 1);
+                } else {                               // as if it had been read behind the border
+                    const uint4 few = load_few<T>(v.z + t, P.vocab - t);
+                    raw.v[k][0] = v.off ? shifted(make_uint4(0, 0, 0, 0), few, 16u - v.off) : few;
                     raw.v[k][1] = shifted(few, make_uint4(0, 0, 0, 0), 16u - v.off);
                 }
-            } else if constexpr (kPairs) {
-                raw.v[k][0] = __ldg(v.vecs + t / kVec);
-                if (v.off) raw.v[k][1] = __ldg(v.vecs + t / kVec + 1);
-            } else {
-                raw.v[k][0] = __ldg(v.vecs + t / kVec);
             }
+        } else {                                       // (a row is whole vectors)
+#pragma unroll
+            for (int k = 0; k < kLoads; ++k)
+                if (c0 + place(k * kVec) < v.hi) raw.v[k][0] = __ldg(reinterpret_cast<const uint4*>(v.z + c0 + place(k * kVec)));
         }
     };
     auto values = [&](const Slice& v, int c0, const Raw& raw, float (&x)[16]) {
