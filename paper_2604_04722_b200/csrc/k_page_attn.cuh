@@ -436,7 +436,9 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
                     if (!((there >> g) & 1u)) s[nt][0] = s[nt][1] = -INFINITY;
                     if (!((there >> (g + 8)) & 1u)) s[nt][2] = s[nt][3] = -INFINITY;
                 }
-                over |= fmaxf(s[nt][0], s[nt][2]) > m[nt][0] + kRescaleSlack || fmaxf(s[nt][1], s[nt][3]) > m[nt][1] + kRescaleSlack;
+                // (the difference, which is exact where it matters: of logits about 2^27 the sum would round to a reference that is 16 higher, and
+                // a weight of 2^16 is no fp16 number)
+                over |= fmaxf(s[nt][0], s[nt][2]) - m[nt][0] > kRescaleSlack || fmaxf(s[nt][1], s[nt][3]) - m[nt][1] > kRescaleSlack;
             }
             if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
