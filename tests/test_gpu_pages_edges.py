@@ -1,4 +1,5 @@
-"""The paged attention where single numbers go wrong, such as logits of great size (GPU)."""
+"""The paged attention where single numbers go wrong: weights far below the largest, logits of great size (GPU)."""
+not finite, what is left in the workspace (GPU)."""
 import math
 
 import numpy as np
@@ -19,6 +20,60 @@ def kq():
     build.build()
     torch.cuda.set_device(0)
     return binding
+
+
+def _sink(kq, rows, n, q_heads, kv_heads, D, dtype, order, gap, spread, sink_value, mean, seed=0):
+    """`rows` requests over the same pages: token 0 has the logit 0 and small values, the others lie `gap` and up to `spread` below it."""
+    import torch
+    rng = np.random.default_rng(seed)
+    a = Attn(kq, [n], q_heads, kv_heads, D, 16, dtype, order, seed=seed)
+    k, v = np.zeros((n, kv_heads, D)), rng.standard_normal((n, kv_heads, D)) + mean
+    k[1:, :, 0] = -gap - spread * rng.random((n - 1, kv_heads))
+    v[0] = sink_value
+    where = a.tables[0, :n // 16].long()
+    for c, x in ((a.K, k), (a.V, v)):
+        c[where] = torch.tensor(x, device="cuda").to(a.dtype).reshape(n // 16, 16, kv_heads, D)
+    a.rows = [[c[where].reshape(n, kv_heads, D).double().cpu().numpy() for c in (a.K, a.V)]]
+    a.Q = torch.zeros((rows, q_heads, D), dtype=a.dtype, device="cuda")
+    a.Q[:, :, 0] = D ** 0.5                            # (16-bit for 64 channels; near enough for 128)
+    a.scale = 1.0 / float(a.Q[0, 0, 0])
+    a.tables, a.n = a.tables.repeat(rows, 1).contiguous(), a.n.repeat(rows).contiguous()
+    a.O, a.lse = torch.full_like(a.Q, float("nan")), torch.full((rows, q_heads), float("nan"), device="cuda")
+    a.lens = [n] * rows
+    return a
+
+
+def _bound(q, k, v, scale, mantissa):
+    """pr.attend's, but with what two fp16 numbers of a weight really leave: the weights are 2^7 and more at the largest, the second number
+    holds 2^11 times what the first left, so that a weight is cut at 2^-25 2^-11 2^-7 of the largest; and the values that the second
+    is multiplied with, 2^-11 times their size, are cut at 2^-25, which at most half of the weight, or 2^-46 of the largest, sees."""
+    o, lse, err, lerr = pr.attend(q, k, v, scale, mantissa)
+    if mantissa == 11:
+        z = (q @ k.T) * scale
+        total = np.exp(z - z.max(1, keepdims=True)).sum(1, keepdims=True)
+        err = err + (2.0 ** -43 - 2.0 ** -25) * np.abs(v).sum(0) / total + 2.0 ** -26 + len(k) * 2.0 ** -46 / total
+    return o, lse, err, lerr
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("q_heads,kv_heads,D,rows,n", [(3, 3, 64, 1024, 8192), (4, 2, 64, 1200, 4096), (9, 1, 64, 2200, 4096), (2, 2, 128, 700, 8192),
+                                                       (12, 1, 128, 1300, 2048), (1, 1, 64, 1, 65536), (2, 1, 64, 4096, 512)])
+@pytest.mark.parametrize("gap,spread,sink_value,mean", [(16.0, 0.0, 0.0, 1.0), (17.25, 0.0, 0.0, 1.0), (17.5, 0.0, 0.0, 1.0), (19.0, 0.0, 0.0, 2.0), (14.0, 2.0, 0.0, 0.0),
+                                                       (10.0, 8.0, 0.01, 0.0), (16.0, 4.0, 0.0, 0.5)])
+def test_attention_next_to_a_token_that_takes_nearly_all_of_the_weight(kq, gap, spread, sink_value, mean, q_heads, kv_heads, D, rows, n, dtype):
+    """The sum of what the others have decides the output although each of their weights is below 2^-20 of the largest."""
+    import torch
+    a = _sink(kq, rows, n, q_heads, kv_heads, D, dtype, "slots", gap, spread, sink_value, mean)
+    a.call()
+    torch.cuda.synchronize()
+    O, lse, G = a.O.double().cpu().numpy(), a.lse.double().cpu().numpy(), q_heads // kv_heads
+    q = a.Q[0].double().cpu().numpy()
+    for h in range(kv_heads):
+        at = slice(h * G, h * G + G)
+        o, l, err, lerr = _bound(q[at], a.rows[0][0][:, h], a.rows[0][1][:, h], a.scale, a.mantissa)
+        over = np.abs(O[:, at] - o) / err
+        assert np.all(over <= 1), (h, over.max())
+        assert np.all(np.abs(lse[:, at] - l) <= lerr)
 
 
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
