@@ -448,10 +448,14 @@ __global__ void __launch_bounds__(kBeamThreads, 2) k_beam_select(const BeamParam
                     keep(lane == 0, BeamPick{score_of(0.f), (uint32_t)row, (uint32_t)P.end_token});
                     continue;
                 }
-                // logits below this do not reach it (or what has to be beaten; exactly: below)
+                // Logits below this do not reach it (or what has to be beaten; exactly: below).  A score was rounded when the logit was added to
+                // `off`, by up to 2^-53 of its size, which is more than all logits where beams have scores like -1e30; so are the
+                // differences here, and 2^-51 of both is more than all of these.
                 auto least_logit = [&]() {
-                    const uint64_t score = worst.score > reach ? worst.score : reach;
-                    return score == 0 ? -FLT_MAX : fmaxf(-FLT_MAX, nextafterf(__double2float_rd((key_score(score) - off) + (double)row_top), -INFINITY));
+                    const uint64_t key = worst.score > reach ? worst.score : reach;
+                    if (key == 0) return -FLT_MAX;
+                    const double score = key_score(key), rounded = (fabs(score) + fabs(off)) * 0x1p-51;
+                    return fmaxf(-FLT_MAX, nextafterf(__double2float_rd((score - off - rounded) + (double)row_top), -INFINITY));
                 };
                 float least = least_logit();
                 const Slice v = slice_of(task);
