@@ -429,8 +429,8 @@ int kvq_page_attn(const kvq_page_cache* cache, const void* Q, void* O, float* ls
  *                 n_out == beams), the token and the score; -1, -1 and -inf where candidates run out
  *   finished_out_opt  dev uint8 [batch][n_out] or NULL: 1 for a beam that had ended, takes end_token or is missing
  * Where n_out == beams, scores_out may be scores and finished_out_opt finished_opt; otherwise no output overlaps an input.
- * Scores are compared in fp64; a beam's sum of exponentials is good to 2^-20 or better, and candidates of different beams that are closer
- * than that may change places.
+ * Scores are compared in fp64; a beam's sum of exponentials is good to 2^-17 at worst and to 2^-22 on ordinary rows, and candidates of
+ * different beams that are closer than that may change places.
  * Candidates whose score is not finite do not count (masked tokens, beams of score -inf; a row with a NaN or +inf has
  * none).  1 <= beams, n_out <= KVQ_MAX_BEAMS; 1 <= vocab <= 2^30.  batch == 0 is a no-op.  One launch.
  */

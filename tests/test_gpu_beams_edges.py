@@ -1,4 +1,5 @@
-"""The selection of beams where single numbers go wrong: scores of great size (GPU)."""
+"""The selection of beams where single numbers go wrong: scores of great size, sums of very many entries, rows that rise from end
+to end (GPU)."""
 import math
 
 import numpy as np
@@ -76,3 +77,40 @@ def test_scores_that_fp64_does_not_tell_apart_are_ties(kq, score):
             parents, tokens, out, _ = _run(kq, z, np.full((2, 3), score, np.float32), None, n, -1)
             assert parents.tolist() == [[3 * b] * n for b in range(2)] and tokens.tolist() == [list(range(n))] * 2
             assert np.all(out == np.float32(score))
+
+
+def _sum_error(kq, z):
+    """How far each beam's logarithm of its sum of exponentials is off, from the scores of its candidates (in fp64 but for their last rounding)."""
+    import torch
+    B, W, V = z.shape
+    parents, tokens, out, _ = _run(kq, z, np.zeros((B, W), np.float32), None, W, -1)
+    worst = 0.0
+    for b in {0, B // 2, B - 1}:
+        x = z[b].double()
+        want = (x - torch.logsumexp(x, 1, keepdim=True)).cpu().numpy()
+        for p, t, s in zip(parents[b], tokens[b], out[b].astype(np.float64)):
+            exact = want[p - b * W, t]
+            worst = max(worst, abs(s - exact) - 2.0 ** -24 * abs(exact))
+    return worst
+
+
+@pytest.mark.parametrize("rise", [0.5, 4.0, 30.0, 400.0])
+@pytest.mark.parametrize("B,W,V", [(1, 32, 1 << 20), (300, 17, 40000), (1, 4, 3000000)])
+def test_sums_of_rows_that_rise_from_end_to_end(kq, B, W, V, rise):
+    """A warp's reference moves up chunk by chunk.  Errors per entry: its distance d to the reference in log2 units three times rounded, 2.25 |d| 2^-24 ln 2,
+    where the mean of |d| is at most log2 V + 6 (entropy, and a reference that lies up to 4 nats low); the exponential's own 2^-22, once more for
+    each of the five or fewer times that the reference moves by 4 and still matters, and for the lanes' join; eight fp32 additions, 8 x 2^-24.  For
+    V = 2^22 that is (2.25 x 0.694 x 28 + 4 x 7 + 8) 2^-24 = 80 x 2^-24."""
+    import torch
+    row = torch.linspace(0, rise, V, device="cuda")
+    z = torch.stack([row + 0.01 * w for w in range(W)])[None].expand(B, W, V).contiguous()
+    assert _sum_error(kq, z) <= 80 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("gap", [9.3, 11.0, 11.7, 12.4, 13.9, 15.3])
+def test_sums_of_flat_rows_under_one_peak(kq, gap):
+    """All entries but one have the same distance from the reference and so the same error: the bound above without moves."""
+    import torch
+    z = torch.full((1, 32, 1 << 20), 0.0, device="cuda") + torch.linspace(-0.3, 0.3, 32, device="cuda")[None, :, None]
+    z[:, :, 777] += gap
+    assert _sum_error(kq, z) <= 60 * 2.0 ** -24
