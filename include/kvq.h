@@ -410,7 +410,8 @@ int kvq_page_append(const kvq_page_cache* cache, const void* K, const void* V, c
  * order in which CTAs run).
  * workspace: dev, 16-byte aligned, at least kvq_page_attn_workspace_bytes (host uint64; KVQ_ERR_NOMEM if less), zero before its
  * first use; every call leaves it ready for the next, of any shape.  Calls that may overlap on the device, captured ones too,
- * need a workspace each.  0 <= batch <= KVQ_MAX_PAGE_ROWS (0 is a no-op), scale finite, table_width >= 1.  One launch.
+ * need a workspace each.  0 <= batch <= KVQ_MAX_PAGE_ROWS (0 is a no-op), scale finite, also in log2 units
+ * (times 1.4427), table_width >= 1.  One launch.
  */
 int kvq_page_attn_workspace_bytes(int batch, int q_heads, int kv_heads, int head_dim, uint64_t* bytes_out);
 int kvq_page_attn(const kvq_page_cache* cache, const void* Q, void* O, float* lse_opt, const int32_t* tables, int table_width,

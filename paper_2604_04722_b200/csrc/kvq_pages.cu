@@ -257,7 +257,9 @@ int kvq_page_attn_workspace_bytes(int batch, int q_heads, int kv_heads, int head
 int kvq_page_attn(const kvq_page_cache* cache, const void* Q, void* O, float* lse_opt, const int32_t* tables, int table_width,
                   const int32_t* lens, int batch, int q_heads, float scale, void* workspace, uint64_t workspace_bytes,
                   void* stream) {
-    if (!cache_ok(cache) || !attn_shape_ok(batch, q_heads, cache->kv_heads, cache->head_dim) || table_width < 1 || !std::isfinite(scale)) return KVQ_ERR_ARG;
+    if (!cache_ok(cache) || !attn_shape_ok(batch, q_heads, cache->kv_heads, cache->head_dim) || table_width < 1) return KVQ_ERR_ARG;
+    const float scale2 = scale * kLog2e;               // (Inf times a product of zero would be NaN)
+    if (!std::isfinite(scale2)) return KVQ_ERR_ARG;
     if (batch == 0) return KVQ_OK;
     if (!Q || !O || !tables || !lens || !workspace || !aligned(Q, 16) || !aligned(O, 16) || !aligned(tables, 4) || !aligned(lens, 4) ||
         !aligned(lse_opt, 4) || !aligned(workspace, 16))
@@ -290,7 +292,7 @@ int kvq_page_attn(const kvq_page_cache* cache, const void* Q, void* O, float* ls
     p.q_heads = q_heads;
     p.kv_heads = cache->kv_heads;
     p.head_blocks = (p.group + 8 * space.nt - 1) / (8 * space.nt);
-    p.scale2 = scale * kLog2e;
+    p.scale2 = scale2;
     p.by_page = FastDiv((uint32_t)cache->page_size);
     p.by_units = FastDiv((uint32_t)(p.kv_heads * p.head_blocks));
     p.by_blocks = FastDiv((uint32_t)p.head_blocks);
