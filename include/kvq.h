@@ -346,7 +346,7 @@ int kvq_verify_tree(const float* target, const float* draft_opt, const int32_t* 
  * Keys and values of one layer lie in n_pages pages of page_size slots; element (page, slot, head, channel) is at
  * K + page * page_stride + slot * slot_stride + head * head_stride + channel (in elements; V the same), so that pages may be kept slot by slot or
  * head by head, and keys and values in one tensor.  K and V dev, 16-byte aligned; strides multiples of 8, not negative.
- * head_dim a multiple of 8 (kvq_page_attn: 64 or 128); dtype KVQ_FP16 or KVQ_BF16.  A request's
+ * head_dim a multiple of 8 up to 1024 (kvq_page_attn: 64 or 128), 1 <= kv_heads <= 1024, n_pages and page_size >= 1; dtype KVQ_FP16 or KVQ_BF16.  A request's
  * row of a block table (int32) lists its pages in order; its token at position t is in slot t % page_size of entry t / page_size.  A page
  * that is not full is listed by one row only; full ones may be shared.
  */
@@ -395,14 +395,15 @@ int kvq_page_step(const int32_t* tables_in, int32_t* tables_out, int table_width
 /*
  * Stores n_new tokens of one layer: K, V dev 16-bit [n_new][kv_heads][head_dim], 16-byte aligned, to slots (dev int64 [n_new]; one
  * outside the cache, such as -1, is passed over).  copies_opt (dev int32 [batch][3] or NULL): what kvq_page_step listed; the
- * first slots of a page are copied to another page in the same launch.  A slot may be given once.
+ * first slots of a page are copied to another page in the same launch.  A slot may be given once.  n_new, batch >= 0, n_new + batch < 2^31;
+ * with copies batch <= KVQ_MAX_PAGE_ROWS.  One launch, none if there is nothing to store or copy.
  */
 int kvq_page_append(const kvq_page_cache* cache, const void* K, const void* V, const int64_t* slots, int n_new,
                     const int32_t* copies_opt, int batch, void* stream);
 
 /*
  * Attention of one new token per request over its pages: O = Softmax(scale * q K^T) V over the first lens[b] tokens, query head h
- * reading KV head h / (q_heads / kv_heads).  Q, O: dev [batch][q_heads][head_dim] of the cache's type, 16-byte aligned
+ * reading KV head h / (q_heads / kv_heads); kv_heads divides q_heads <= 16384.  Q, O: dev [batch][q_heads][head_dim] of the cache's type, 16-byte aligned
  * (O may be Q); lse_opt dev fp32 [batch][q_heads] or NULL: the logarithm of the sum of exponentials.  A row of length 0 (or less) gets zeros and
  * -inf; lengths beyond the table count as its width.  Slots behind a row's length may hold anything, and tokens on pages outside
  * the cache (such as -1) do not take part.  A value that is not finite makes NaN of its channel, and a key that is not of the
@@ -433,7 +434,7 @@ int kvq_page_attn(const kvq_page_cache* cache, const void* Q, void* O, float* ls
  * Scores are compared in fp64; a beam's sum of exponentials is good to 2^-17 at worst and to 2^-22 on ordinary rows, and candidates of
  * different beams that are closer than that may change places.
  * Candidates whose score is not finite do not count (masked tokens, beams of score -inf; a row with a NaN or +inf has
- * none).  1 <= beams, n_out <= KVQ_MAX_BEAMS; 1 <= vocab <= 2^30.  batch == 0 is a no-op.  One launch.
+ * none).  1 <= beams, n_out <= KVQ_MAX_BEAMS; 1 <= vocab <= 2^30; 0 <= batch <= 2^24 (0 is a no-op).  One launch.
  */
 #define KVQ_MAX_BEAMS 32
 int kvq_beam_select(const void* logits, int dtype, const float* scores, const uint8_t* finished_opt, int batch, int beams,
