@@ -406,9 +406,10 @@ int kvq_page_append(const kvq_page_cache* cache, const void* K, const void* V, c
  * reading KV head h / (q_heads / kv_heads); kv_heads divides q_heads <= 16384.  Q, O: dev [batch][q_heads][head_dim] of the cache's type, 16-byte aligned
  * (O may be Q); lse_opt dev fp32 [batch][q_heads] or NULL: the logarithm of the sum of exponentials.  A row of length 0 (or less) gets zeros and
  * -inf; lengths beyond the table count as its width.  Slots behind a row's length may hold anything, and tokens on pages outside
- * the cache (such as -1) do not take part.  A value that is not finite makes NaN of its channel, and a key that is not of the
- * whole row, in the heads that read it.  Sums are fp32; equal calls give equal bits (the cut of the work does not depend on the
- * order in which CTAs run).
+ * the cache (such as -1) do not take part.  What is not finite counts as the formula has it, logit by logit (fp32; larger ones overflow): one of
+ * NaN or +Inf makes NaN of its head's row, one of -Inf (an infinite channel of a key, by the query's sign) has a weight of zero, and a row of nothing
+ * else is as one of length 0.  A value of Inf or NaN makes its channel Inf or NaN in the heads that read it.  Sums are fp32; equal calls
+ * give equal bits (the cut of the work does not depend on the order in which CTAs run).
  * workspace: dev, 16-byte aligned, at least kvq_page_attn_workspace_bytes (host uint64; KVQ_ERR_NOMEM if less), zero before its
  * first use; every call leaves it ready for the next, of any shape.  Calls that may overlap on the device, captured ones too,
  * need a workspace each.  0 <= batch <= KVQ_MAX_PAGE_ROWS (0 is a no-op), scale finite, also in log2 units

@@ -1,5 +1,5 @@
-"""The paged attention where single numbers go wrong: weights far below the largest, logits of great size (GPU)."""
-not finite, what is left in the workspace (GPU)."""
+"""The paged attention where single numbers go wrong: weights far below the largest, logits of great size, keys and values that are
+not finite (GPU)."""
 import math
 
 import numpy as np
@@ -97,3 +97,38 @@ def test_attention_with_logits_whose_steps_are_as_large_as_the_slack(kq, power, 
     torch.cuda.synchronize()
     O = a.O.float()
     assert torch.isfinite(a.lse).all() and torch.isfinite(O).all() and O.min() >= 1.0 and O.max() <= 2.0
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("lens", [[200, 200, 200], [200, 16, 9000], [1, 1, 1]])
+def test_attention_of_infinite_keys_and_values(kq, lens, D, dtype):
+    """By the sign of a query's channel a key of +-Inf gives its heads a logit of +Inf (NaN) or -Inf (a weight of zero)."""
+    import torch
+    a = Attn(kq, lens, 6, 2, D, 16, dtype, seed=D)
+    a.Q[:, :, 7] = torch.tensor([1.0, -1.0, 2.0, 1.0, 1.0, -3.0], device="cuda")        # heads 0 to 2 read KV head 0, 3 to 5 the other
+    at = lambda b, t: (int(a.tables[b, t // 16]), t % 16)
+    last = [n - 1 for n in lens]
+    a.K[at(0, last[0]) + (0, 7)] = math.inf
+    a.K[at(1, last[1]) + (1, 7)] = -math.inf
+    a.V[at(2, last[2]) + (0, 3)] = math.inf
+    a.V[at(2, last[2]) + (0, 5)] = -math.inf
+    a.call()
+    torch.cuda.synchronize()
+    O, lse = a.O.double().cpu().numpy(), a.lse.double().cpu().numpy()
+    gone = {(0, 0): False, (0, 1): True, (0, 2): False, (1, 3): True, (1, 4): True, (1, 5): False}          # True: without that token
+    for b, n in enumerate(lens):
+        k, v = a.rows[b]
+        for h in range(6):
+            g = h // 3
+            if gone.get((b, h)) is False:
+                assert np.all(np.isnan(O[b, h])) and math.isnan(lse[b, h]), (b, h)
+                continue
+            kk, vv = (x[:-1, g] if (b, h) in gone else x[:, g] for x in (k, v))
+            o, l, err, lerr = pr.attend(a.Q[b, h:h + 1].double().cpu().numpy(), kk, vv, a.scale, a.mantissa)
+            some = np.ones(D, bool)
+            if b == 2 and g == 0:
+                some[[3, 5]] = False
+                assert not np.isfinite(O[b, h, [3, 5]]).any()
+            assert np.all(np.abs(O[b, h, some] - o[0, some]) <= err[0, some]), (b, h)
+            assert lse[b, h] == l[0] or abs(lse[b, h] - l[0]) <= lerr[0]
