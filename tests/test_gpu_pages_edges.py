@@ -1,5 +1,5 @@
 """The paged attention where single numbers go wrong: weights far below the largest, logits of great size, keys and values that are
-not finite (GPU)."""
+not finite, what is left in the workspace (GPU)."""
 import math
 
 import numpy as np
@@ -132,3 +132,17 @@ def test_attention_of_infinite_keys_and_values(kq, lens, D, dtype):
                 assert not np.isfinite(O[b, h, [3, 5]]).any()
             assert np.all(np.abs(O[b, h, some] - o[0, some]) <= err[0, some]), (b, h)
             assert lse[b, h] == l[0] or abs(lse[b, h] - l[0]) <= lerr[0]
+
+
+def test_what_a_call_leaves_in_its_workspace(kq):
+    """The arrival counters, 4096 bytes, are back at zero; records behind them may hold anything.  (Units as long as 1.3 warps' shares: CTA 0's
+    second warp ends one that the first began and goes on.)"""
+    a = Attn(kq, [320] * 600, 3, 3, 64, 16)
+    a.work[4096:] = 255
+    for _ in range(3):
+        a.call()
+    o = a.O.clone()
+    assert not a.work[:4096].any()
+    assert (a.work[6208:6208 + 2112] != 255).any()     # the record of CTA 0's second warp (8 heads of 66 floats)
+    a.call()
+    assert o.equal(a.O) and o.isfinite().all()
