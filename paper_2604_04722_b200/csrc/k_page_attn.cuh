@@ -139,8 +139,10 @@ __global__ void __launch_bounds__(AttnGeom<D, W>::kThreads, AttnGeom<D, W>::kCta
     // decide the output while the sum of weights counts them.  So the reference lies 2^7 below the largest weight (with the slack 2^15 at most),
     // and the second number of a weight is kept 2^11 times as large, which the values that it is multiplied with make up for: a weight is cut at
     // 2^-43 of the largest.  (Four multiplications for every 16 x 16 values: 16 x 8192 tokens 174.4 us, without 173.3, 32 of up to 8192 with 16 heads
-    // per KV head 51.8 and 51.7; a sum of its own for the second product 65.3 there.)  bf16 reaches as far as fp32.
-    constexpr float kHead = BF ? 0.f : 7.f, kMost = kRescaleSlack + kHead, kSecond = BF ? 1.f : 2048.f;
+    // per KV head 51.8 and 51.7; a sum of its own for the second product 65.3 there.)  bf16 weights
+    // reach as far down as fp32, but so do the values upwards: the reference lies 2^8 above the largest weight, so that with the slack none passes one
+    // and what is summed is no larger than n values.
+    constexpr float kHead = BF ? -kRescaleSlack : 7.f, kMost = kRescaleSlack + kHead, kSecond = BF ? 1.f : 2048.f;
     constexpr int kMt = D / 16, kR = 8 * NT, kStages = G::kStages, kAttnWarps = G::kWarps, kAttnThreads = G::kThreads, kWarpsLog2 = W == 8 ? 3 : 4;
     namespace cg = cooperative_groups;
     // (powers of two throughout: a division of integers takes longer than all else between two round trips to memory)

@@ -1,5 +1,5 @@
-"""The paged attention where single numbers go wrong: weights far below the largest, logits of great size, keys and values that are
-not finite, what is left in the workspace (GPU)."""
+"""The paged attention where single numbers go wrong: weights far below the largest, logits and values of great size, keys and values
+that are not finite, what is left in the workspace (GPU)."""
 import math
 
 import numpy as np
@@ -146,3 +146,28 @@ def test_what_a_call_leaves_in_its_workspace(kq):
     assert (a.work[6208:6208 + 2112] != 255).any()     # the record of CTA 0's second warp (8 heads of 66 floats)
     a.call()
     assert o.equal(a.O) and o.isfinite().all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("lens", [[320], [320] * 700, [9000]])
+@pytest.mark.parametrize("step", [0.5, 3.0, 5.5, 7.0])
+def test_attention_of_very_large_values(kq, step, lens, D):
+    """bf16 values near 2^120 under logits that rise from tile to tile: no weight may exceed one, or the sums pass fp32."""
+    import torch
+    a = Attn(kq, [lens[0]], 4, 2, D, 16, "bf16", seed=D)
+    n, where = lens[0], a.tables[0, :-(-lens[0] // 16)].long()
+    a.Q = torch.zeros((1, 4, D), dtype=torch.bfloat16, device="cuda")
+    a.Q[..., 0], a.scale = 1.0, 1.0
+    k = torch.zeros((len(where) * 16, 2, D), device="cuda")
+    k[:, :, 0] = (torch.arange(len(k), device="cuda") // 16 % 8)[:, None] * step       # (rises and falls)
+    v = (torch.rand(k.shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)) + 1.0) * 2.0 ** 120
+    v[:] *= torch.where(torch.arange(len(k), device="cuda") < 64, 1.0, 2.0 ** -12)[:, None, None]
+    for c, x in ((a.K, k), (a.V, v)):
+        c[where] = x.bfloat16().reshape(len(where), 16, 2, D)
+    a.rows = [[c[where].reshape(-1, 2, D)[:n].double().cpu().numpy() for c in (a.K, a.V)]]
+    rows = len(lens)
+    a.Q, a.tables, a.n, a.lens = a.Q.repeat(rows, 1, 1), a.tables.repeat(rows, 1).contiguous(), a.n.repeat(rows), lens
+    a.O, a.lse = torch.full_like(a.Q, float("nan")), torch.full((rows, 4), float("nan"), device="cuda")
+    a.rows, a.live = a.rows * rows, a.live * rows
+    a.call()
+    a.check(pairs={(b, h) for b in range(0, rows, 50) for h in range(2)})
