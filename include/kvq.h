@@ -435,7 +435,7 @@ int kvq_page_attn(const kvq_page_cache* cache, const void* Q, void* O, float* ls
  * Scores are compared in fp64; a beam's sum of exponentials is good to 2^-17 at worst and to 2^-22 on ordinary rows, and candidates of
  * different beams that are closer than that may change places.
  * Candidates whose score is not finite do not count (masked tokens, beams of score -inf; a row with a NaN or +inf has
- * none).  1 <= beams, n_out <= KVQ_MAX_BEAMS; 1 <= vocab <= 2^30; 0 <= batch <= 2^24 (0 is a no-op).  One launch.
+ * none); finite means in fp64, and a score below fp32's range is returned as -inf.  1 <= beams, n_out <= KVQ_MAX_BEAMS; 1 <= vocab <= 2^30; 0 <= batch <= 2^24 (0 is a no-op).  One launch.
  */
 #define KVQ_MAX_BEAMS 32
 int kvq_beam_select(const void* logits, int dtype, const float* scores, const uint8_t* finished_opt, int batch, int beams,

@@ -11,9 +11,9 @@
 // those only the entries that reach it are kept, a few more than n in all.  A CTA ranks its own, sends its n best to the first
 // CTA (a second barrier), and that ranks them.  Scores are compared in fp64.
 //
-// Bound: of many requests the loop over the logits: an exponential each, and the instructions around it (64 requests of 16 beams over
-// 32000 bf16 logits: 25.5 us, the bytes alone 10; the exponentials are 7 of it; over 32003, where rows are not aligned and every load becomes
-// two, 32).  Of few requests the chain of the rows' loads, two cluster barriers, the bound, a second read and two rankings: 9.1 us for
+// Bound: of many requests instructions and the barriers between the phases: 64 requests of 16 beams over 32000 bf16 logits take 25.5 us,
+// the bytes alone 10; over 32003, where rows are not aligned and every load becomes two, 32, of which the loop over the logits is 17 (five to six
+// instructions a logit; with what lies behind it 20, issue slots half busy).  Of few requests the chain of the rows' loads, two cluster barriers, the bound, a second read and two rankings: 9.1 us for
 // one request of 4 beams over 49152 logits.  Keeping the slices' best entries in the first pass took 94 us where this takes 32.
 #pragma once
 #include <cooperative_groups.h>

@@ -11,7 +11,7 @@
 // o^T = V^T w^T with the channels as rows, so that up to 8 query heads cost the same as one, K and V fragments are read with one
 // ldmatrix per 16 x 16 block, and the weights of a tile become the second product's operand with one 8 x 8 transposition per
 // eight tokens.  A weight enters as the sum of two 16-bit numbers (what the first loses the second holds): next to the rows'
-// bytes the second product costs little (16 x 8192 tokens 1.3 of 174 us, 8 x 4001 0.4 of 11.5), and with 8-bit mantissas (bf16) one rounding of the weights would be as large as the
+// bytes the second product costs little (16 x 8192 fp16 tokens 2.4 of 174 us, 8 x 4001 bf16 ones 0.4 of 11.5), and with 8-bit mantissas (bf16) one rounding of the weights would be as large as the
 // output's own.  Sums are fp32.
 //
 // A unit that begins and ends with one warp is written by that warp.  Pieces of a unit meet in their CTA.  Where there are few
@@ -20,8 +20,8 @@
 // more units than that, CTAs take equal shares of the axis, a share's border moves to a unit's if that is near, and what is left over
 // meets in records of the workspace: the CTA that delivers a unit's last record joins them, in the order of the axis whoever comes last.
 //
-// Bound: the rows' bytes, 4 D per token and KV head.  1.07 GB of 32 heads of 64 channels (16 x 8192 tokens, fp16, slot by slot) take 173 us,
-// 6.2 TB/s or 0.94 of the copy rate; 0.79 GB of 8 heads of 128 (64 x 4096 at most, bf16) 133 us, 0.90.  Small calls are a chain of memory
+// Bound: the rows' bytes, 4 D per token and KV head.  1.07 GB of 32 heads of 64 channels (16 x 8192 tokens, fp16, slot by slot) take 171 to 177 us,
+// 6.1 to 6.3 TB/s or 0.92 to 0.96 of the copy rate; 0.79 GB of 8 heads of 128 (64 x 4096 at most, bf16) 133 us, 0.90.  Small calls are a chain of memory
 // round trips (lengths, tables, rows), a tile's dependent instructions and the joins: 1 x 512 tokens 6.4 us.
 #pragma once
 #include <cooperative_groups.h>

@@ -114,3 +114,13 @@ def test_sums_of_flat_rows_under_one_peak(kq, gap):
     z = torch.full((1, 32, 1 << 20), 0.0, device="cuda") + torch.linspace(-0.3, 0.3, 32, device="cuda")[None, :, None]
     z[:, :, 777] += gap
     assert _sum_error(kq, z) <= 60 * 2.0 ** -24
+
+
+def test_scores_below_the_range_of_fp32(kq):
+    """A candidate counts while its score is finite in fp64; it is returned as -inf, with its beam and token, if fp32 does not hold it."""
+    import torch
+    low = float(np.finfo(np.float32).min)
+    z = torch.tensor([[[low, 1.0, -math.inf, 0.5, low]]], device="cuda")
+    parents, tokens, out, over = _run(kq, z, np.full((1, 1), low, np.float32), None, 6, 3)
+    assert tokens[0].tolist() == [1, 3, 0, 4, -1, -1] and parents[0].tolist() == [0, 0, 0, 0, -1, -1] and over[0].tolist() == [0, 1, 0, 0, 1, 1]
+    assert out[0].tolist() == [low, low] + [-math.inf] * 4
